@@ -367,6 +367,32 @@ int gnnfd_layer_gat(const gnnfd_csr_t* csr, const void* d_x, int64_t ldx, gnnfd_
                     const float* d_a_dst, float negative_slope, int mode, void* d_out, int64_t ldo, gnnfd_dtype_t odt,
                     int32_t chunk_width, void* d_scratch, size_t scratch_bytes, int32_t* d_status, void* stream);
 
+/* ------------------------------------------------------------------ learned vertex features
+ *
+ * For graphs whose vertices have no features of their own (or a type, a degree, a name instead): a table with a learned row per
+ * id, looked up ahead of the first layer, and the table's gradient for its training.  (The paper's graphs come with features.)
+ *
+ * gnnfd_embedding: out[i, :] = scale * table[ids[i], :] for i < n (n may be 0).  d_ids [n] of type itype; d_table [vocab, ldt] of type tdt;
+ * d_out [n, ldo] of type odt, not overlapping the table.  An id outside [0, vocab) gives a row of zeros and sets bit 0 of
+ * *d_status (d_status may be NULL; the caller has set it to 0).
+ *
+ * gnnfd_embedding_backward: grad[r, :] = scale * sum of dout[i, :] over the i with ids[i] == r, for all vocab rows; rows that no id
+ * names become 0.  Sums are fp32 in an order that depends on the ids alone: equal inputs give equal bits.  With accumulate != 0 the
+ * sums are added to what d_grad holds (of type gdt, rounded once) and rows that no id names are left as they are.  Ids equal to `padding`
+ * (-1: none) take no part: their row is treated as one that no id names.  Ids outside [0, vocab) take no part and set bit 0 of *d_status;
+ * bit 1 is set if a block of the sort gave up waiting for another one (grad is then incomplete).  d_dout [n, ldd] of type ddt;
+ * d_grad [vocab, ldg], not overlapping it.  d_scratch: gnnfd_embedding_backward_workspace_bytes(n, vocab, f) bytes, 256-byte
+ * aligned (0 bytes up to 8192 ids, NULL is then accepted).  Both calls only enqueue work. */
+int gnnfd_embedding(int64_t n, const void* d_ids, gnnfd_itype_t itype, int64_t vocab, const void* d_table, int64_t ldt,
+                    gnnfd_dtype_t tdt, int32_t f, float scale, void* d_out, int64_t ldo, gnnfd_dtype_t odt, int32_t* d_status,
+                    void* stream);
+
+int gnnfd_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int32_t f, size_t* scratch_bytes);
+
+int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, const void* d_dout, int64_t ldd, gnnfd_dtype_t ddt,
+                             int64_t vocab, int32_t f, float scale, int64_t padding, int accumulate, void* d_grad, int64_t ldg,
+                             gnnfd_dtype_t gdt, void* d_scratch, size_t scratch_bytes, int32_t* d_status, void* stream);
+
 /* ------------------------------------------------------------------ diagnostics */
 
 const char* gnnfd_status_string(int status);
@@ -393,8 +419,8 @@ int gnnfd_kernel_timing_read(const char** names, double* ms, int64_t* launches, 
  * incomplete. */
 int gnnfd_debug_combine_fault(int64_t wait_ns, int32_t skip_k_block);
 
-/* Drill of the CSR build's give-up path, for tests.  It arms the NEXT gnnfd_build_csr or gnnfd_oneshot_* call made by this host
- * thread, and only that one: a block of the sort gives up after max_polls reads (rounded up to 256; 0 keeps the usual million)
+/* Drill of the CSR build's give-up path, for tests.  It arms the NEXT gnnfd_build_csr, gnnfd_oneshot_* or gnnfd_embedding_backward
+ * (digits only; it reports through *d_status) call made by this host thread, and only that one: a block of the sort gives up after max_polls reads (rounded up to 256; 0 keeps the usual million)
  * of a word that another block has not written yet, and in sweep `sweep` (0 ..: the digits; one past the last digit: the row
  * order; two past it, in gnnfd_oneshot_* calls without duplicate removal: the row pointers' sums) nobody takes the first tile, so all others wait for it and give up.  The kernels that follow do nothing, the
  * call returns GNNFD_CUDA_ERROR and no handle, nothing outside the call's buffers is touched and the device stays usable.

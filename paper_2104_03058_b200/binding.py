@@ -83,6 +83,9 @@ def lib() -> ctypes.CDLL:
         L.gnnfd_layer_sage.argtypes = layer
         L.gnnfd_layer_gat.argtypes = [vp, vp, i64, i32, i32, vp, i64, i32, i32, vp, vp, fl, ctypes.c_int, vp, i64, i32, i32,
                                       vp, sz, vp, vp]
+        L.gnnfd_embedding.argtypes = [i64, vp, i32, i64, vp, i64, i32, i32, fl, vp, i64, i32, vp, vp]
+        L.gnnfd_embedding_backward_workspace_bytes.argtypes = [i64, i64, i32, pp(sz)]
+        L.gnnfd_embedding_backward.argtypes = [i64, vp, i32, vp, i64, i32, i64, i32, fl, i64, ctypes.c_int, vp, i64, i32, vp, sz, vp, vp]
         L.gnnfd_debug_combine_fault.argtypes = [i64, i32]
         L.gnnfd_debug_build_fault.argtypes = [i32, i32]
         L.gnnfd_status_string.argtypes = [ctypes.c_int]
@@ -684,6 +687,123 @@ def layer(csr: Csr, model: str, x: torch.Tensor, w_t: torch.Tensor, f_in: int | 
         fn = lib().gnnfd_layer_gcn if model == "gcn" else lib().gnnfd_layer_sage
         _check(fn(csr.handle, xp, ldx, _dtype_code(x), f_in, wp, ldw, f_out, _combine_mode(mode), op, ldo,
                   _dtype_code(out), chunk_width, scr, scr_n, sp, _stream_ptr(stream)), "gnnfd_layer_" + model)
+    return out
+
+
+def _on_device(t: torch.Tensor, stream, work):
+    """work(stream handle) with the device of `t` current: kernels are launched on the current device, and the stream handed over is
+    that device's current one where none is named."""
+    index = t.device.index
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, t.device))
+        handle = stream.cuda_stream
+    else:
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
+        return work(handle)
+    with torch.cuda.device(index):
+        return work(handle)
+
+
+def _take(make, stream):
+    """Memory that a call allocates: taken under the stream the work runs on (see _alloc_bytes)."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _index_list(ids: torch.Tensor, name: str):
+    """(contiguous ids, count, type code) of a 1-D device tensor of ids."""
+    if not ids.is_cuda or ids.dim() != 1:
+        raise ValueError("%s must be a 1-D CUDA tensor" % name)
+    if ids.dtype == torch.int32:
+        code = I32
+    elif ids.dtype == torch.int64:
+        code = I64
+    else:
+        raise TypeError("%s must be int32 or int64" % name)
+    if not ids.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return ids.data_ptr(), ids.shape[0], code
+
+
+def _status_ptr(status, device):
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.numel() < 1 or status.device != device:
+        raise ValueError("status must be an int32 tensor on %s" % device)
+    return status.data_ptr()
+
+
+def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int | None = None, out: torch.Tensor | None = None,
+              out_dtype=None, status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """gnnfd_embedding: out[i] = scale * table[ids[i], :f].  ``status`` is an int32 tensor of one element whose bit 0 the kernel sets
+    where an id lies outside the table (its output row is zero)."""
+    f = table.shape[1] if f is None else f
+    ip, n, itype = _index_list(ids, "ids")
+    tp, ldt = _matrix(table, f, "table")
+    fresh = out is None
+    if fresh:
+        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=table.device), stream)
+    op, ldo = _matrix(out, f, "out")
+    if ids.device != table.device or out.device != table.device:
+        raise ValueError("table, ids and out must be on one device")
+    if not fresh:
+        _need_ids(out, n, "out")
+        _no_overlap(table, out, "table", "out")
+        _no_overlap(ids, out, "ids", "out")
+    sp = _status_ptr(status, table.device)
+    tdt, odt = _dtype_code(table), _dtype_code(out)
+    _on_device(table, stream, lambda s: _check(lib().gnnfd_embedding(n, ip, itype, table.shape[0], tp, ldt, tdt, f, scale, op, ldo, odt, sp, s),
+                                               "gnnfd_embedding"))
+    return out
+
+
+def _need_ids(t, n: int, name: str):
+    if t.shape[0] < n:
+        raise ValueError("%s has %d rows for %d ids" % (name, t.shape[0], n))
+
+
+def embedding_backward_workspace_bytes(n: int, vocab: int, f: int) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_embedding_backward_workspace_bytes(n, vocab, f, ctypes.byref(s)), "gnnfd_embedding_backward_workspace_bytes")
+    return s.value
+
+
+def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale: float = 1.0, padding_idx: int | None = None,
+                       accumulate: bool = False, f: int | None = None, out: torch.Tensor | None = None, out_dtype=None, scratch=None,
+                       status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """gnnfd_embedding_backward: the gradient [vocab, f] of a table from the gradients of the rows looked up.  ``accumulate`` adds to
+    ``out`` (which must then be given); ids equal to ``padding_idx`` take no part; ``status``: see the header."""
+    f = dout.shape[1] if f is None else f
+    ip, n, itype = _index_list(ids, "ids")
+    dp, ldd = _matrix(dout, f, "dout")
+    _need_ids(dout, n, "dout")
+    fresh = out is None
+    if fresh:
+        if accumulate:
+            raise ValueError("accumulate needs the gradient to add to (out)")
+        out = _take(lambda: torch.empty((vocab, f), dtype=out_dtype or torch.float32, device=dout.device), stream)
+    op, ldo = _matrix(out, f, "out")
+    if ids.device != dout.device or out.device != dout.device:
+        raise ValueError("ids, dout and out must be on one device")
+    if not fresh:
+        if out.shape[0] < vocab:
+            raise ValueError("out has %d rows, the table has %d" % (out.shape[0], vocab))
+        _no_overlap(dout, out, "dout", "out")
+        _no_overlap(ids, out, "ids", "out")
+    if scratch is None:
+        need = embedding_backward_workspace_bytes(n, vocab, f)
+        scratch = _alloc_bytes(need, dout.device, stream) if need else None
+    scr, scr_n = _scratch_args(scratch, dout.device)
+    sp = _status_ptr(status, dout.device)
+    padding = -1 if padding_idx is None else padding_idx
+    ddt, odt = _dtype_code(dout), _dtype_code(out)
+    _on_device(dout, stream, lambda s: _check(lib().gnnfd_embedding_backward(n, ip, itype, dp, ldd, ddt, vocab, f, scale, padding,
+                                                                             int(accumulate), op, ldo, odt, scr, scr_n, sp, s),
+                                              "gnnfd_embedding_backward"))
     return out
 
 

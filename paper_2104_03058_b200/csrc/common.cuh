@@ -144,6 +144,23 @@ int csr_sizes(int64_t n, int64_t e, uint32_t flags, bool for_smaller, size_t* pe
 int build_csr_impl(int64_t n, int64_t e, const void* d_src, const void* d_dst, gnnfd_itype_t itype, uint32_t flags, bool need_perm,
                    bool need_weights, void* d_persistent, size_t persistent_bytes, void* d_scratch, size_t scratch_bytes, cudaStream_t s,
                    gnnfd_csr_t** out);                                // csr_build.cu
+
+// Ids sorted with their positions (csr_build.cu): words id << val_bits | position + 1 in ascending order, ids outside [0, vocab) last (there are
+// counts->n_valid others).  Where counts->sort_failed is set the words mean nothing.
+struct SortedIds {
+    unsigned long long *words, *other;
+    BuildCounts* counts;
+    int32_t *digit_count, *ticket;
+    uint8_t* extra;                    // so many bytes of the caller's, zeroed with the rest
+    uint32_t *published, *published_alt;
+    size_t zero_bytes;
+    int val_bits;
+};
+struct SortDrill { int max_polls, sweep; };
+SortDrill take_sort_drill();           // what gnnfd_debug_build_fault armed on this thread (sweep -1: nothing)
+int carve_sorted_ids(Carver& c, int64_t n, int64_t vocab, size_t extra, SortedIds* p);
+int sort_ids(int64_t n, int64_t vocab, const void* d_ids, gnnfd_itype_t itype, const SortDrill& drill, SortedIds& p, cudaStream_t s);
+
 int combine_impl(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f_in, const void* d_w_t, int64_t ldw,
                  int32_t f_out, void* d_z, int64_t ldz, gnnfd_dtype_t zdt, int mode, const float* d_a_src,
                  const float* d_a_dst, int32_t heads, int32_t dim, float* d_s_src, float* d_s_dst, int32_t* d_status,

@@ -1488,8 +1488,13 @@ static int launch_edge_sweep(bool has_vals, bool entries, SweepArgs& a, cudaStre
 }
 
 // One-shot settings of the drill (see gnnfd_debug_build_fault): consumed by the next build on this thread.
-struct BuildDrill { int max_polls, sweep; };
-static thread_local BuildDrill t_drill = {kMaxPolls, -1};
+static thread_local SortDrill t_drill = {kMaxPolls, -1};
+SortDrill take_sort_drill()
+{
+    const SortDrill drill = t_drill;
+    t_drill = SortDrill{kMaxPolls, -1};
+    return drill;
+}
 
 // need_perm, need_weights: whether the caller looks at perm and edge_w (their places are left as they are where not).  Edge ids that nobody
 // needs do not travel through the sort, unless duplicates are removed, where the order among them decides.
@@ -1497,8 +1502,7 @@ int build_csr_impl(int64_t n, int64_t e, const void* d_src, const void* d_dst, g
                    bool need_weights, void* d_persistent, size_t persistent_bytes, void* d_scratch, size_t scratch_bytes, cudaStream_t s,
                    gnnfd_csr_t** out)
 {
-    const BuildDrill drill = t_drill;
-    t_drill = BuildDrill{kMaxPolls, -1};
+    const SortDrill drill = take_sort_drill();
     if (!out) return GNNFD_INVALID_ARG;
     *out = nullptr;
     BuildLayout L;
@@ -1705,6 +1709,80 @@ int build_csr_impl(int64_t n, int64_t e, const void* d_src, const void* d_dst, g
     return GNNFD_OK;
 }
 
+// ------------------------------------------------------------------ ids sorted with their positions
+
+// Words id << val_bits | position + 1 share 64 bits for any number of ids below 2^31.
+struct IdLayout { int val_bits, passes, digit_bits; };
+static int id_layout(int64_t n, int64_t vocab, IdLayout* L)
+{
+    if (n <= 0 || vocab <= 0) return GNNFD_INVALID_ARG;
+    if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
+    int key_bits = 1;
+    while ((int64_t(1) << key_bits) < vocab + 1) ++key_bits;              // vocab itself marks ids out of range
+    L->val_bits = 1;
+    while ((int64_t(1) << L->val_bits) < n + 1) ++L->val_bits;
+    L->passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits;
+    L->digit_bits = (key_bits + L->passes - 1) / L->passes;
+    return GNNFD_OK;
+}
+
+int carve_sorted_ids(Carver& c, int64_t n, int64_t vocab, size_t extra, SortedIds* p)
+{
+    IdLayout L;
+    const int rc = id_layout(n, vocab, &L);
+    if (rc) return rc;
+    p->words = c.take<u64>((size_t)n);
+    p->other = c.take<u64>((size_t)n);
+    const size_t zero_begin = c.off;
+    p->counts = c.take<BuildCounts>(1);
+    p->digit_count = c.take<int32_t>((size_t)L.passes * kRadix);
+    p->ticket = c.take<int32_t>((size_t)L.passes);
+    p->extra = c.take<uint8_t>(extra);
+    p->published = c.take<uint32_t>((size_t)kRadix * sweep_tiles(n));
+    p->zero_bytes = c.off - zero_begin;
+    p->published_alt = c.take<uint32_t>((size_t)kRadix * sweep_tiles(n));
+    p->val_bits = L.val_bits;
+    return GNNFD_OK;
+}
+
+// The sort of the build, run over the ids alone: an id is both ends of an edge whose key has no bits for the source, so key and
+// candidate number are id and position, and ids outside [0, vocab) take the place of dropped edges.
+int sort_ids(int64_t n, int64_t vocab, const void* d_ids, gnnfd_itype_t itype, const SortDrill& drill, SortedIds& p, cudaStream_t s)
+{
+    IdLayout L;
+    int rc = id_layout(n, vocab, &L);
+    if (rc) return rc;
+    if (drill.sweep >= 0 && (drill.sweep >= L.passes || sweep_tiles(n) < 2)) return GNNFD_INVALID_ARG;
+    GNNFD_CUDA_CHECK(cudaMemsetAsync(p.counts, 0, p.zero_bytes, s));
+    if (drill.sweep >= 0) GNNFD_CUDA_CHECK(cudaMemsetAsync(p.ticket + drill.sweep, 1, 1, s));      // tile 0 is never drawn
+    SweepArgs sw{};
+    sw.cand = Candidates{d_ids, d_ids, vocab, n, n, 0u, 0};
+    sw.m = n;
+    sw.val_bits = L.val_bits;
+    sw.counts = p.counts;
+    sw.max_polls = drill.max_polls;
+    sw.mask = (1 << L.digit_bits) - 1;
+    const unsigned walkers = blocks_for(n, kHistTile) < 6u * kSmCount ? blocks_for(n, kHistTile) : 6u * kSmCount;
+    GNNFD_LAUNCH("edge_histograms", s, itype == GNNFD_I32 ? histogram_kernel<int32_t>(L.passes) : histogram_kernel<long long>(L.passes), walkers,
+                 kThreads, (size_t)L.passes * kRadix * sizeof(int32_t), sw.cand, 0, L.digit_bits, L.passes, p.digit_count, p.counts);
+    for (int pass = 0; pass < L.passes; ++pass) {
+        sw.shift = pass * L.digit_bits + L.val_bits;
+        sw.digit_count = p.digit_count + (size_t)pass * kRadix;
+        sw.ticket = p.ticket + pass;
+        sw.published = p.published;
+        sw.published_next = pass + 1 == L.passes ? nullptr : p.published_alt;
+        sw.keys_in = p.words;
+        sw.keys_out = p.other;
+        if (pass > 0) rc = launch_edge_sweep<kWords>(false, false, sw, s);
+        else if (itype == GNNFD_I32) rc = launch_edge_sweep<kEdges32>(false, false, sw, s);
+        else rc = launch_edge_sweep<kEdges64>(false, false, sw, s);
+        if (rc) return rc;
+        std::swap(p.words, p.other);
+        std::swap(p.published, p.published_alt);
+    }
+    return GNNFD_OK;
+}
+
 static size_t scratch_size(const BuildLayout& L)
 {
     Carver c(nullptr, ~size_t(0));
@@ -1765,7 +1843,7 @@ int gnnfd_debug_build_fault(int32_t max_polls, int32_t sweep)
 {
     using namespace gnnfd;
     if (max_polls < 0 || max_polls > kMaxPolls || sweep < 0) return GNNFD_INVALID_ARG;
-    t_drill = BuildDrill{max_polls ? max_polls : kMaxPolls, sweep};
+    t_drill = SortDrill{max_polls ? max_polls : kMaxPolls, sweep};
     return GNNFD_OK;
 }
 

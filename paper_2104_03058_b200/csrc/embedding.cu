@@ -1,0 +1,688 @@
+// Learned vertex features: rows of a table looked up by id and scaled, and the table's gradient as sums over the sorted ids.
+//
+//   out[i, :] = scale * table[ids[i], :]
+//   grad[r, :] = scale * (dout rows of the ids i with ids[i] == r, added in ascending i), all rows of the table
+//
+// Neither does arithmetic worth counting: both are bound by HBM (the lookup reads n rows and writes n rows, the gradient
+// reads n rows and writes `vocab` rows), or by latency on small batches.
+#include "schedule.cuh"
+#include "vec.cuh"
+
+namespace gnnfd {
+
+constexpr int kEmbedBlock = 256;
+constexpr unsigned kSms = 148;
+
+// V elements of T with one load or store (16, 8, 4 or 2 bytes), as fp32 values
+template <typename T, int V>
+__device__ __forceinline__ void load_packed(const T* p, float (&x)[V])
+{
+    constexpr int kBytes = V * (int)sizeof(T);
+    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
+    if constexpr (kBytes == 16) {
+        const uint4 v = load16(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (kBytes == 8) {
+        asm("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    } else if constexpr (kBytes == 4) {
+        asm("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    } else {
+        unsigned short h;
+        asm("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
+        w[0] = h;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i]);
+        else x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);      // bf16 -> fp32 is exact
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_packed(T* p, const float (&x)[V])
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (V % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) __stcs(reinterpret_cast<float4*>(p + i), make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]));
+        } else if constexpr (V == 2) {
+            __stcs(reinterpret_cast<float2*>(p), make_float2(x[0], x[1]));
+        } else {
+            __stcs(p, x[0]);
+        }
+    } else {
+        if constexpr (V == 8) {
+            __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]),
+                                                           pack_bf16(x[6], x[7])));
+        } else if constexpr (V == 4) {
+            __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])));
+        } else if constexpr (V == 2) {
+            __stcs(reinterpret_cast<unsigned int*>(p), pack_bf16(x[0], x[1]));
+        } else {
+            *p = __float2bfloat16_rn(x[0]);
+        }
+    }
+}
+
+// widest vector, in elements, that rows of `in` and of `out` can be read and written in: 16 bytes of `in`, 2 elements or 1
+static int embed_vector(const void* in, int64_t ld_in, gnnfd_dtype_t in_type, const void* out, int64_t ld_out, gnnfd_dtype_t out_type)
+{
+    const int in_size = in_type == GNNFD_F32 ? 4 : 2, out_size = out_type == GNNFD_F32 ? 4 : 2;
+    auto fits = [&](int v) {
+        const int in_bytes = v * in_size, out_bytes = v * out_size < 16 ? v * out_size : 16;
+        return (uintptr_t)in % in_bytes == 0 && (uintptr_t)out % out_bytes == 0 && ld_in * in_size % in_bytes == 0 &&
+               ld_out * out_size % out_bytes == 0;
+    };
+    return fits(16 / in_size) ? 16 / in_size : fits(2) ? 2 : 1;
+}
+static int lanes_log2(int f, int v)
+{
+    const int l = ilog2((f + v - 1) / v);
+    return l < 5 ? l : 5;
+}
+
+// ------------------------------------------------------------------ lookup
+
+struct LookupArgs {
+    const void *ids, *table;
+    void* out;
+    int64_t n, vocab, ldt, ldo;
+    int32_t* status;
+    float scale;
+    int32_t f, lpr_log2;
+};
+
+// 2^lpr_log2 lanes per row, U rows of a group in flight together.
+template <typename IdT, typename TI, typename TO, int V, int U>
+__global__ void __launch_bounds__(kEmbedBlock) embedding_rows(const __grid_constant__ LookupArgs a)
+{
+    grid_dependency<true>();
+    const int lpr = 1 << a.lpr_log2, groups = kEmbedBlock >> a.lpr_log2;
+    const int lane = threadIdx.x & (lpr - 1);
+    const int64_t row0 = (int64_t)blockIdx.x * (groups * U) + (threadIdx.x >> a.lpr_log2);
+    const TI* src[U];
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t row = row0 + (int64_t)u * groups;
+        src[u] = nullptr;
+        if (row < a.n) {
+            const int64_t id = (int64_t) static_cast<const IdT*>(a.ids)[row];
+            if ((uint64_t)id < (uint64_t)a.vocab) src[u] = static_cast<const TI*>(a.table) + id * a.ldt;
+            else bad = true;
+        }
+    }
+    if (bad && a.status) atomicOr(a.status, 1);
+    TO* const out = static_cast<TO*>(a.out);
+    for (int c = lane * V; c < a.f; c += lpr * V) {
+        if (c + V <= a.f) {
+            float x[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (src[u]) load_packed<TI, V>(src[u] + c, x[u]);
+                else
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = row0 + (int64_t)u * groups;
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u][i] = src[u] ? x[u][i] * a.scale : 0.f;
+                if (row < a.n) store_packed<TO, V>(out + row * a.ldo + c, x[u]);
+            }
+        } else {
+            for (int i = c; i < a.f; ++i)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t row = row0 + (int64_t)u * groups;
+                    float x[1] = {0.f};
+                    if (src[u]) load_packed<TI, 1>(src[u] + i, x);
+                    x[0] = src[u] ? x[0] * a.scale : 0.f;
+                    if (row < a.n) store_packed<TO, 1>(out + row * a.ldo + i, x);
+                }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+
+struct GradArgs {
+    const void* ids;
+    const void* dout;
+    void* out;
+    int64_t n, vocab, ldd, ldo, padding;
+    const unsigned long long* words;       // sorted: id << val_bits | position + 1; ids out of range last
+    const BuildCounts* counts;
+    float *head, *tail;                    // [blocks, fpad] partial sums of the run that a block starts / ends inside of
+    uint8_t* mark;                         // [vocab] rows that get a sum, zeroed (null where the gradient is added to what is there)
+    int32_t* status;
+    float scale;
+    int32_t f, fpad, lpr_log2, val_bits, per_block, n_blocks, col_tiles, accumulate;
+};
+
+template <typename TO, int V>
+__device__ __forceinline__ void write_row(const GradArgs& a, int64_t row, int c, float (&x)[V])
+{
+    if (row == a.padding) return;
+    TO* const p = static_cast<TO*>(a.out) + row * a.ldo + c;
+    const bool add = a.accumulate;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] *= a.scale;
+    if (c + V <= a.f) {
+        if (add) {
+            float old[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float one[1];
+                load_packed<TO, 1>(p + i, one);
+                old[i] = one[0];
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] += old[i];
+        }
+        store_packed<TO, V>(p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (c + i < a.f) {
+                float one[1];
+                one[0] = 0.f;
+                if (add) load_packed<TO, 1>(p + i, one);
+                one[0] += x[i];
+                store_packed<TO, 1>(p + i, one);
+            }
+    }
+}
+
+// Sums over runs of equal ids.  A block takes per_block sorted ids, a group of lanes a consecutive share of them, and walks it with kInFlight
+// rows loaded at a time, adding until the id changes.  A run that lies inside a group's share is written at once; what a group has of a run that
+// goes on before or behind its share meets in shared memory, and is added there in order by the group that has the run's beginning;
+// what a block has of a run that goes on in other blocks is left for embedding_grad_finish.
+constexpr int kInFlight = 8;
+
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_sums(const __grid_constant__ GradArgs a)
+{
+    grid_dependency<true>();
+    __shared__ float ends[2][kEmbedBlock][V];            // a group's first (run begun earlier) and last (run that goes on) sums
+    __shared__ bool through[kEmbedBlock];                // of a group: all of its share belongs to a run begun earlier that goes on
+    if (a.counts->sort_failed) return;
+    const int64_t n_valid = a.counts->n_valid;
+    const int groups = kEmbedBlock >> a.lpr_log2, g = threadIdx.x >> a.lpr_log2, lane = threadIdx.x & ((1 << a.lpr_log2) - 1);
+    const int64_t base = (int64_t)blockIdx.x * a.per_block;
+    if (base >= n_valid) return;
+    const int64_t end = min(base + a.per_block, n_valid);
+    const int share = (a.per_block + groups - 1) / groups;
+    const int64_t first = min(base + (int64_t)g * share, end), last = min(first + share, end);
+    const int c = ((int)blockIdx.y * (1 << a.lpr_log2) + lane) * V;
+    const bool whole = c + V <= a.f;
+    auto key_of = [&](unsigned long long w) { return (int64_t)(w >> a.val_bits); };
+    auto key_at = [&](int64_t i) { return key_of(a.words[i]); };
+    const unsigned long long pos_mask = (1ull << a.val_bits) - 1ull;
+    auto load_row = [&](unsigned long long w, float (&x)[V]) {
+        const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)((w & pos_mask) - 1ull) * a.ldd + c;
+        if (whole) {
+            load_packed<TI, V>(p, x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float one[1] = {0.f};
+                if (c + i < a.f) load_packed<TI, 1>(p + i, one);
+                x[i] = one[0];
+            }
+        }
+    };
+    auto finish_row = [&](int64_t key, float (&x)[V]) {
+        if (c < a.f) write_row<TO, V>(a, key, c, x);
+        if (a.mark && c == 0 && key != a.padding) a.mark[key] = 1;
+    };
+
+    bool head = false, tail = false, passes = false;
+    int64_t cur = -1;
+    if (first < last) {
+        float acc[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = 0.f;
+        cur = key_at(first);
+        bool open = first > 0 && key_at(first - 1) == cur;             // the run was begun earlier
+        auto flush = [&](bool goes_on) {
+            if (open || goes_on) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) ends[open ? 0 : 1][threadIdx.x][i] = acc[i];
+                head |= open;
+                tail |= !open;
+                passes |= open && goes_on;
+            } else {
+                finish_row(cur, acc);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = 0.f;
+        };
+        unsigned long long w[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) w[u] = first + u < last ? a.words[first + u] : 0ull;
+        for (int64_t t = first; t < last; t += kInFlight) {
+            float x[kInFlight][V];
+            unsigned long long next[kInFlight];
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                if (w[u] != 0ull) load_row(w[u], x[u]);
+                else
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) next[u] = t + kInFlight + u < last ? a.words[t + kInFlight + u] : 0ull;
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                if (w[u] == 0ull) continue;                            // (a word holds position + 1: never 0)
+                const int64_t key = key_of(w[u]);
+                if (key != cur) {
+                    flush(false);
+                    cur = key;
+                    open = false;
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += x[u][i];
+            }
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) w[u] = next[u];
+        }
+        flush(last < n_valid && key_at(last) == cur);
+    }
+    through[g] = passes;                                               // (all lanes of a group agree)
+    __syncthreads();
+
+    // which: 0 the run that this group's share begins inside of (asked of the block's first group), 1 the one it ends inside of
+    auto join = [&](int which, int64_t key) {
+        float sum[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = ends[which][threadIdx.x][i];
+        bool goes_on = which == 1 || passes;
+        const int used = ((int)(end - base) + share - 1) / share;      // the groups with a share
+        for (int h = g + 1; goes_on && h < used; ++h) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += ends[0][(h << a.lpr_log2) + lane][i];
+            goes_on = through[h];
+        }
+        if (which == 1 && !goes_on) {
+            finish_row(key, sum);
+            return;
+        }
+        float* const part = (which ? a.tail : a.head) + (int64_t)blockIdx.x * a.fpad + c;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (c + i < a.f) part[i] = sum[i];
+        if (which == 1 && a.mark && c == 0 && key != a.padding) a.mark[key] = 1;
+    };
+    if (head && g == 0) join(0, -1);
+    if (tail) join(1, cur);
+}
+
+// The first n_blocks * col_tiles blocks: a run that begins in block b of the sums and goes on is added up over the blocks it
+// reaches, kJoinWays interleaved walks at a time.  The others: rows that no id names become zero.
+constexpr int kJoinCols = 64, kJoinWays = kEmbedBlock / kJoinCols;
+
+template <typename TO>
+__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __grid_constant__ GradArgs a, int join_tiles, int vec)
+{
+    grid_dependency<true>();
+    __shared__ float sums[kJoinWays][kJoinCols];
+    if (a.counts->sort_failed) {
+        if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, 2);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status && a.counts->bad_index) atomicOr(a.status, 1);
+    const int64_t n_valid = a.counts->n_valid;
+    const int64_t join_blocks = (int64_t)a.n_blocks * join_tiles;
+    if (blockIdx.x < join_blocks) {
+        const int64_t b = blockIdx.x / join_tiles, begin = b * a.per_block, next = begin + a.per_block;
+        auto key_at = [&](int64_t i) { return (int64_t)(a.words[i] >> a.val_bits); };
+        if (next >= n_valid) return;
+        const int64_t key = key_at(next);
+        if (key_at(next - 1) != key || (begin > 0 && key_at(begin - 1) == key)) return;      // nothing goes on, or it was begun earlier
+        const int c = (int)(blockIdx.x % join_tiles) * kJoinCols + (int)threadIdx.x % kJoinCols, way = threadIdx.x / kJoinCols;
+        float sum = 0.f;
+        if (c < a.f) {
+            if (way == 0) sum = a.tail[b * a.fpad + c];
+            constexpr int kAhead = 4;                    // blocks of a walk whose words and sums are read together
+            for (int64_t at = b + 1 + way; at < a.n_blocks && at * a.per_block < n_valid;) {
+                float part[kAhead];
+                bool same[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int64_t block = at + i * kJoinWays;
+                    same[i] = block < a.n_blocks && block * a.per_block < n_valid && key_at(block * a.per_block) == key;
+                    part[i] = same[i] ? a.head[block * a.fpad + c] : 0.f;
+                }
+                bool on = true;
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    on = on && same[i];
+                    if (on) sum += part[i];
+                }
+                if (!on) break;
+                at += kAhead * kJoinWays;
+            }
+        }
+        sums[way][threadIdx.x % kJoinCols] = sum;
+        __syncthreads();
+        if (way != 0 || c >= a.f) return;
+        float x[1] = {sum};
+#pragma unroll
+        for (int w = 1; w < kJoinWays; ++w) x[0] += sums[w][threadIdx.x];
+        write_row<TO, 1>(a, key, c, x);
+        return;
+    }
+    // zero rows: 2^lpr_log2 lanes per row, V elements at a time where rows start on such boundaries
+    const int lpr = 1 << a.lpr_log2, lane = threadIdx.x & (lpr - 1), groups = kEmbedBlock >> a.lpr_log2;
+    const int64_t stride = ((int64_t)gridDim.x - join_blocks) * groups;
+    for (int64_t row = (blockIdx.x - join_blocks) * groups + (threadIdx.x >> a.lpr_log2); row < a.vocab; row += stride) {
+        if (a.mark[row]) continue;
+        char* const p = reinterpret_cast<char*>(static_cast<TO*>(a.out) + row * a.ldo);
+        const int bytes = a.f * (int)sizeof(TO);
+        int at = lane * vec;
+        if (vec == 16)
+            for (; at + 16 <= bytes; at += lpr * 16) __stcs(reinterpret_cast<uint4*>(p + at), make_uint4(0u, 0u, 0u, 0u));
+        else if (vec == 4)
+            for (; at + 4 <= bytes; at += lpr * 4) __stcs(reinterpret_cast<unsigned int*>(p + at), 0u);
+        else
+            for (; at + 2 <= bytes; at += lpr * 2) *reinterpret_cast<unsigned short*>(p + at) = 0;
+        for (int i = at; i < bytes && i < at + vec; i += 2) *reinterpret_cast<unsigned short*>(p + i) = 0;      // what is left of a row
+    }
+}
+
+// A batch of at most kFewIds ids needs no sort: a block that takes an id reads all of them from shared memory, leaves where the same id
+// came earlier, and otherwise adds the rows of all places where it occurs, each of its warps those in a share of the places.
+constexpr int kFewIds = 8192;
+
+template <typename IdT>
+__device__ __forceinline__ int few_id(const GradArgs& a, int64_t i, bool* bad)
+{
+    const int64_t id = (int64_t) static_cast<const IdT*>(a.ids)[i];
+    const bool inside = (uint64_t)id < (uint64_t)a.vocab;
+    *bad = *bad || !inside;
+    return inside && id != a.padding ? (int)id : -1;
+}
+
+template <typename IdT, typename TI, typename TO, int V>
+__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_few(const __grid_constant__ GradArgs a)
+{
+    grid_dependency<true>();
+    extern __shared__ int few_ids[];
+    __shared__ float part[kEmbedBlock / 32 - 1][32][V];
+    const int n = (int)a.n, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += kEmbedBlock) few_ids[i] = few_id<IdT>(a, i, &bad);
+    if (bad && blockIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status, 1);
+    __syncthreads();
+    const int c = ((int)blockIdx.y * 32 + lane) * V;
+    const int share = ((n + 255) / 256) * 32;                          // places per warp, whole steps of 32
+    for (int mine = blockIdx.x; mine < n; mine += gridDim.x) {
+        const int id = few_ids[mine];
+        bool earlier = id < 0;
+        for (int i = threadIdx.x; i < mine && !earlier; i += kEmbedBlock) earlier = few_ids[i] == id;
+        if (__syncthreads_or(earlier)) continue;
+        float acc[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = 0.f;
+        const int begin = warp * share, end = min(begin + share, n);
+        for (int i0 = max(begin, mine / 32 * 32); i0 < end; i0 += 32) {
+            unsigned here = __ballot_sync(0xffffffffu, i0 + lane < end && few_ids[i0 + lane] == id);
+            while (here) {
+                float x[4][V];
+                int count = 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
+                    if (here) {
+                        const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)(i0 + __ffs(here) - 1) * a.ldd + c;
+                        if (c + V <= a.f) {
+                            load_packed<TI, V>(p, x[u]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < V; ++i)
+                                if (c + i < a.f) {
+                                    float one[1];
+                                    load_packed<TI, 1>(p + i, one);
+                                    x[u][i] = one[0];
+                                }
+                        }
+                        here &= here - 1u;
+                        ++count;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (u < count)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[i] += x[u][i];
+            }
+        }
+        if (warp > 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i) part[warp - 1][lane][i] = acc[i];
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 0; w < kEmbedBlock / 32 - 1; ++w)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += part[w][lane][i];
+            if (c < a.f) write_row<TO, V>(a, id, c, acc);
+        }
+        __syncthreads();
+    }
+}
+
+// all rows of a gradient that is not added to; four bytes at a time where rows allow it
+template <typename Word>
+__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_clear(void* out, int64_t pitch_words, int64_t rows, int32_t words)
+{
+    grid_dependency<true>();
+    const int64_t total = rows * words, step = (int64_t)gridDim.x * kEmbedBlock;
+    int64_t i = (int64_t)blockIdx.x * kEmbedBlock + threadIdx.x;
+    if (pitch_words == words) {                           // no padding columns
+        for (; i < total; i += step) static_cast<Word*>(out)[i] = Word();
+        return;
+    }
+    for (; i < total; i += step) {
+        const int64_t row = total <= 0x7fffffffll ? (int64_t)((uint32_t)i / (uint32_t)words) : i / words;
+        static_cast<Word*>(out)[row * pitch_words + (i - row * words)] = Word();
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+template <typename IdT, typename TI, typename TO, int V>
+static void launch_lookup(const LookupArgs& a, cudaStream_t s)
+{
+    const int64_t rows = kEmbedBlock >> a.lpr_log2;
+    // four rows in flight per group once that still gives every SM four blocks
+    if (a.n >= rows * 4 * 4 * kSms)
+        GNNFD_LAUNCH("embedding_rows", s, (embedding_rows<IdT, TI, TO, V, 4>), (unsigned)((a.n + rows * 4 - 1) / (rows * 4)), kEmbedBlock, 0, a);
+    else
+        GNNFD_LAUNCH("embedding_rows", s, (embedding_rows<IdT, TI, TO, V, 1>), (unsigned)((a.n + rows - 1) / rows), kEmbedBlock, 0, a);
+}
+
+template <typename IdT, typename TI, typename TO>
+static void lookup_vector(const LookupArgs& a, int v, cudaStream_t s)
+{
+    if (v == 16 / (int)sizeof(TI)) launch_lookup<IdT, TI, TO, 16 / sizeof(TI)>(a, s);
+    else if (v == 2) launch_lookup<IdT, TI, TO, 2>(a, s);
+    else launch_lookup<IdT, TI, TO, 1>(a, s);
+}
+
+template <typename IdT>
+static void lookup_types(const LookupArgs& a, int v, gnnfd_dtype_t tdt, gnnfd_dtype_t odt, cudaStream_t s)
+{
+    if (tdt == GNNFD_F32) {
+        if (odt == GNNFD_F32) lookup_vector<IdT, float, float>(a, v, s);
+        else lookup_vector<IdT, float, __nv_bfloat16>(a, v, s);
+    } else {
+        if (odt == GNNFD_F32) lookup_vector<IdT, __nv_bfloat16, float>(a, v, s);
+        else lookup_vector<IdT, __nv_bfloat16, __nv_bfloat16>(a, v, s);
+    }
+}
+
+// ids per block of the sums: as many as leave every SM sixteen blocks, 64 to 1024
+static int ids_per_block(int64_t n)
+{
+    int t = 64;
+    while (t < 1024 && (int64_t)t * 2 * kSms * 16 <= n) t *= 2;
+    return t;
+}
+
+struct GradScratch {
+    SortedIds sorted;
+    float *head, *tail;
+};
+
+static int carve_grad(Carver& c, int64_t n, int64_t vocab, int32_t f, GradScratch* g)
+{
+    const int rc = carve_sorted_ids(c, n, vocab, (size_t)vocab, &g->sorted);
+    if (rc) return rc;
+    const size_t blocks = (size_t)((n + ids_per_block(n) - 1) / ids_per_block(n)), fpad = align_up((size_t)f, 4);
+    g->head = c.take<float>(blocks * fpad);
+    g->tail = c.take<float>(blocks * fpad);
+    return GNNFD_OK;
+}
+
+template <typename TI, typename TO, int V>
+static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool accumulate, cudaStream_t s)
+{
+    if (few) {
+        const dim3 grid((unsigned)(a.n < 8 * kSms ? a.n : 8 * kSms), (unsigned)((a.f + 32 * V - 1) / (32 * V)));
+        const size_t smem = (size_t)a.n * sizeof(int);
+        if (itype == GNNFD_I32) GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<int32_t, TI, TO, V>), grid, kEmbedBlock, smem, a);
+        else GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<long long, TI, TO, V>), grid, kEmbedBlock, smem, a);
+    } else {
+        GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V>), dim3((unsigned)a.n_blocks, (unsigned)a.col_tiles), kEmbedBlock,
+                     0, a);
+        const int join_tiles = (a.f + kJoinCols - 1) / kJoinCols;
+        const int64_t groups = kEmbedBlock >> a.lpr_log2, zero = accumulate ? 0 : (a.vocab + groups - 1) / groups;
+        const int64_t grid = (int64_t)a.n_blocks * join_tiles + (zero < 16 * kSms ? zero : 16 * kSms);
+        if (grid > 0x7fffffffll) return GNNFD_TOO_LARGE;
+        const uintptr_t bits = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
+        const int vec = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+        GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, join_tiles, vec);
+    }
+    GNNFD_CUDA_CHECK(cudaGetLastError());
+    return GNNFD_OK;
+}
+
+template <typename TI, typename TO>
+static int grad_vector(const GradArgs& a, int v, gnnfd_itype_t itype, bool few, bool accumulate, cudaStream_t s)
+{
+    if (v == 16 / (int)sizeof(TI)) return launch_grad<TI, TO, 16 / sizeof(TI)>(a, itype, few, accumulate, s);
+    if (v == 2) return launch_grad<TI, TO, 2>(a, itype, few, accumulate, s);
+    return launch_grad<TI, TO, 1>(a, itype, few, accumulate, s);
+}
+
+static int clear_rows(void* out, int64_t ldo, gnnfd_dtype_t odt, int64_t rows, int32_t f, cudaStream_t s)
+{
+    const int64_t size = odt == GNNFD_F32 ? 4 : 2, pitch = ldo * size, bytes = f * size;
+    const uintptr_t bits = (uintptr_t)out | (uintptr_t)pitch | (uintptr_t)bytes;
+    const int64_t word = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2, total = rows * (bytes / word);
+    const int64_t blocks = (total + kEmbedBlock * 4 - 1) / (kEmbedBlock * 4);
+    const unsigned grid = (unsigned)(blocks < 16 * kSms ? blocks : 16 * kSms);
+    if (word == 16) GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint4>, grid, kEmbedBlock, 0, out, pitch / 16, rows, (int32_t)(bytes / 16));
+    else if (word == 4) GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint32_t>, grid, kEmbedBlock, 0, out, pitch / 4, rows, (int32_t)(bytes / 4));
+    else GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint16_t>, grid, kEmbedBlock, 0, out, pitch / 2, rows, (int32_t)(bytes / 2));
+    GNNFD_CUDA_CHECK(cudaGetLastError());
+    return GNNFD_OK;
+}
+
+static bool known(gnnfd_dtype_t t) { return t == GNNFD_F32 || t == GNNFD_BF16; }
+
+}  // namespace gnnfd
+
+extern "C" {
+
+int gnnfd_embedding(int64_t n, const void* d_ids, gnnfd_itype_t itype, int64_t vocab, const void* d_table, int64_t ldt, gnnfd_dtype_t tdt,
+                    int32_t f, float scale, void* d_out, int64_t ldo, gnnfd_dtype_t odt, int32_t* d_status, void* stream)
+{
+    using namespace gnnfd;
+    if (n < 0 || vocab <= 0 || f <= 0 || ldt < f || ldo < f) return GNNFD_INVALID_ARG;
+    if (!known(tdt) || !known(odt) || (itype != GNNFD_I32 && itype != GNNFD_I64)) return GNNFD_UNSUPPORTED;
+    if (n > 0x7fffffffll || vocab > 0x7fffffffll) return GNNFD_TOO_LARGE;
+    if (n == 0) return GNNFD_OK;
+    if (!d_ids || !d_table || !d_out) return GNNFD_INVALID_ARG;
+    const int v = embed_vector(d_table, ldt, tdt, d_out, ldo, odt);
+    const LookupArgs a{d_ids, d_table, d_out, n, vocab, ldt, ldo, d_status, scale, f, lanes_log2(f, v)};
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (itype == GNNFD_I32) lookup_types<int32_t>(a, v, tdt, odt, s);
+    else lookup_types<long long>(a, v, tdt, odt, s);
+    GNNFD_CUDA_CHECK(cudaGetLastError());
+    return GNNFD_OK;
+}
+
+int gnnfd_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int32_t f, size_t* scratch_bytes)
+{
+    using namespace gnnfd;
+    if (n < 0 || vocab <= 0 || f <= 0 || !scratch_bytes) return GNNFD_INVALID_ARG;
+    if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
+    *scratch_bytes = 0;
+    if (n <= kFewIds) return GNNFD_OK;
+    Carver c(nullptr, ~size_t(0));
+    GradScratch g;
+    const int rc = carve_grad(c, n, vocab, f, &g);
+    if (rc == GNNFD_OK) *scratch_bytes = c.off;
+    return rc;
+}
+
+int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, const void* d_dout, int64_t ldd, gnnfd_dtype_t ddt,
+                             int64_t vocab, int32_t f, float scale, int64_t padding, int accumulate, void* d_grad, int64_t ldg,
+                             gnnfd_dtype_t gdt, void* d_scratch, size_t scratch_bytes, int32_t* d_status, void* stream)
+{
+    using namespace gnnfd;
+    const SortDrill drill = take_sort_drill();
+    if (n < 0 || vocab <= 0 || f <= 0 || ldd < f || ldg < f || !d_grad) return GNNFD_INVALID_ARG;
+    if (!known(ddt) || !known(gdt) || (itype != GNNFD_I32 && itype != GNNFD_I64)) return GNNFD_UNSUPPORTED;
+    if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
+    if (n > 0 && (!d_ids || !d_dout)) return GNNFD_INVALID_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool few = n <= kFewIds;
+    if (few && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
+    const int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
+    GradArgs a{};
+    a.ids = d_ids; a.dout = d_dout; a.out = d_grad;
+    a.n = n; a.vocab = vocab; a.ldd = ldd; a.ldo = ldg; a.padding = padding;
+    a.status = d_status; a.accumulate = accumulate != 0; a.scale = scale; a.f = f; a.fpad = (int32_t)align_up((size_t)f, 4);
+    a.lpr_log2 = lanes_log2(f, v);
+    a.col_tiles = (f + (v << a.lpr_log2) - 1) / (v << a.lpr_log2);
+    if (few) {
+        if (!accumulate) {
+            const int rc = clear_rows(d_grad, ldg, gdt, vocab, f, s);
+            if (rc) return rc;
+        }
+        if (n == 0) return GNNFD_OK;
+    } else {
+        if (!d_scratch || ((uintptr_t)d_scratch & 255u)) return GNNFD_INVALID_ARG;
+        Carver c(d_scratch, scratch_bytes);
+        GradScratch g;
+        int rc = carve_grad(c, n, vocab, f, &g);
+        if (rc) return rc;
+        if (!c.ok) return GNNFD_WORKSPACE_TOO_SMALL;
+        rc = sort_ids(n, vocab, d_ids, itype, drill, g.sorted, s);
+        if (rc) return rc;
+        a.words = g.sorted.words; a.val_bits = g.sorted.val_bits; a.counts = g.sorted.counts;
+        a.mark = accumulate ? nullptr : g.sorted.extra;
+        a.head = g.head; a.tail = g.tail;
+        a.per_block = ids_per_block(n);
+        a.n_blocks = (int32_t)((n + a.per_block - 1) / a.per_block);
+    }
+    if (ddt == GNNFD_F32)
+        return gdt == GNNFD_F32 ? grad_vector<float, float>(a, v, itype, few, accumulate, s)
+                                : grad_vector<float, __nv_bfloat16>(a, v, itype, few, accumulate, s);
+    return gdt == GNNFD_F32 ? grad_vector<__nv_bfloat16, float>(a, v, itype, few, accumulate, s)
+                            : grad_vector<__nv_bfloat16, __nv_bfloat16>(a, v, itype, few, accumulate, s);
+}
+
+}  // extern "C"
