@@ -367,6 +367,45 @@ int gnnfd_layer_gat(const gnnfd_csr_t* csr, const void* d_x, int64_t ldx, gnnfd_
                     const float* d_a_dst, float negative_slope, int mode, void* d_out, int64_t ldo, gnnfd_dtype_t odt,
                     int32_t chunk_width, void* d_scratch, size_t scratch_bytes, int32_t* d_status, void* stream);
 
+/* ------------------------------------------------------------------ dot-product attention over a graph
+ *
+ * The attention of transformer layers with the graph as its mask: vertex v attends to the sources of the edges that end in it, so the graphs
+ * of a batch (or documents) do not see one another, and a batch of small graphs that are attended as wholes is the CSR of
+ * all their pairs.  (The paper's attention model scores an edge by a sum of two halves instead: gnnfd_aggregate_gat.)  For CSR entry k of row v with
+ * source u and head h
+ *   t = scale * <q[v, h], key[u, h]>,   s[k, h] = (softcap > 0 ? softcap * tanh(t / softcap) : t) + bias[dist[k], h]
+ *   p = softmax of s[., h] over the entries of the row,   out[v, h] = sum_k p[k, h] * value[u, h]
+ * Multi-edges are separate terms.  q, key, value, out: [n, ld] with heads * dim columns (column j belongs to head j / dim; dim up to
+ * 256 for fp32, 512 for bf16); the three inputs have type dt.  d_dist [nnz] int32, in CSR slot order: the bucket of every entry, say the distance of its ends;
+ * buckets below 0 or past the last one count as the first or last.  d_bias [buckets, heads] fp32.  Both NULL (buckets 0): no bias.  A bias of
+ * -infinity takes an entry out, whatever q, key and value hold for it.  Rows without entries, or with none left, give 0.
+ * d_lse (may be NULL): [n, heads, 2] fp32, 8-byte aligned, receives each row's largest score and the sum of e^(s - largest): the
+ * logarithm of the softmax's denominator in two parts, as the gradient needs it ((-infinity, 0) for rows without entries).
+ * chunk_width: as for the other aggregations, but a multiple of dim (or >= heads * dim): a chunk holds whole heads.
+ * d_scratch: gnnfd_attention_workspace_bytes(csr, heads, dim) bytes, 256-byte aligned (0 and NULL where the graph has no hub row).  fp32 sums and
+ * softmax; the call only enqueues work. */
+int gnnfd_attention_workspace_bytes(const gnnfd_csr_t* csr, int32_t heads, int32_t dim, size_t* scratch_bytes);
+
+int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,
+                              int64_t ldv, gnnfd_dtype_t dt, int32_t heads, int32_t dim, float scale, float softcap,
+                              const int32_t* d_dist, const float* d_bias, int32_t buckets, void* d_out, int64_t ldo, gnnfd_dtype_t odt,
+                              float* d_lse, int32_t chunk_width, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* The gradients of the above for d_dout [n, lddo] of type dt, the gradient of out: d_dq, d_dk, d_dv [n, ld*] of type gdt and, where d_dbias is not NULL,
+ * d_dbias [buckets, heads] fp32.  csr_t: the CSR of the reversed edges, gnnfd_build_csr of the same edge list with d_src and d_dst exchanged and
+ * the same flags; d_dist_t: the buckets in csr_t's slot order.  d_lse as written by the forward call with the same arguments.  Nothing is
+ * added with atomics: gradients of vertices that many edges share are sums over the rows of csr_t.
+ * d_scratch: gnnfd_attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets) bytes (buckets may be 0 there where d_dbias is NULL). */
+int gnnfd_attention_backward_workspace_bytes(const gnnfd_csr_t* csr, const gnnfd_csr_t* csr_t, int32_t heads, int32_t dim, int32_t buckets,
+                                             size_t* scratch_bytes);
+
+int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t* csr_t, const void* d_q, int64_t ldq, const void* d_k,
+                                       int64_t ldk, const void* d_v, int64_t ldv, const void* d_dout, int64_t lddo, gnnfd_dtype_t dt,
+                                       const float* d_lse, int32_t heads, int32_t dim, float scale, float softcap, const int32_t* d_dist,
+                                       const int32_t* d_dist_t, const float* d_bias, int32_t buckets, void* d_dq, int64_t lddq, void* d_dk,
+                                       int64_t lddk, void* d_dv, int64_t lddv, gnnfd_dtype_t gdt, float* d_dbias, int32_t chunk_width,
+                                       void* d_scratch, size_t scratch_bytes, void* stream);
+
 /* ------------------------------------------------------------------ learned vertex features
  *
  * For graphs whose vertices have no features of their own (or a type, a degree, a name instead): a table with a learned row per

@@ -83,6 +83,12 @@ def lib() -> ctypes.CDLL:
         L.gnnfd_layer_sage.argtypes = layer
         L.gnnfd_layer_gat.argtypes = [vp, vp, i64, i32, i32, vp, i64, i32, i32, vp, vp, fl, ctypes.c_int, vp, i64, i32, i32,
                                       vp, sz, vp, vp]
+        L.gnnfd_attention_workspace_bytes.argtypes = [vp, i32, i32, pp(sz)]
+        L.gnnfd_aggregate_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, fl, fl, vp, vp, i32, vp, i64, i32, vp, i32,
+                                                vp, sz, vp]
+        L.gnnfd_attention_backward_workspace_bytes.argtypes = [vp, vp, i32, i32, i32, pp(sz)]
+        L.gnnfd_aggregate_attention_backward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, fl, fl, vp, vp, vp,
+                                                         i32, vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, sz, vp]
         L.gnnfd_embedding.argtypes = [i64, vp, i32, i64, vp, i64, i32, i32, fl, vp, i64, i32, vp, vp]
         L.gnnfd_embedding_backward_workspace_bytes.argtypes = [i64, i64, i32, pp(sz)]
         L.gnnfd_embedding_backward.argtypes = [i64, vp, i32, vp, i64, i32, i64, i32, fl, i64, ctypes.c_int, vp, i64, i32, vp, sz, vp, vp]
@@ -735,6 +741,130 @@ def _status_ptr(status, device):
     if status.dtype != torch.int32 or status.numel() < 1 or status.device != device:
         raise ValueError("status must be an int32 tensor on %s" % device)
     return status.data_ptr()
+
+
+def edge_values(csr: Csr, values: torch.Tensor, loop=0) -> torch.Tensor:
+    """The values [e] of the input edges in CSR slot order: a reverse edge that the build added has its edge's value, an added
+    self-loop the value ``loop``."""
+    if values.dim() != 1 or values.device != csr.device:
+        raise ValueError("values must be a 1-D tensor on %s" % csr.device)
+    perm, e = csr.perm.long(), values.shape[0]
+    if e == 0:
+        return torch.full((csr.nnz,), loop, dtype=values.dtype, device=csr.device)
+    return torch.where(perm < 0, torch.full((), loop, dtype=values.dtype, device=csr.device), values[perm.clamp_min(0) % e])
+
+
+def _attention_operands(csr: Csr, f: int, heads: int, dist, bias, **tensors):
+    """(pointer, leading dimension) of each [n, >= f] operand, the inputs of one type, then (dist pointer, bias pointer, buckets)."""
+    first = next(iter(tensors.values()))
+    got = []
+    for name, t in tensors.items():
+        got.append(_matrix(t, f, name))
+        if t.device != csr.device:
+            _same_device(csr.device, **{name: t})
+        if t.dtype != first.dtype:
+            raise TypeError("%s must have one dtype" % ", ".join(tensors))
+        _need_rows(t, csr.n, name)
+    if (dist is None) != (bias is None):
+        raise ValueError("dist and bias come together")
+    if bias is None:
+        return got, None, None, 0
+    if bias.dtype != torch.float32 or bias.dim() != 2 or bias.shape[1] != heads or bias.shape[0] < 1 or not bias.is_contiguous():
+        raise ValueError("bias must be a contiguous float32 [buckets, heads = %d] tensor" % heads)
+    _check_dist(csr, dist, "dist")
+    _same_device(csr.device, bias=bias)
+    return got, dist.data_ptr(), bias.data_ptr(), bias.shape[0]
+
+
+def _check_dist(csr: Csr, dist, name: str):
+    if dist.dtype != torch.int32 or dist.dim() != 1 or dist.shape[0] < csr.nnz or not dist.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of nnz = %d values" % (name, csr.nnz))
+    _same_device(csr.device, **{name: dist})
+
+
+def attention_workspace_bytes(csr: Csr, heads: int, dim: int) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_attention_workspace_bytes(csr.handle, heads, dim, ctypes.byref(s)), "gnnfd_attention_workspace_bytes")
+    return s.value
+
+
+def aggregate_attention(csr: Csr, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, dim: int, scale: float | None = None,
+                        softcap: float = 0.0, dist: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                        chunk_width: int | None = None, out: torch.Tensor | None = None, out_dtype=None, with_lse: bool = False,
+                        scratch=None, stream=None):
+    """gnnfd_aggregate_attention: softmax attention of every vertex over the sources of its edges.  ``scale`` defaults to dim ** -0.5;
+    ``dist`` holds a bucket of ``bias`` ([buckets, heads]) per CSR slot (see edge_values).  With ``with_lse`` the call returns
+    (out, lse [n, heads, 2]), which aggregate_attention_backward takes."""
+    f = heads * dim
+    scale = dim ** -0.5 if scale is None else scale
+    chunk_width = f if chunk_width is None else chunk_width
+    ((qp, ldq), (kp, ldk), (vp_, ldv)), dp, bp, buckets = _attention_operands(csr, f, heads, dist, bias, q=q, k=k, v=v)
+    fresh = out is None
+    if fresh:
+        out = _take(lambda: torch.empty((csr.n, f), dtype=out_dtype or torch.float32, device=csr.device), stream)
+    op, ldo = _matrix(out, f, "out")
+    if not fresh:
+        _same_device(csr.device, out=out)
+        _need_rows(out, csr.n, "out")
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            _no_overlap(t, out, name, "out")
+    lse = _take(lambda: torch.empty((csr.n, heads, 2), dtype=torch.float32, device=csr.device), stream) if with_lse else None
+    if scratch is None:
+        need = attention_workspace_bytes(csr, heads, dim)
+        scratch = _alloc_bytes(need, csr.device, stream) if need else None
+    scr, scr_n = _scratch_args(scratch, csr.device)
+    dt, odt, lp = _dtype_code(q), _dtype_code(out), lse.data_ptr() if with_lse else None
+    _on_device(q, stream, lambda s: _check(lib().gnnfd_aggregate_attention(csr.handle, qp, ldq, kp, ldk, vp_, ldv, dt, heads, dim, scale, softcap, dp,
+                                                                           bp, buckets, op, ldo, odt, lp, chunk_width, scr, scr_n, s),
+                                           "gnnfd_aggregate_attention"))
+    return (out, lse) if with_lse else out
+
+
+def attention_backward_workspace_bytes(csr: Csr, csr_t: Csr, heads: int, dim: int, buckets: int = 0) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_attention_backward_workspace_bytes(csr.handle, csr_t.handle, heads, dim, buckets, ctypes.byref(s)),
+           "gnnfd_attention_backward_workspace_bytes")
+    return s.value
+
+
+def aggregate_attention_backward(csr: Csr, csr_t: Csr, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, dout: torch.Tensor,
+                                 lse: torch.Tensor, heads: int, dim: int, scale: float | None = None, softcap: float = 0.0,
+                                 dist: torch.Tensor | None = None, dist_t: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                                 chunk_width: int | None = None, out_dtype=None, scratch=None, stream=None):
+    """gnnfd_aggregate_attention_backward: (dq, dk, dv, dbias) for the gradient ``dout`` of aggregate_attention's result; dbias is None
+    without a bias.  ``csr_t`` is the CSR of the reversed edges (build_csr with src and dst exchanged and the same flags), ``dist_t`` the
+    buckets in its slot order, ``lse`` what the forward call returned."""
+    f = heads * dim
+    scale = dim ** -0.5 if scale is None else scale
+    chunk_width = f if chunk_width is None else chunk_width
+    if csr_t.device != csr.device or csr_t.n != csr.n or csr_t.nnz != csr.nnz:
+        raise ValueError("csr_t must be the reverse of csr: as many vertices and entries, on the same device")
+    operands, dp, bp, buckets = _attention_operands(csr, f, heads, dist, bias, q=q, k=k, v=v, dout=dout)
+    (qp, ldq), (kp, ldk), (vp_, ldv), (gp, ldg) = operands
+    if (dist_t is None) != (bias is None):
+        raise ValueError("dist_t and bias come together")
+    dtp = None
+    if dist_t is not None:
+        _check_dist(csr_t, dist_t, "dist_t")
+        dtp = dist_t.data_ptr()
+    if lse.dtype != torch.float32 or lse.dim() != 3 or lse.shape[0] < csr.n or tuple(lse.shape[1:]) != (heads, 2) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 [n, heads, 2] tensor")
+    _same_device(csr.device, lse=lse)
+    odt = out_dtype or torch.float32
+
+    def make():
+        grads = [torch.empty((csr.n, f), dtype=odt, device=csr.device) for _ in range(3)]
+        return grads + [torch.empty((buckets, heads), dtype=torch.float32, device=csr.device) if buckets else None]
+
+    dq, dk, dv, dbias = _take(make, stream)
+    if scratch is None:
+        scratch = _alloc_bytes(attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets), csr.device, stream)
+    scr, scr_n = _scratch_args(scratch, csr.device)
+    dt, code, bgp = _dtype_code(q), _dtype_code(dq), dbias.data_ptr() if buckets else None
+    _on_device(q, stream, lambda s: _check(lib().gnnfd_aggregate_attention_backward(
+        csr.handle, csr_t.handle, qp, ldq, kp, ldk, vp_, ldv, gp, ldg, dt, lse.data_ptr(), heads, dim, scale, softcap, dp, dtp, bp, buckets,
+        dq.data_ptr(), f, dk.data_ptr(), f, dv.data_ptr(), f, code, bgp, chunk_width, scr, scr_n, s), "gnnfd_aggregate_attention_backward"))
+    return dq, dk, dv, dbias
 
 
 def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int | None = None, out: torch.Tensor | None = None,
