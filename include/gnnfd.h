@@ -406,6 +406,42 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
                                        int64_t lddk, void* d_dv, int64_t lddv, gnnfd_dtype_t gdt, float* d_dbias, int32_t chunk_width,
                                        void* d_scratch, size_t scratch_bytes, void* stream);
 
+/* ------------------------------------------------------------------ group norm with an activation, over the graphs of a batch
+ *
+ * The step between two layers (the Update of Algorithm 1 is left to the user by the paper): rows graph_ptr[b] .. graph_ptr[b + 1] - 1 are the
+ * vertices of graph b, a group is f / groups neighbouring columns, and over the rows of a graph and the columns of a group
+ *   out = act((x - mean) * rstd * weight + bias),   rstd = (variance + eps)^-1/2  (the variance of all values there, not corrected).
+ * groups = 1 normalises a graph as a whole, groups = f each column of a graph by itself.
+ * d_x [n, ldx] of type xdt, d_out [n, ldo] of type odt (may be d_x itself, with ldo = ldx and odt = xdt).  d_graph_ptr [graphs + 1] of type itype, ascending
+ * from 0; NULL: one graph of n rows (graphs = 1).  Rows behind the last offset are left as they are; graphs may be empty (mean 0,
+ * rstd eps^-1/2).  Offsets outside [0, n] or not ascending are cut to what is inside: nothing outside of the arrays is touched.  d_weight, d_bias [f] fp32,
+ * either may be NULL (1 and 0).  d_mean, d_rstd [graphs, groups] fp32 receive the statistics; both may be NULL.  f up to 8192.
+ * Statistics, sums and the activation are fp32 or wider; the result is rounded once.  d_scratch:
+ * gnnfd_group_norm_workspace_bytes(n, f, groups, graphs, 0) bytes, 256-byte aligned.  The call only enqueues work. */
+typedef enum {
+    GNNFD_ACT_NONE = 0,
+    GNNFD_ACT_RELU = 1,
+    GNNFD_ACT_ELU = 2,   /* z > 0 ? z : e^z - 1 */
+    GNNFD_ACT_SILU = 3,  /* z / (1 + e^-z) */
+    GNNFD_ACT_GELU = 4   /* z / 2 * (1 + erf(z / sqrt 2)) */
+} gnnfd_activation_t;
+
+int gnnfd_group_norm_workspace_bytes(int64_t n, int32_t f, int32_t groups, int64_t graphs, int backward, size_t* scratch_bytes);
+
+int gnnfd_group_norm(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f, int32_t groups, int64_t graphs,
+                     const void* d_graph_ptr, gnnfd_itype_t itype, const float* d_weight, const float* d_bias, float eps, int activation,
+                     void* d_out, int64_t ldo, gnnfd_dtype_t odt, float* d_mean, float* d_rstd, void* d_scratch, size_t scratch_bytes,
+                     void* stream);
+
+/* The gradients of the above for d_dout [n, ldd] of type xdt: d_dx [n, lddx] of type gdt (rows behind the last offset are left as they
+ * are), and d_dweight, d_dbias [f] fp32, sums over the rows of all graphs (both NULL: not wanted).  d_mean, d_rstd as the forward call
+ * gave them; the other arguments as there.  relu's slope at 0 is 0.  d_dx may be d_dout itself (same pitch and type).  d_scratch:
+ * gnnfd_group_norm_workspace_bytes(n, f, groups, graphs, 1) bytes. */
+int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f,
+                              int32_t groups, int64_t graphs, const void* d_graph_ptr, gnnfd_itype_t itype, const float* d_weight,
+                              const float* d_bias, const float* d_mean, const float* d_rstd, int activation, void* d_dx, int64_t lddx,
+                              gnnfd_dtype_t gdt, float* d_dweight, float* d_dbias, void* d_scratch, size_t scratch_bytes, void* stream);
+
 /* ------------------------------------------------------------------ learned vertex features
  *
  * For graphs whose vertices have no features of their own (or a type, a degree, a name instead): a table with a learned row per

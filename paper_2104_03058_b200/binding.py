@@ -19,6 +19,7 @@ CSR_ADD_SELF_LOOPS, CSR_DEDUP, CSR_SYMMETRIZE, CSR_INPUT_ORDER = 1, 2, 4, 8
 OK, INVALID_ARG, BAD_INDEX, TOO_LARGE, WORKSPACE_TOO_SMALL, UNSUPPORTED, CUDA_ERROR = 0, -1, -2, -3, -4, -5, -6
 STATIC_SCRATCH_EXCEEDED = -7
 COMBINE_TF32, COMBINE_FP32 = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 
@@ -89,6 +90,10 @@ def lib() -> ctypes.CDLL:
         L.gnnfd_attention_backward_workspace_bytes.argtypes = [vp, vp, i32, i32, i32, pp(sz)]
         L.gnnfd_aggregate_attention_backward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, fl, fl, vp, vp, vp,
                                                          i32, vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, sz, vp]
+        L.gnnfd_group_norm_workspace_bytes.argtypes = [i64, i32, i32, i64, ctypes.c_int, pp(sz)]
+        L.gnnfd_group_norm.argtypes = [i64, vp, i64, i32, i32, i32, i64, vp, i32, vp, vp, fl, ctypes.c_int, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.gnnfd_group_norm_backward.argtypes = [i64, vp, i64, vp, i64, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, ctypes.c_int, vp, i64,
+                                                i32, vp, vp, vp, sz, vp]
         L.gnnfd_embedding.argtypes = [i64, vp, i32, i64, vp, i64, i32, i32, fl, vp, i64, i32, vp, vp]
         L.gnnfd_embedding_backward_workspace_bytes.argtypes = [i64, i64, i32, pp(sz)]
         L.gnnfd_embedding_backward.argtypes = [i64, vp, i32, vp, i64, i32, i64, i32, fl, i64, ctypes.c_int, vp, i64, i32, vp, sz, vp, vp]
@@ -865,6 +870,113 @@ def aggregate_attention_backward(csr: Csr, csr_t: Csr, q: torch.Tensor, k: torch
         csr.handle, csr_t.handle, qp, ldq, kp, ldk, vp_, ldv, gp, ldg, dt, lse.data_ptr(), heads, dim, scale, softcap, dp, dtp, bp, buckets,
         dq.data_ptr(), f, dk.data_ptr(), f, dv.data_ptr(), f, code, bgp, chunk_width, scr, scr_n, s), "gnnfd_aggregate_attention_backward"))
     return dq, dk, dv, dbias
+
+
+def group_norm_workspace_bytes(n: int, f: int, groups: int, graphs: int = 1, backward: bool = False) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_group_norm_workspace_bytes(n, f, groups, graphs, int(backward), ctypes.byref(s)), "gnnfd_group_norm_workspace_bytes")
+    return s.value
+
+
+def _norm_operands(x, groups: int, weight, bias, graph_ptr, activation: str, f: int):
+    """(weight pointer, bias pointer, graphs, offsets pointer, offsets type, activation code)"""
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != f or not t.is_contiguous() or t.device != x.device):
+            raise ValueError("%s must be a contiguous float32 tensor of %d values on %s" % (name, f, x.device))
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s" % ", ".join(ACTIVATIONS))
+    if groups < 1 or f % groups:
+        raise ValueError("%d columns do not make %d groups" % (f, groups))
+    graphs, pp, itype = 1, None, I32
+    if graph_ptr is not None:
+        pp, count, itype = _index_list(graph_ptr, "graph_ptr")
+        if count < 2 or graph_ptr.device != x.device:
+            raise ValueError("graph_ptr must hold graphs + 1 >= 2 offsets on %s" % x.device)
+        graphs = count - 1
+    return (None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), graphs, pp, itype,
+            ACTIVATIONS[activation])
+
+
+def _same_place(a, b) -> bool:
+    return a.data_ptr() == b.data_ptr() and a.stride() == b.stride() and a.dtype == b.dtype
+
+
+def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               graph_ptr: torch.Tensor | None = None, eps: float = 1e-5, activation: str = "none", f: int | None = None,
+               out: torch.Tensor | None = None, out_dtype=None, with_stats: bool = False, scratch=None, stream=None):
+    """gnnfd_group_norm: rows of x are vertices, ``graph_ptr`` [graphs + 1] the row offsets of the graphs of a batch (None: one graph), and
+    each of ``groups`` groups of columns is normalised over the rows of its graph, scaled, shifted and passed through the activation
+    ("none", "relu", "elu", "silu", "gelu").  ``out`` may be x itself.  Rows behind the last offset keep what ``out`` holds (undefined
+    where the call allocates it).  With ``with_stats`` the call returns (out, mean, rstd), each [graphs, groups], for group_norm_backward."""
+    f = x.shape[1] if f is None else f
+    n = x.shape[0]
+    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
+    xp, ldx = _matrix(x, f, "x")
+    if out is None:
+        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=x.device), stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        if not _same_place(x, out):
+            _no_overlap(x, out, "x", "out")
+    op, ldo = _matrix(out, f, "out")
+    mean = rstd = None
+    if with_stats:
+        mean, rstd = _take(lambda: torch.empty((2, graphs, groups), dtype=torch.float32, device=x.device), stream)
+    if scratch is None:
+        scratch = _alloc_bytes(group_norm_workspace_bytes(n, f, groups, graphs), x.device, stream)
+    scr, scr_n = _scratch_args(scratch, x.device)
+    xdt, odt = _dtype_code(x), _dtype_code(out)
+    mp, rp = (mean.data_ptr(), rstd.data_ptr()) if with_stats else (None, None)
+    _on_device(x, stream, lambda s: _check(lib().gnnfd_group_norm(n, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, eps, act, op, ldo, odt,
+                                                                  mp, rp, scr, scr_n, s), "gnnfd_group_norm"))
+    return (out, mean, rstd) if with_stats else out
+
+
+def _need_rows_of(t, rows: int, name: str):
+    if t.shape[0] < rows:
+        raise ValueError("%s has %d rows, x has %d" % (name, t.shape[0], rows))
+
+
+def group_norm_backward(dout: torch.Tensor, x: torch.Tensor, groups: int, mean: torch.Tensor, rstd: torch.Tensor,
+                        weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, graph_ptr: torch.Tensor | None = None,
+                        activation: str = "none", f: int | None = None, out: torch.Tensor | None = None, out_dtype=None,
+                        with_params: bool = True, scratch=None, stream=None):
+    """gnnfd_group_norm_backward: (dx, dweight, dbias) for the gradient ``dout`` of group_norm's result, of the type of x; dweight and dbias are
+    None where ``with_params`` is false.  ``mean`` and ``rstd`` are what the forward call returned; ``out`` receives dx and may be dout itself."""
+    f = x.shape[1] if f is None else f
+    n = x.shape[0]
+    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
+    xp, ldx = _matrix(x, f, "x")
+    dp, ldd = _matrix(dout, f, "dout")
+    if dout.dtype != x.dtype:
+        raise TypeError("dout must have the dtype of x")
+    _need_rows_of(dout, n, "dout")
+    _same_device(x.device, dout=dout)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or tuple(t.shape) != (graphs, groups) or not t.is_contiguous() or t.device != x.device:
+            raise ValueError("%s must be a contiguous float32 [graphs = %d, groups = %d] tensor on %s" % (name, graphs, groups, x.device))
+    if out is None:
+        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=x.device), stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        _no_overlap(x, out, "x", "out")
+        if not _same_place(dout, out):
+            _no_overlap(dout, out, "dout", "out")
+    op, ldo = _matrix(out, f, "out")
+    dweight = dbias = None
+    if with_params:
+        dweight, dbias = _take(lambda: torch.empty((2, f), dtype=torch.float32, device=x.device), stream)
+    if scratch is None:
+        scratch = _alloc_bytes(group_norm_workspace_bytes(n, f, groups, graphs, True), x.device, stream)
+    scr, scr_n = _scratch_args(scratch, x.device)
+    xdt, odt = _dtype_code(x), _dtype_code(out)
+    dwp, dbp = (dweight.data_ptr(), dbias.data_ptr()) if with_params else (None, None)
+    _on_device(x, stream, lambda s: _check(lib().gnnfd_group_norm_backward(n, dp, ldd, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, mean.data_ptr(),
+                                                                           rstd.data_ptr(), act, op, ldo, odt, dwp, dbp, scr, scr_n, s),
+                                           "gnnfd_group_norm_backward"))
+    return out, dweight, dbias
 
 
 def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int | None = None, out: torch.Tensor | None = None,

@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(_PKG, "libgnnfd.so")
 _OBJ_DIR = os.path.join(_PKG, "_build")
 
 SOURCES = ["runtime.cu", "csr_build.cu", "aggregate.cu", "aggregate_static.cu", "gat.cu", "edge_softmax.cu", "tune.cu", "combine.cu", "layer.cu", "oneshot.cu",
-           "embedding.cu", "attention.cu"]
+           "embedding.cu", "attention.cu", "group_norm.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

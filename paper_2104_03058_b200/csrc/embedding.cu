@@ -6,69 +6,12 @@
 // Neither does arithmetic worth counting: both are bound by HBM (the lookup reads n rows and writes n rows, the gradient
 // reads n rows and writes `vocab` rows), or by latency on small batches.
 #include "schedule.cuh"
-#include "vec.cuh"
+#include "rows.cuh"
 
 namespace gnnfd {
 
 constexpr int kEmbedBlock = 256;
 constexpr unsigned kSms = 148;
-
-// V elements of T with one load or store (16, 8, 4 or 2 bytes), as fp32 values
-template <typename T, int V>
-__device__ __forceinline__ void load_packed(const T* p, float (&x)[V])
-{
-    constexpr int kBytes = V * (int)sizeof(T);
-    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
-    if constexpr (kBytes == 16) {
-        const uint4 v = load16(p);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else if constexpr (kBytes == 8) {
-        asm("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    } else if constexpr (kBytes == 4) {
-        asm("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    } else {
-        unsigned short h;
-        asm("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
-        w[0] = h;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i]);
-        else x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);      // bf16 -> fp32 is exact
-    }
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-template <typename T, int V>
-__device__ __forceinline__ void store_packed(T* p, const float (&x)[V])
-{
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (V % 4 == 0) {
-#pragma unroll
-            for (int i = 0; i < V; i += 4) __stcs(reinterpret_cast<float4*>(p + i), make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]));
-        } else if constexpr (V == 2) {
-            __stcs(reinterpret_cast<float2*>(p), make_float2(x[0], x[1]));
-        } else {
-            __stcs(p, x[0]);
-        }
-    } else {
-        if constexpr (V == 8) {
-            __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]),
-                                                           pack_bf16(x[6], x[7])));
-        } else if constexpr (V == 4) {
-            __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])));
-        } else if constexpr (V == 2) {
-            __stcs(reinterpret_cast<unsigned int*>(p), pack_bf16(x[0], x[1]));
-        } else {
-            *p = __float2bfloat16_rn(x[0]);
-        }
-    }
-}
 
 // widest vector, in elements, that rows of `in` and of `out` can be read and written in: 16 bytes of `in`, 2 elements or 1
 static int embed_vector(const void* in, int64_t ld_in, gnnfd_dtype_t in_type, const void* out, int64_t ld_out, gnnfd_dtype_t out_type)
@@ -222,22 +165,11 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_sums(const __grid_
     const int share = (a.per_block + groups - 1) / groups;
     const int64_t first = min(base + (int64_t)g * share, end), last = min(first + share, end);
     const int c = ((int)blockIdx.y * (1 << a.lpr_log2) + lane) * V;
-    const bool whole = c + V <= a.f;
     auto key_of = [&](unsigned long long w) { return (int64_t)(w >> a.val_bits); };
     auto key_at = [&](int64_t i) { return key_of(a.words[i]); };
     const unsigned long long pos_mask = (1ull << a.val_bits) - 1ull;
-    auto load_row = [&](unsigned long long w, float (&x)[V]) {
-        const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)((w & pos_mask) - 1ull) * a.ldd + c;
-        if (whole) {
-            load_packed<TI, V>(p, x);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float one[1] = {0.f};
-                if (c + i < a.f) load_packed<TI, 1>(p + i, one);
-                x[i] = one[0];
-            }
-        }
+    auto load_dout = [&](unsigned long long w, float (&x)[V]) {
+        load_row<TI, V>(static_cast<const TI*>(a.dout) + (int64_t)((w & pos_mask) - 1ull) * a.ldd + c, a.f - c, x);
     };
     auto finish_row = [&](int64_t key, float (&x)[V]) {
         if (c < a.f) write_row<TO, V>(a, key, c, x);
@@ -273,7 +205,7 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_sums(const __grid_
             unsigned long long next[kInFlight];
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) {
-                if (w[u] != 0ull) load_row(w[u], x[u]);
+                if (w[u] != 0ull) load_dout(w[u], x[u]);
                 else
 #pragma unroll
                     for (int i = 0; i < V; ++i) x[u][i] = 0.f;
@@ -445,17 +377,7 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_few(const __grid_c
                     for (int i = 0; i < V; ++i) x[u][i] = 0.f;
                     if (here) {
                         const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)(i0 + __ffs(here) - 1) * a.ldd + c;
-                        if (c + V <= a.f) {
-                            load_packed<TI, V>(p, x[u]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < V; ++i)
-                                if (c + i < a.f) {
-                                    float one[1];
-                                    load_packed<TI, 1>(p + i, one);
-                                    x[u][i] = one[0];
-                                }
-                        }
+                        load_row<TI, V>(p, a.f - c, x[u]);
                         here &= here - 1u;
                         ++count;
                     }
