@@ -78,19 +78,4 @@ __device__ __forceinline__ void load_row(const T* p, int left, float (&x)[V])
         x[i] = one[0];
     }
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_row(T* p, int left, const float (&x)[V])
-{
-    if (left >= V) {
-        store_packed<T, V>(p, x);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i < left) {
-            const float one[1] = {x[i]};
-            store_packed<T, 1>(p + i, one);
-        }
-}
-
 }  // namespace gnnfd

@@ -1,9 +1,9 @@
 """Group norm with an activation and its gradients against an evaluation in 64 bits.
 
-Tolerances are first-order bounds, computed beside the reference (u = 2^-24 a rounding, R the largest distance of a value from its mean).  Means and sums
-of squares are taken over up to 64 rows at a time from distances to one of the rows (at most 2 R): the mean is off by at most u |mean| + 80 u 2 R from
-these sums and per_group / 32 + 5 more additions of distances of up to 2 R; a sum of squares of k <= 64 distances by (k + 3) u of itself, that is the
-variance by 70 u 4 R^2, and twice that with its square of the sum, and as much again in merging.  The rest is counted rounding by rounding.  Being
+Tolerances are first-order bounds, computed beside the reference (u = 2^-24 a rounding, R the largest distance of a value from its mean).  Distances are
+counted from the mean of some of the values, so none is above 2 R, and a thread adds up at most 128 rows of them here (pieces of graphs this size are
+shorter): the mean is off by at most u |mean| + 128 u 2 R and what per_group / 16 + 42 more additions add; a sum of k <= 128 squares by
+(k + 3) u of itself, that is the variance by 135 u 4 R^2, twice that with the square of the sum, and as much again in merging.  Being
 bounds, they are wide for most values, so fp32 results also have to be within 16 u in the root mean square: an output carries
 about ten roundings, half a step each at most, and the statistics' errors average out over thousands of terms."""
 import math
@@ -66,7 +66,7 @@ def reference(x, groups, weight, bias, ptr, act, eps, dout=None):
         0, row[:, None].expand(used, groups), off.abs().amax(2), "amax")
     rstd = (var + eps) ** -0.5
     e_mean = U * mean.abs() + (160 + per / 16 + 10) * U * 2 * top
-    e_var = 2 * 70 * U * 4 * top ** 2 * 2 + 4 * U * var
+    e_var = 2 * 135 * U * 4 * top ** 2 * 2 + 4 * U * var
     e_r = 0.5 * e_var / (var + eps) + 2 * U
     rr, er = rstd[row][:, :, None], e_r[row][:, :, None]
     xhat = off * rr
