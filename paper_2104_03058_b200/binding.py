@@ -701,28 +701,31 @@ def layer(csr: Csr, model: str, x: torch.Tensor, w_t: torch.Tensor, f_in: int | 
     return out
 
 
-def _on_device(t: torch.Tensor, stream, work):
-    """work(stream handle) with the device of `t` current: kernels are launched on the current device, and the stream handed over is
-    that device's current one where none is named."""
-    index = t.device.index
-    if stream is not None:
-        if stream.device != t.device:
-            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, t.device))
-        handle = stream.cuda_stream
-    else:
-        handle = torch._C._cuda_getCurrentRawStream(index)
-    if index == torch.cuda.current_device():
-        return work(handle)
-    with torch.cuda.device(index):
-        return work(handle)
+# Kernels are launched on the current device, so the entry points below make that of their tensors current where it is another one: they call
+# themselves once more inside _elsewhere.
+_current_device = torch._C._cuda_getDevice
 
 
-def _take(make, stream):
-    """Memory that a call allocates: taken under the stream the work runs on (see _alloc_bytes)."""
+def _elsewhere(device, stream, again, *args, **kwargs):
+    with torch.cuda.device(device):
+        return again(*args, stream=stream, **kwargs)
+
+
+def _stream_handle(index: int, stream) -> int:
+    """Raw handle of the stream named, or of the current one of device `index`, which is the current device."""
     if stream is None:
-        return make()
+        return torch._C._cuda_getCurrentRawStream(index)
+    if stream.device.index != index:
+        raise ValueError("the stream is on %s, the tensors are on cuda:%d" % (stream.device, index))
+    return stream.cuda_stream
+
+
+def _new(like: torch.Tensor, shape, dtype, stream):
+    """Memory that a call allocates beside a tensor: taken under the stream the work runs on (see _alloc_bytes)."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return make()
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _index_list(ids: torch.Tensor, name: str):
@@ -800,28 +803,30 @@ def aggregate_attention(csr: Csr, q: torch.Tensor, k: torch.Tensor, v: torch.Ten
     """gnnfd_aggregate_attention: softmax attention of every vertex over the sources of its edges.  ``scale`` defaults to dim ** -0.5;
     ``dist`` holds a bucket of ``bias`` ([buckets, heads]) per CSR slot (see edge_values).  With ``with_lse`` the call returns
     (out, lse [n, heads, 2]), which aggregate_attention_backward takes."""
+    index = csr.device.index
+    if index != _current_device():
+        return _elsewhere(csr.device, stream, aggregate_attention, csr, q, k, v, heads, dim, scale, softcap, dist, bias, chunk_width, out,
+                          out_dtype, with_lse, scratch)
     f = heads * dim
     scale = dim ** -0.5 if scale is None else scale
     chunk_width = f if chunk_width is None else chunk_width
     ((qp, ldq), (kp, ldk), (vp_, ldv)), dp, bp, buckets = _attention_operands(csr, f, heads, dist, bias, q=q, k=k, v=v)
     fresh = out is None
     if fresh:
-        out = _take(lambda: torch.empty((csr.n, f), dtype=out_dtype or torch.float32, device=csr.device), stream)
+        out = _new(q, (csr.n, f), out_dtype or torch.float32, stream)
     op, ldo = _matrix(out, f, "out")
     if not fresh:
         _same_device(csr.device, out=out)
         _need_rows(out, csr.n, "out")
         for name, t in (("q", q), ("k", k), ("v", v)):
             _no_overlap(t, out, name, "out")
-    lse = _take(lambda: torch.empty((csr.n, heads, 2), dtype=torch.float32, device=csr.device), stream) if with_lse else None
-    if scratch is None:
-        need = attention_workspace_bytes(csr, heads, dim)
-        scratch = _alloc_bytes(need, csr.device, stream) if need else None
+    lse = _new(q, (csr.n, heads, 2), torch.float32, stream) if with_lse else None
+    if scratch is None and csr.n_segments:
+        scratch = _new(q, attention_workspace_bytes(csr, heads, dim), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, csr.device)
     dt, odt, lp = _dtype_code(q), _dtype_code(out), lse.data_ptr() if with_lse else None
-    _on_device(q, stream, lambda s: _check(lib().gnnfd_aggregate_attention(csr.handle, qp, ldq, kp, ldk, vp_, ldv, dt, heads, dim, scale, softcap, dp,
-                                                                           bp, buckets, op, ldo, odt, lp, chunk_width, scr, scr_n, s),
-                                           "gnnfd_aggregate_attention"))
+    _check(lib().gnnfd_aggregate_attention(csr.handle, qp, ldq, kp, ldk, vp_, ldv, dt, heads, dim, scale, softcap, dp, bp, buckets, op, ldo, odt, lp,
+                                           chunk_width, scr, scr_n, _stream_handle(index, stream)), "gnnfd_aggregate_attention")
     return (out, lse) if with_lse else out
 
 
@@ -839,6 +844,10 @@ def aggregate_attention_backward(csr: Csr, csr_t: Csr, q: torch.Tensor, k: torch
     """gnnfd_aggregate_attention_backward: (dq, dk, dv, dbias) for the gradient ``dout`` of aggregate_attention's result; dbias is None
     without a bias.  ``csr_t`` is the CSR of the reversed edges (build_csr with src and dst exchanged and the same flags), ``dist_t`` the
     buckets in its slot order, ``lse`` what the forward call returned."""
+    index = csr.device.index
+    if index != _current_device():
+        return _elsewhere(csr.device, stream, aggregate_attention_backward, csr, csr_t, q, k, v, dout, lse, heads, dim, scale, softcap, dist,
+                          dist_t, bias, chunk_width, out_dtype, scratch)
     f = heads * dim
     scale = dim ** -0.5 if scale is None else scale
     chunk_width = f if chunk_width is None else chunk_width
@@ -857,18 +866,16 @@ def aggregate_attention_backward(csr: Csr, csr_t: Csr, q: torch.Tensor, k: torch
     _same_device(csr.device, lse=lse)
     odt = out_dtype or torch.float32
 
-    def make():
-        grads = [torch.empty((csr.n, f), dtype=odt, device=csr.device) for _ in range(3)]
-        return grads + [torch.empty((buckets, heads), dtype=torch.float32, device=csr.device) if buckets else None]
-
-    dq, dk, dv, dbias = _take(make, stream)
+    dq, dk, dv = (_new(q, (csr.n, f), odt, stream) for _ in range(3))
+    dbias = _new(q, (buckets, heads), torch.float32, stream) if buckets else None
     if scratch is None:
-        scratch = _alloc_bytes(attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets), csr.device, stream)
+        scratch = _new(q, max(256, attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets)), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, csr.device)
     dt, code, bgp = _dtype_code(q), _dtype_code(dq), dbias.data_ptr() if buckets else None
-    _on_device(q, stream, lambda s: _check(lib().gnnfd_aggregate_attention_backward(
+    _check(lib().gnnfd_aggregate_attention_backward(
         csr.handle, csr_t.handle, qp, ldq, kp, ldk, vp_, ldv, gp, ldg, dt, lse.data_ptr(), heads, dim, scale, softcap, dp, dtp, bp, buckets,
-        dq.data_ptr(), f, dk.data_ptr(), f, dv.data_ptr(), f, code, bgp, chunk_width, scr, scr_n, s), "gnnfd_aggregate_attention_backward"))
+        dq.data_ptr(), f, dk.data_ptr(), f, dv.data_ptr(), f, code, bgp, chunk_width, scr, scr_n, _stream_handle(index, stream)),
+        "gnnfd_aggregate_attention_backward")
     return dq, dk, dv, dbias
 
 
@@ -908,12 +915,15 @@ def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     each of ``groups`` groups of columns is normalised over the rows of its graph, scaled, shifted and passed through the activation
     ("none", "relu", "elu", "silu", "gelu").  ``out`` may be x itself.  Rows behind the last offset keep what ``out`` holds (undefined
     where the call allocates it).  With ``with_stats`` the call returns (out, mean, rstd), each [graphs, groups], for group_norm_backward."""
-    f = x.shape[1] if f is None else f
-    n = x.shape[0]
-    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, group_norm, x, groups, weight, bias, graph_ptr, eps, activation, f, out, out_dtype, with_stats, scratch)
+    n, width = x.shape
+    f = width if f is None else f
     xp, ldx = _matrix(x, f, "x")
+    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
     if out is None:
-        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=x.device), stream)
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
     else:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
@@ -922,14 +932,14 @@ def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     op, ldo = _matrix(out, f, "out")
     mean = rstd = None
     if with_stats:
-        mean, rstd = _take(lambda: torch.empty((2, graphs, groups), dtype=torch.float32, device=x.device), stream)
+        mean, rstd = _new(x, (2, graphs, groups), torch.float32, stream)
     if scratch is None:
-        scratch = _alloc_bytes(group_norm_workspace_bytes(n, f, groups, graphs), x.device, stream)
+        scratch = _new(x, group_norm_workspace_bytes(n, f, groups, graphs), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, x.device)
     xdt, odt = _dtype_code(x), _dtype_code(out)
     mp, rp = (mean.data_ptr(), rstd.data_ptr()) if with_stats else (None, None)
-    _on_device(x, stream, lambda s: _check(lib().gnnfd_group_norm(n, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, eps, act, op, ldo, odt,
-                                                                  mp, rp, scr, scr_n, s), "gnnfd_group_norm"))
+    _check(lib().gnnfd_group_norm(n, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, eps, act, op, ldo, odt, mp, rp, scr, scr_n,
+                                  _stream_handle(index, stream)), "gnnfd_group_norm")
     return (out, mean, rstd) if with_stats else out
 
 
@@ -944,10 +954,14 @@ def group_norm_backward(dout: torch.Tensor, x: torch.Tensor, groups: int, mean: 
                         with_params: bool = True, scratch=None, stream=None):
     """gnnfd_group_norm_backward: (dx, dweight, dbias) for the gradient ``dout`` of group_norm's result, of the type of x; dweight and dbias are
     None where ``with_params`` is false.  ``mean`` and ``rstd`` are what the forward call returned; ``out`` receives dx and may be dout itself."""
-    f = x.shape[1] if f is None else f
-    n = x.shape[0]
-    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, group_norm_backward, dout, x, groups, mean, rstd, weight, bias, graph_ptr, activation, f, out,
+                          out_dtype, with_params, scratch)
+    n, width = x.shape
+    f = width if f is None else f
     xp, ldx = _matrix(x, f, "x")
+    wp, bp, graphs, pp, itype, act = _norm_operands(x, groups, weight, bias, graph_ptr, activation, f)
     dp, ldd = _matrix(dout, f, "dout")
     if dout.dtype != x.dtype:
         raise TypeError("dout must have the dtype of x")
@@ -957,7 +971,7 @@ def group_norm_backward(dout: torch.Tensor, x: torch.Tensor, groups: int, mean: 
         if t.dtype != torch.float32 or tuple(t.shape) != (graphs, groups) or not t.is_contiguous() or t.device != x.device:
             raise ValueError("%s must be a contiguous float32 [graphs = %d, groups = %d] tensor on %s" % (name, graphs, groups, x.device))
     if out is None:
-        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=x.device), stream)
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
     else:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
@@ -967,15 +981,14 @@ def group_norm_backward(dout: torch.Tensor, x: torch.Tensor, groups: int, mean: 
     op, ldo = _matrix(out, f, "out")
     dweight = dbias = None
     if with_params:
-        dweight, dbias = _take(lambda: torch.empty((2, f), dtype=torch.float32, device=x.device), stream)
+        dweight, dbias = _new(x, (2, f), torch.float32, stream)
     if scratch is None:
-        scratch = _alloc_bytes(group_norm_workspace_bytes(n, f, groups, graphs, True), x.device, stream)
+        scratch = _new(x, group_norm_workspace_bytes(n, f, groups, graphs, True), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, x.device)
     xdt, odt = _dtype_code(x), _dtype_code(out)
     dwp, dbp = (dweight.data_ptr(), dbias.data_ptr()) if with_params else (None, None)
-    _on_device(x, stream, lambda s: _check(lib().gnnfd_group_norm_backward(n, dp, ldd, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, mean.data_ptr(),
-                                                                           rstd.data_ptr(), act, op, ldo, odt, dwp, dbp, scr, scr_n, s),
-                                           "gnnfd_group_norm_backward"))
+    _check(lib().gnnfd_group_norm_backward(n, dp, ldd, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, mean.data_ptr(), rstd.data_ptr(), act,
+                                           op, ldo, odt, dwp, dbp, scr, scr_n, _stream_handle(index, stream)), "gnnfd_group_norm_backward")
     return out, dweight, dbias
 
 
@@ -983,14 +996,18 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int
               out_dtype=None, status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """gnnfd_embedding: out[i] = scale * table[ids[i], :f].  ``status`` is an int32 tensor of one element whose bit 0 the kernel sets
     where an id lies outside the table (its output row is zero)."""
-    f = table.shape[1] if f is None else f
+    index = table.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(table.device, stream, embedding, table, ids, scale, f, out, out_dtype, status)
+    vocab, width = table.shape
+    f = width if f is None else f
     ip, n, itype = _index_list(ids, "ids")
     tp, ldt = _matrix(table, f, "table")
     fresh = out is None
     if fresh:
-        out = _take(lambda: torch.empty((n, f), dtype=out_dtype or torch.float32, device=table.device), stream)
+        out = _new(table, (n, f), out_dtype or torch.float32, stream)
     op, ldo = _matrix(out, f, "out")
-    if ids.device != table.device or out.device != table.device:
+    if ids.get_device() != index or out.get_device() != index:
         raise ValueError("table, ids and out must be on one device")
     if not fresh:
         _need_ids(out, n, "out")
@@ -998,8 +1015,7 @@ def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int
         _no_overlap(ids, out, "ids", "out")
     sp = _status_ptr(status, table.device)
     tdt, odt = _dtype_code(table), _dtype_code(out)
-    _on_device(table, stream, lambda s: _check(lib().gnnfd_embedding(n, ip, itype, table.shape[0], tp, ldt, tdt, f, scale, op, ldo, odt, sp, s),
-                                               "gnnfd_embedding"))
+    _check(lib().gnnfd_embedding(n, ip, itype, vocab, tp, ldt, tdt, f, scale, op, ldo, odt, sp, _stream_handle(index, stream)), "gnnfd_embedding")
     return out
 
 
@@ -1019,6 +1035,10 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
                        status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """gnnfd_embedding_backward: the gradient [vocab, f] of a table from the gradients of the rows looked up.  ``accumulate`` adds to
     ``out`` (which must then be given); ids equal to ``padding_idx`` take no part; ``status``: see the header."""
+    index = dout.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(dout.device, stream, embedding_backward, ids, dout, vocab, scale, padding_idx, accumulate, f, out, out_dtype, scratch,
+                          status)
     f = dout.shape[1] if f is None else f
     ip, n, itype = _index_list(ids, "ids")
     dp, ldd = _matrix(dout, f, "dout")
@@ -1027,9 +1047,9 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
     if fresh:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to (out)")
-        out = _take(lambda: torch.empty((vocab, f), dtype=out_dtype or torch.float32, device=dout.device), stream)
+        out = _new(dout, (vocab, f), out_dtype or torch.float32, stream)
     op, ldo = _matrix(out, f, "out")
-    if ids.device != dout.device or out.device != dout.device:
+    if ids.get_device() != index or out.get_device() != index:
         raise ValueError("ids, dout and out must be on one device")
     if not fresh:
         if out.shape[0] < vocab:
@@ -1038,14 +1058,13 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
         _no_overlap(ids, out, "ids", "out")
     if scratch is None:
         need = embedding_backward_workspace_bytes(n, vocab, f)
-        scratch = _alloc_bytes(need, dout.device, stream) if need else None
+        scratch = _new(dout, need, torch.uint8, stream) if need else None
     scr, scr_n = _scratch_args(scratch, dout.device)
     sp = _status_ptr(status, dout.device)
     padding = -1 if padding_idx is None else padding_idx
     ddt, odt = _dtype_code(dout), _dtype_code(out)
-    _on_device(dout, stream, lambda s: _check(lib().gnnfd_embedding_backward(n, ip, itype, dp, ldd, ddt, vocab, f, scale, padding,
-                                                                             int(accumulate), op, ldo, odt, scr, scr_n, sp, s),
-                                              "gnnfd_embedding_backward"))
+    _check(lib().gnnfd_embedding_backward(n, ip, itype, dp, ldd, ddt, vocab, f, scale, padding, int(accumulate), op, ldo, odt, scr, scr_n, sp,
+                                          _stream_handle(index, stream)), "gnnfd_embedding_backward")
     return out
 
 

@@ -65,20 +65,18 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_rows(const __grid_const
     TO* const out = static_cast<TO*>(a.out);
     for (int c = lane * V; c < a.f; c += lpr * V) {
         if (c + V <= a.f) {
-            float x[U][V];
+            Raw<TI, V> raw[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (src[u]) load_packed<TI, V>(src[u] + c, x[u]);
-                else
-#pragma unroll
-                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
-            }
+            for (int u = 0; u < U; ++u)
+                if (src[u]) raw[u].load(src[u] + c);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t row = row0 + (int64_t)u * groups;
+                float x[V];
+                raw[u].get(x);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[u][i] = src[u] ? x[u][i] * a.scale : 0.f;
-                if (row < a.n) store_packed<TO, V>(out + row * a.ldo + c, x[u]);
+                for (int i = 0; i < V; ++i) x[i] = src[u] ? x[i] * a.scale : 0.f;
+                if (row < a.n) store_packed<TO, V>(out + row * a.ldo + c, x);
             }
         } else {
             for (int i = c; i < a.f; ++i)
@@ -107,7 +105,7 @@ struct GradArgs {
     uint8_t* mark;                         // [vocab] rows that get a sum, zeroed (null where the gradient is added to what is there)
     int32_t* status;
     float scale;
-    int32_t f, fpad, lpr_log2, val_bits, per_block, n_blocks, col_tiles, accumulate;
+    int32_t f, fpad, lpr_log2, val_bits, per_block, n_blocks, wide, accumulate;
 };
 
 template <typename TO, int V>
@@ -144,173 +142,192 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int64_t row, int c,
     }
 }
 
-// Sums over runs of equal ids.  A block takes per_block sorted ids, a group of lanes a consecutive share of them, and walks it with kInFlight
-// rows loaded at a time, adding until the id changes.  A run that lies inside a group's share is written at once; what a group has of a run that
-// goes on before or behind its share meets in shared memory, and is added there in order by the group that has the run's beginning;
-// what a block has of a run that goes on in other blocks is left for embedding_grad_finish.
+// Sums over runs of equal ids.  A block takes per_block sorted ids, a group of lanes a consecutive share of them.  The lanes of a group read as many words
+// at a time and pass them round; kInFlight rows are loaded together and added until the id changes.  A run that lies inside a group's share is
+// written at once; what a group has of a run that goes on before or behind its share meets in shared memory, and is added there in order by the group that
+// has the run's beginning; what a block has of a run that goes on in other blocks is left for embedding_grad_finish.
+//
+// Q: vectors per lane, 32 lanes apart, for rows of more than 32 vectors: narrow vectors would leave little in flight and read the words once per 32 of
+// them (300,000 ids, 602 fp32 columns in rows that start on 8 bytes: 8-byte vectors 400 us, four of them a lane 213).
 constexpr int kInFlight = 8;
+constexpr int wide_lane(int v) { return v == 8 ? 1 : v == 4 ? 2 : 4; }       // the most vectors of a lane
 
-template <typename TI, typename TO, int V>
-__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_sums(const __grid_constant__ GradArgs a)
+template <typename TI, typename TO, int V, int Q>
+__global__ void __launch_bounds__(kEmbedBlock, V == 8 ? 2 : 3) embedding_grad_sums(const __grid_constant__ GradArgs a)
 {
+    constexpr int U = Q == 1 ? kInFlight : kInFlight / 2, W = V * Q;
     grid_dependency<true>();
-    __shared__ float ends[2][kEmbedBlock][V];            // a group's first (run begun earlier) and last (run that goes on) sums
+    constexpr unsigned kFull = 0xffffffffu;
+    __shared__ float ends[2][kEmbedBlock][W];            // a group's first (run begun earlier) and last (run that goes on) sums
     __shared__ bool through[kEmbedBlock];                // of a group: all of its share belongs to a run begun earlier that goes on
     if (a.counts->sort_failed) return;
     const int64_t n_valid = a.counts->n_valid;
-    const int groups = kEmbedBlock >> a.lpr_log2, g = threadIdx.x >> a.lpr_log2, lane = threadIdx.x & ((1 << a.lpr_log2) - 1);
+    const int lpr = 1 << a.lpr_log2, groups = kEmbedBlock >> a.lpr_log2, g = threadIdx.x >> a.lpr_log2, lane = threadIdx.x & (lpr - 1);
     const int64_t base = (int64_t)blockIdx.x * a.per_block;
     if (base >= n_valid) return;
     const int64_t end = min(base + a.per_block, n_valid);
     const int share = (a.per_block + groups - 1) / groups;
-    const int64_t first = min(base + (int64_t)g * share, end), last = min(first + share, end);
-    const int c = ((int)blockIdx.y * (1 << a.lpr_log2) + lane) * V;
-    auto key_of = [&](unsigned long long w) { return (int64_t)(w >> a.val_bits); };
-    auto key_at = [&](int64_t i) { return key_of(a.words[i]); };
-    const unsigned long long pos_mask = (1ull << a.val_bits) - 1ull;
-    auto load_dout = [&](unsigned long long w, float (&x)[V]) {
-        load_row<TI, V>(static_cast<const TI*>(a.dout) + (int64_t)((w & pos_mask) - 1ull) * a.ldd + c, a.f - c, x);
-    };
-    auto finish_row = [&](int64_t key, float (&x)[V]) {
-        if (c < a.f) write_row<TO, V>(a, key, c, x);
+    const int64_t first = min(base + (int64_t)g * share, end);
+    const int count = (int)(min(first + share, end) - first);
+    const int c = ((int)blockIdx.y * lpr * Q + lane) * V, pitch_q = lpr * V;      // vector q: columns c + q * pitch_q ..
+    auto key_of = [&](unsigned long long w) { return (uint32_t)(w >> a.val_bits); };
+    const uint32_t pos_mask = (uint32_t)((1ull << a.val_bits) - 1ull);
+    const TI* const dout = static_cast<const TI*>(a.dout) + c;
+    const uint32_t pitch = (uint32_t)a.ldd;
+    auto finish_row = [&](uint32_t key, float (&x)[Q][V]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (c + q * pitch_q < a.f) write_row<TO, V>(a, key, c + q * pitch_q, x[q]);
         if (a.mark && c == 0 && key != a.padding) a.mark[key] = 1;
     };
 
     bool head = false, tail = false, passes = false;
-    int64_t cur = -1;
-    if (first < last) {
-        float acc[V];
+    float acc[Q][V];
+    auto clear = [&]() {
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.f;
-        cur = key_at(first);
-        bool open = first > 0 && key_at(first - 1) == cur;             // the run was begun earlier
-        auto flush = [&](bool goes_on) {
-            if (open || goes_on) {
+        for (int q = 0; q < Q; ++q)
 #pragma unroll
-                for (int i = 0; i < V; ++i) ends[open ? 0 : 1][threadIdx.x][i] = acc[i];
-                head |= open;
-                tail |= !open;
-                passes |= open && goes_on;
-            } else {
-                finish_row(cur, acc);
+            for (int i = 0; i < V; ++i) acc[q][i] = 0.f;
+    };
+    clear();
+    uint32_t cur = count > 0 ? key_of(a.words[first]) : 0u;
+    bool open = count > 0 && first > 0 && key_of(a.words[first - 1]) == cur;       // the run was begun earlier
+    auto flush = [&](bool goes_on) {
+        if (open || goes_on) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) ends[open ? 0 : 1][threadIdx.x][i] = acc[i / V][i % V];
+            head |= open;
+            tail |= !open;
+            passes |= open && goes_on;
+        } else {
+            finish_row(cur, acc);
+        }
+        clear();
+    };
+    unsigned long long word = lane < count ? a.words[first + lane] : 0ull;
+    for (int t0 = 0; t0 < share; t0 += lpr) {              // (all groups of a warp make as many turns)
+        const uint32_t key = key_of(word), pos = ((uint32_t)word & pos_mask) - 1u;
+        const int valid = count - t0;                      // of this turn's ids, where below lpr
+        word = t0 + lpr + lane < count ? a.words[first + t0 + lpr + lane] : 0ull;
+        for (int j0 = 0; j0 < lpr; j0 += U) {
+            if (t0 + j0 >= share) break;
+            float x[U][Q][V];
+            uint32_t k[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t at = __shfl_sync(kFull, pos, j0 + u, lpr);
+                k[u] = __shfl_sync(kFull, key, j0 + u, lpr);
+                const TI* const p = dout + (uint64_t)at * pitch;
+                if (j0 + u < valid)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) {
+                        if (c + q * pitch_q + V <= a.f) load_packed<TI, V>(p + q * pitch_q, x[u][q]);
+                        else load_row<TI, V>(p + q * pitch_q, a.f - c - q * pitch_q, x[u][q]);
+                    }
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] = 0.f;
-        };
-        unsigned long long w[kInFlight];
-#pragma unroll
-        for (int u = 0; u < kInFlight; ++u) w[u] = first + u < last ? a.words[first + u] : 0ull;
-        for (int64_t t = first; t < last; t += kInFlight) {
-            float x[kInFlight][V];
-            unsigned long long next[kInFlight];
-#pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                if (w[u] != 0ull) load_dout(w[u], x[u]);
-                else
-#pragma unroll
-                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
-            }
-#pragma unroll
-            for (int u = 0; u < kInFlight; ++u) next[u] = t + kInFlight + u < last ? a.words[t + kInFlight + u] : 0ull;
-#pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                if (w[u] == 0ull) continue;                            // (a word holds position + 1: never 0)
-                const int64_t key = key_of(w[u]);
-                if (key != cur) {
+            for (int u = 0; u < U; ++u) {
+                if (j0 + u >= valid) continue;
+                if (k[u] != cur) {
                     flush(false);
-                    cur = key;
+                    cur = k[u];
                     open = false;
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += x[u][i];
-            }
+                for (int q = 0; q < Q; ++q)
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) w[u] = next[u];
+                    for (int i = 0; i < V; ++i) acc[q][i] += x[u][q][i];
+            }
         }
-        flush(last < n_valid && key_at(last) == cur);
     }
-    through[g] = passes;                                               // (all lanes of a group agree)
+    if (count > 0) flush(first + count < n_valid && key_of(a.words[first + count]) == cur);
+    if (lane == 0) through[g] = passes;
     __syncthreads();
 
     // which: 0 the run that this group's share begins inside of (asked of the block's first group), 1 the one it ends inside of
-    auto join = [&](int which, int64_t key) {
-        float sum[V];
+    auto join = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = ends[which][threadIdx.x][i];
+        for (int i = 0; i < W; ++i) acc[i / V][i % V] = ends[which][threadIdx.x][i];
         bool goes_on = which == 1 || passes;
         const int used = ((int)(end - base) + share - 1) / share;      // the groups with a share
         for (int h = g + 1; goes_on && h < used; ++h) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += ends[0][(h << a.lpr_log2) + lane][i];
+            for (int i = 0; i < W; ++i) acc[i / V][i % V] += ends[0][(h << a.lpr_log2) + lane][i];
             goes_on = through[h];
         }
         if (which == 1 && !goes_on) {
-            finish_row(key, sum);
+            finish_row(cur, acc);
             return;
         }
-        float* const part = (which ? a.tail : a.head) + (int64_t)blockIdx.x * a.fpad + c;
+        float* const part = (which ? a.tail : a.head) + (int64_t)blockIdx.x * a.fpad;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (c + i < a.f) part[i] = sum[i];
-        if (which == 1 && a.mark && c == 0 && key != a.padding) a.mark[key] = 1;
+        for (int i = 0; i < W; ++i) {
+            const int col = c + i / V * pitch_q + i % V;
+            if (col < a.f) part[col] = acc[i / V][i % V];
+        }
+        if (which == 1 && a.mark && c == 0 && cur != a.padding) a.mark[cur] = 1;
     };
-    if (head && g == 0) join(0, -1);
-    if (tail) join(1, cur);
+    if (head && g == 0) join(0);
+    if (tail) join(1);
 }
 
-// The first n_blocks * col_tiles blocks: a run that begins in block b of the sums and goes on is added up over the blocks it
-// reaches, kJoinWays interleaved walks at a time.  The others: rows that no id names become zero.
-constexpr int kJoinCols = 64, kJoinWays = kEmbedBlock / kJoinCols;
+// The first n_blocks blocks: a run that begins in block b of the sums and goes on is added up over the blocks it
+// reaches, in interleaved walks for as many columns as leave four of them or less.  The others: rows that no id names become zero.
 
 template <typename TO>
-__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __grid_constant__ GradArgs a, int join_tiles, int vec)
+__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __grid_constant__ GradArgs a, int vec)
 {
     grid_dependency<true>();
-    __shared__ float sums[kJoinWays][kJoinCols];
+    __shared__ float sums[kEmbedBlock];
     if (a.counts->sort_failed) {
         if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, 2);
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status && a.counts->bad_index) atomicOr(a.status, 1);
     const int64_t n_valid = a.counts->n_valid;
-    const int64_t join_blocks = (int64_t)a.n_blocks * join_tiles;
+    const int64_t join_blocks = a.n_blocks;
     if (blockIdx.x < join_blocks) {
-        const int64_t b = blockIdx.x / join_tiles, begin = b * a.per_block, next = begin + a.per_block;
+        const int64_t b = blockIdx.x, begin = b * a.per_block, next = begin + a.per_block;
         auto key_at = [&](int64_t i) { return (int64_t)(a.words[i] >> a.val_bits); };
         if (next >= n_valid) return;
         const int64_t key = key_at(next);
         if (key_at(next - 1) != key || (begin > 0 && key_at(begin - 1) == key)) return;      // nothing goes on, or it was begun earlier
-        const int c = (int)(blockIdx.x % join_tiles) * kJoinCols + (int)threadIdx.x % kJoinCols, way = threadIdx.x / kJoinCols;
-        float sum = 0.f;
-        if (c < a.f) {
-            if (way == 0) sum = a.tail[b * a.fpad + c];
-            constexpr int kAhead = 4;                    // blocks of a walk whose words and sums are read together
-            for (int64_t at = b + 1 + way; at < a.n_blocks && at * a.per_block < n_valid;) {
-                float part[kAhead];
-                bool same[kAhead];
+        const int cols = a.f <= 64 ? 64 : a.f <= 128 ? 128 : 256, ways = kEmbedBlock / cols;
+        const int at_col = threadIdx.x & (cols - 1), way = threadIdx.x / cols;
+        for (int c0 = 0; c0 < a.f; c0 += cols) {
+            const int c = c0 + at_col;
+            float sum = 0.f;
+            if (c < a.f) {
+                if (way == 0) sum = a.tail[b * a.fpad + c];
+                constexpr int kAhead = 4;                // blocks of a walk whose words and sums are read together
+                for (int64_t at = b + 1 + way; at < a.n_blocks && at * a.per_block < n_valid;) {
+                    float part[kAhead];
+                    bool same[kAhead];
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int64_t block = at + i * kJoinWays;
-                    same[i] = block < a.n_blocks && block * a.per_block < n_valid && key_at(block * a.per_block) == key;
-                    part[i] = same[i] ? a.head[block * a.fpad + c] : 0.f;
-                }
-                bool on = true;
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int64_t block = at + i * ways;
+                        same[i] = block < a.n_blocks && block * a.per_block < n_valid && key_at(block * a.per_block) == key;
+                        part[i] = same[i] ? a.head[block * a.fpad + c] : 0.f;
+                    }
+                    bool on = true;
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    on = on && same[i];
-                    if (on) sum += part[i];
+                    for (int i = 0; i < kAhead; ++i) {
+                        on = on && same[i];
+                        if (on) sum += part[i];
+                    }
+                    if (!on) break;
+                    at += kAhead * ways;
                 }
-                if (!on) break;
-                at += kAhead * kJoinWays;
             }
+            sums[threadIdx.x] = sum;
+            __syncthreads();
+            if (way == 0 && c < a.f) {
+                float x[1] = {sum};
+                for (int w = 1; w < ways; ++w) x[0] += sums[w * cols + at_col];
+                write_row<TO, 1>(a, key, c, x);
+            }
+            __syncthreads();
         }
-        sums[way][threadIdx.x % kJoinCols] = sum;
-        __syncthreads();
-        if (way != 0 || c >= a.f) return;
-        float x[1] = {sum};
-#pragma unroll
-        for (int w = 1; w < kJoinWays; ++w) x[0] += sums[w][threadIdx.x];
-        write_row<TO, 1>(a, key, c, x);
         return;
     }
     // zero rows: 2^lpr_log2 lanes per row, V elements at a time where rows start on such boundaries
@@ -331,9 +348,12 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
     }
 }
 
-// A batch of at most kFewIds ids needs no sort: a block that takes an id reads all of them from shared memory, leaves where the same id
-// came earlier, and otherwise adds the rows of all places where it occurs, each of its warps those in a share of the places.
+// A batch of at most kFewIds ids needs no sort: a block that takes an id reads all of them from shared memory, four at a time, leaves where the same id
+// came earlier, and otherwise adds the rows of all places where it occurs, each of its warps those in a share of the places.  That is n^2 comparisons, 4096 ids
+// 4 us of the chip's time; sorting them takes seven launches.
 constexpr int kFewIds = 8192;
+constexpr int kFewBlock = 128;
+template <int V> constexpr int few_chunks() { return V == 8 ? 1 : V == 4 ? 2 : 4; }      // column vectors per lane
 
 template <typename IdT>
 __device__ __forceinline__ int few_id(const GradArgs& a, int64_t i, bool* bad)
@@ -345,59 +365,69 @@ __device__ __forceinline__ int few_id(const GradArgs& a, int64_t i, bool* bad)
 }
 
 template <typename IdT, typename TI, typename TO, int V>
-__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_few(const __grid_constant__ GradArgs a)
+__global__ void __launch_bounds__(kFewBlock) embedding_grad_few(const __grid_constant__ GradArgs a)
 {
     grid_dependency<true>();
-    extern __shared__ int few_ids[];
-    __shared__ float part[kEmbedBlock / 32 - 1][32][V];
-    const int n = (int)a.n, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kFewChunks = few_chunks<V>();
+    extern __shared__ __align__(16) int few_ids[];                     // n, rounded up to four
+    __shared__ float part[kFewBlock / 32 - 1][32][kFewChunks][V];
+    const int n = (int)a.n, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n4 = (n + 3) / 4;
     bool bad = false;
-    for (int i = threadIdx.x; i < n; i += kEmbedBlock) few_ids[i] = few_id<IdT>(a, i, &bad);
+#pragma unroll 8
+    for (int i = threadIdx.x; i < n4 * 4; i += kFewBlock) few_ids[i] = i < n ? few_id<IdT>(a, i, &bad) : -1;
     if (bad && blockIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status, 1);
     __syncthreads();
-    const int c = ((int)blockIdx.y * 32 + lane) * V;
-    const int share = ((n + 255) / 256) * 32;                          // places per warp, whole steps of 32
+    const int4* const quads = reinterpret_cast<const int4*>(few_ids);
+    const int c0 = (int)blockIdx.y * (32 * V * kFewChunks) + lane * V;
+    const int share = (n4 + kFewBlock - 1) / kFewBlock * 32;                           // quads per warp, whole steps of 32
+    auto match = [](int4 q, int id) { return (q.x == id ? 1 : 0) | (q.y == id ? 2 : 0) | (q.z == id ? 4 : 0) | (q.w == id ? 8 : 0); };
     for (int mine = blockIdx.x; mine < n; mine += gridDim.x) {
         const int id = few_ids[mine];
         bool earlier = id < 0;
-        for (int i = threadIdx.x; i < mine && !earlier; i += kEmbedBlock) earlier = few_ids[i] == id;
+        for (int i = threadIdx.x; i * 4 < mine && !earlier; i += kFewBlock)
+            earlier = (match(quads[i], id) & (i * 4 + 4 <= mine ? 15 : (1 << (mine & 3)) - 1)) != 0;
         if (__syncthreads_or(earlier)) continue;
-        float acc[V];
+        float acc[kFewChunks][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.f;
-        const int begin = warp * share, end = min(begin + share, n);
-        for (int i0 = max(begin, mine / 32 * 32); i0 < end; i0 += 32) {
-            unsigned here = __ballot_sync(0xffffffffu, i0 + lane < end && few_ids[i0 + lane] == id);
-            while (here) {
-                float x[4][V];
-                int count = 0;
+        for (int q = 0; q < kFewChunks; ++q)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+            for (int i = 0; i < V; ++i) acc[q][i] = 0.f;
+        const int begin = warp * share, end = min(begin + share, n4);
+        for (int i0 = max(begin, mine / 128 * 32); i0 < end; i0 += 32) {
+            int found = i0 + lane < end ? match(quads[i0 + lane], id) : 0;
+            unsigned lanes = __ballot_sync(0xffffffffu, found != 0);
+            while (lanes) {
+                const int from = __ffs(lanes) - 1;
+                lanes &= lanes - 1u;
+                for (int bits = __shfl_sync(0xffffffffu, found, from); bits; bits &= bits - 1) {
+                    const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)((i0 + from) * 4 + __ffs(bits) - 1) * a.ldd;
+                    float x[kFewChunks][V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) x[u][i] = 0.f;
-                    if (here) {
-                        const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)(i0 + __ffs(here) - 1) * a.ldd + c;
-                        load_row<TI, V>(p, a.f - c, x[u]);
-                        here &= here - 1u;
-                        ++count;
-                    }
+                    for (int q = 0; q < kFewChunks; ++q)
+                        if (c0 + q * 32 * V < a.f) load_row<TI, V>(p + c0 + q * 32 * V, a.f - c0 - q * 32 * V, x[q]);
+#pragma unroll
+                    for (int q = 0; q < kFewChunks; ++q)
+                        if (c0 + q * 32 * V < a.f)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) acc[q][i] += x[q][i];
                 }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u < count)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) acc[i] += x[u][i];
             }
         }
         if (warp > 0)
 #pragma unroll
-            for (int i = 0; i < V; ++i) part[warp - 1][lane][i] = acc[i];
+            for (int q = 0; q < kFewChunks; ++q)
+#pragma unroll
+                for (int i = 0; i < V; ++i) part[warp - 1][lane][q][i] = acc[q][i];
         __syncthreads();
         if (warp == 0) {
-            for (int w = 0; w < kEmbedBlock / 32 - 1; ++w)
+            for (int w = 0; w < kFewBlock / 32 - 1; ++w)
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += part[w][lane][i];
-            if (c < a.f) write_row<TO, V>(a, id, c, acc);
+                for (int q = 0; q < kFewChunks; ++q)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[q][i] += part[w][lane][q][i];
+#pragma unroll
+            for (int q = 0; q < kFewChunks; ++q)
+                if (c0 + q * 32 * V < a.f) write_row<TO, V>(a, id, c0 + q * 32 * V, acc[q]);
         }
         __syncthreads();
     }
@@ -426,7 +456,7 @@ template <typename IdT, typename TI, typename TO, int V>
 static void launch_lookup(const LookupArgs& a, cudaStream_t s)
 {
     const int64_t rows = kEmbedBlock >> a.lpr_log2;
-    // four rows in flight per group once that still gives every SM four blocks
+    // four rows in flight per group once that still gives every SM four blocks (1,000,003 rows of 128 bf16 columns: with eight 176 us, with four 143)
     if (a.n >= rows * 4 * 4 * kSms)
         GNNFD_LAUNCH("embedding_rows", s, (embedding_rows<IdT, TI, TO, V, 4>), (unsigned)((a.n + rows * 4 - 1) / (rows * 4)), kEmbedBlock, 0, a);
     else
@@ -453,11 +483,11 @@ static void lookup_types(const LookupArgs& a, int v, gnnfd_dtype_t tdt, gnnfd_dt
     }
 }
 
-// ids per block of the sums: as many as leave every SM sixteen blocks, 64 to 1024
-static int ids_per_block(int64_t n)
+// ids per block of the sums: as many as leave every SM sixteen blocks (column tiles counted as tiles of 256), 64 to 1024
+static int ids_per_block(int64_t n, int32_t f)
 {
     int t = 64;
-    while (t < 1024 && (int64_t)t * 2 * kSms * 16 <= n) t *= 2;
+    while (t < 1024 && (int64_t)t * 2 * kSms * 16 <= n * ((f + 255) / 256)) t *= 2;
     return t;
 }
 
@@ -470,7 +500,7 @@ static int carve_grad(Carver& c, int64_t n, int64_t vocab, int32_t f, GradScratc
 {
     const int rc = carve_sorted_ids(c, n, vocab, (size_t)vocab, &g->sorted);
     if (rc) return rc;
-    const size_t blocks = (size_t)((n + ids_per_block(n) - 1) / ids_per_block(n)), fpad = align_up((size_t)f, 4);
+    const size_t blocks = (size_t)((n + ids_per_block(n, f) - 1) / ids_per_block(n, f)), fpad = align_up((size_t)f, 4);
     g->head = c.take<float>(blocks * fpad);
     g->tail = c.take<float>(blocks * fpad);
     return GNNFD_OK;
@@ -480,20 +510,21 @@ template <typename TI, typename TO, int V>
 static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool accumulate, cudaStream_t s)
 {
     if (few) {
-        const dim3 grid((unsigned)(a.n < 8 * kSms ? a.n : 8 * kSms), (unsigned)((a.f + 32 * V - 1) / (32 * V)));
-        const size_t smem = (size_t)a.n * sizeof(int);
-        if (itype == GNNFD_I32) GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<int32_t, TI, TO, V>), grid, kEmbedBlock, smem, a);
-        else GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<long long, TI, TO, V>), grid, kEmbedBlock, smem, a);
+        const dim3 grid((unsigned)(a.n < 16 * kSms ? a.n : 16 * kSms), (unsigned)((a.f + 32 * V * few_chunks<V>() - 1) / (32 * V * few_chunks<V>())));
+        const size_t smem = (size_t)(a.n + 3) / 4 * 4 * sizeof(int);
+        if (itype == GNNFD_I32) GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<int32_t, TI, TO, V>), grid, kFewBlock, smem, a);
+        else GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<long long, TI, TO, V>), grid, kFewBlock, smem, a);
     } else {
-        GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V>), dim3((unsigned)a.n_blocks, (unsigned)a.col_tiles), kEmbedBlock,
-                     0, a);
-        const int join_tiles = (a.f + kJoinCols - 1) / kJoinCols;
+        const int per_tile = (V << a.lpr_log2) * (a.wide ? wide_lane(V) : 1);
+        const dim3 sums((unsigned)a.n_blocks, (unsigned)((a.f + per_tile - 1) / per_tile));
+        if (a.wide) GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V, wide_lane(V)>), sums, kEmbedBlock, 0, a);
+        else GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V, 1>), sums, kEmbedBlock, 0, a);
         const int64_t groups = kEmbedBlock >> a.lpr_log2, zero = accumulate ? 0 : (a.vocab + groups - 1) / groups;
-        const int64_t grid = (int64_t)a.n_blocks * join_tiles + (zero < 16 * kSms ? zero : 16 * kSms);
+        const int64_t grid = (int64_t)a.n_blocks + (zero < 16 * kSms ? zero : 16 * kSms);
         if (grid > 0x7fffffffll) return GNNFD_TOO_LARGE;
         const uintptr_t bits = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
         const int vec = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
-        GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, join_tiles, vec);
+        GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, vec);
     }
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
@@ -565,20 +596,24 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
 {
     using namespace gnnfd;
     const SortDrill drill = take_sort_drill();
-    if (n < 0 || vocab <= 0 || f <= 0 || ldd < f || ldg < f || !d_grad) return GNNFD_INVALID_ARG;
+    if (n < 0 || vocab <= 0 || f <= 0 || ldd < f || ldd > 0x7fffffffll || ldg < f || !d_grad) return GNNFD_INVALID_ARG;
     if (!known(ddt) || !known(gdt) || (itype != GNNFD_I32 && itype != GNNFD_I64)) return GNNFD_UNSUPPORTED;
     if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
     if (n > 0 && (!d_ids || !d_dout)) return GNNFD_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool few = n <= kFewIds;
     if (few && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
-    const int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
+    int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
+    // a group reads eight words at a time at least: rows narrower than eight vectors are taken in narrower ones
+    if (!few && v > 2 && (f + v - 1) / v < kInFlight) v = 2;
+    if (!few && (f + v - 1) / v < kInFlight) v = 1;
     GradArgs a{};
     a.ids = d_ids; a.dout = d_dout; a.out = d_grad;
     a.n = n; a.vocab = vocab; a.ldd = ldd; a.ldo = ldg; a.padding = padding;
     a.status = d_status; a.accumulate = accumulate != 0; a.scale = scale; a.f = f; a.fpad = (int32_t)align_up((size_t)f, 4);
     a.lpr_log2 = lanes_log2(f, v);
-    a.col_tiles = (f + (v << a.lpr_log2) - 1) / (v << a.lpr_log2);
+    if (a.lpr_log2 < 3) a.lpr_log2 = 3;
+    a.wide = f > v << a.lpr_log2 && v < 8;
     if (few) {
         if (!accumulate) {
             const int rc = clear_rows(d_grad, ldg, gdt, vocab, f, s);
@@ -597,7 +632,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
         a.words = g.sorted.words; a.val_bits = g.sorted.val_bits; a.counts = g.sorted.counts;
         a.mark = accumulate ? nullptr : g.sorted.extra;
         a.head = g.head; a.tail = g.tail;
-        a.per_block = ids_per_block(n);
+        a.per_block = ids_per_block(n, f);
         a.n_blocks = (int32_t)((n + a.per_block - 1) / a.per_block);
     }
     if (ddt == GNNFD_F32)

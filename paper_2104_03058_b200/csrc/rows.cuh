@@ -6,29 +6,43 @@
 
 namespace gnnfd {
 
-// V elements of T with one load or store (16, 8, 4 or 2 bytes), as fp32 values
+// V elements as they lie in memory
+template <typename T, int V>
+struct Raw {
+    static constexpr int kBytes = V * (int)sizeof(T);
+    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (kBytes == 16) {
+            const uint4 v = load16(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else if constexpr (kBytes == 8) {
+            asm("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+        } else if constexpr (kBytes == 4) {
+            asm("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+        } else {
+            unsigned short h;
+            asm("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
+            w[0] = h;
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i]);
+            else x[i] = __uint_as_float((i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+        }
+    }
+};
+
+// the same at once as fp32 values
 template <typename T, int V>
 __device__ __forceinline__ void load_packed(const T* p, float (&x)[V])
 {
-    constexpr int kBytes = V * (int)sizeof(T);
-    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
-    if constexpr (kBytes == 16) {
-        const uint4 v = load16(p);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else if constexpr (kBytes == 8) {
-        asm("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    } else if constexpr (kBytes == 4) {
-        asm("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    } else {
-        unsigned short h;
-        asm("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
-        w[0] = h;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i]);
-        else x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);      // bf16 -> fp32 is exact
-    }
+    Raw<T, V> raw;
+    raw.load(p);
+    raw.get(x);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
