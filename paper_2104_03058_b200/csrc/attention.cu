@@ -14,6 +14,8 @@
 // the output was rounded to.
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "schedule.cuh"
 #include "vec.cuh"
 
@@ -31,7 +33,8 @@ struct AttendArgs {
     const int32_t* seg_slot;
     const void *own0, *own1;          // rows' vectors: q / q and dout / k and v
     const void *far0, *far1;          // gathered: k and v / k and v / q and dout
-    int64_t ld_own0, ld_own1, ld_far0, ld_far1;
+    int64_t ld_own0, ld_own1;
+    uint32_t pitch_far0, pitch_far1;  // bytes
     const int32_t* dist;              // [nnz] bucket of every entry (null: no bias)
     const float* bias;                // [buckets, heads]
     float2* lse;                      // [n, heads] largest score and sum of exp(score - largest): written (may be null) / read
@@ -60,6 +63,24 @@ __device__ __forceinline__ float ex2(float x)
 }
 // e^(s - m); m is -inf only where every score so far is
 __device__ __forceinline__ float weight(float s, float m) { return ex2((s - (m == -CUDART_INF_F ? 0.f : m)) * kLog2e); }
+
+// tanh, within 8 * 2^-24 of its value.  For |x| < 1/2 its series to x^13 (the next term is 9e-8 of the result at 1/2); from there on 1 - 2 / (1 + e^2|x|): the
+// quotient is below 0.54 and off by about 4 * 2^-24 of itself from the exponential, 2 from the reciprocal and the rest from roundings.  Scores that are
+// capped at a few tens lie mostly in the first part, where an absolute error would be as large as the score.  tanhf, which is within 2 ulp, branches, and took a
+// quarter of the forward walk's instructions.
+__device__ __forceinline__ float tanh_of(float x)
+{
+    const float x2 = x * x;
+    float c = fmaf(x2, 21844.f / 6081075.f, -1382.f / 155925.f);
+    c = fmaf(x2, c, 62.f / 2835.f);
+    c = fmaf(x2, c, -17.f / 315.f);
+    c = fmaf(x2, c, 2.f / 15.f);
+    c = fmaf(x2, c, -1.f / 3.f);
+    const float series = fmaf(x * x2, c, x), size = fabsf(x);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(size * (2.f * kLog2e))));
+    return size < 0.5f ? series : copysignf(fmaf(-2.f, inv, 1.f), x);
+}
 
 // (x, y) += (a, b) * (c, d)
 __device__ __forceinline__ void fma_pairs(float& x, float& y, float a, float b, float c, float d)
@@ -115,12 +136,23 @@ struct Piece {
     }
 };
 
-template <typename P, int E>
-__device__ __forceinline__ float dot(const float (&a)[E], const P& b)
+// (x, y) += the products of two words' bf16 values, exact before they are added
+__device__ __forceinline__ void fma_words(float& x, float& y, uint32_t a, uint32_t b)
+{
+    asm("{\n\t.reg .b16 al, ah, bl, bh;\n\tmov.b32 {al, ah}, %2;\n\tmov.b32 {bl, bh}, %3;\n\t"
+        "fma.rn.f32.bf16 %0, al, bl, %0;\n\tfma.rn.f32.bf16 %1, ah, bh, %1;\n\t}" : "+f"(x), "+f"(y) : "r"(a), "r"(b));
+}
+template <typename T, int E, int LOAD>
+__device__ __forceinline__ float dot(const Piece<T, E, LOAD>& a, const Piece<T, E, LOAD>& b)
 {
     float x = 0.f, y = 0.f;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < E; i += 2) fma_pairs(x, y, a[i], a[i + 1], b.get(i), b.get(i + 1));
+        for (int i = 0; i < E / 2; ++i) fma_words(x, y, a.w[i], b.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; i += 2) fma_pairs(x, y, a.get(i), a.get(i + 1), b.get(i), b.get(i + 1));
+    }
     return x + y;
 }
 template <typename P, int E>
@@ -178,7 +210,7 @@ __global__ void __launch_bounds__(kBlock, 2) attend(const __grid_constant__ Atte
         if (i < a.n_ranges && rb >= a.range[i].first_block) r = i;
     const Range rg = a.range[r];
 
-    const int tid = threadIdx.x, lpr = 1 << a.lpr_log2, lph = 1 << a.lph_log2, ep = 1 << rg.ep_log2, S = lpr << rg.ep_log2;
+    const int tid = threadIdx.x, lpr = 1 << a.lpr_log2, lph = 1 << a.lph_log2, S = lpr << rg.ep_log2;
     const int warps_log2 = S == 32 ? rg.warps_log2 : 0, sharer = (tid / S) & ((1 << warps_log2) - 1);
     const int slot = (rb - rg.first_block) * (kBlock / S >> warps_log2) + (tid / S >> warps_log2);
     const int sl = tid & (S - 1), g = sl >> a.lpr_log2, c = sl & (lpr - 1);
@@ -208,19 +240,12 @@ __global__ void __launch_bounds__(kBlock, 2) attend(const __grid_constant__ Atte
         e = min(b + share, e);
     }
 
-    float own0[E], own1[PASS == kForward ? 1 : E];
-    {
-        P p;
-        p.zero();
-        if (active) p.load(static_cast<const T*>(a.own0) + (int64_t)row * a.ld_own0 + j, left);
-#pragma unroll
-        for (int i = 0; i < E; ++i) own0[i] = left > 0 ? p.get(i) : 0.f;
-        if constexpr (PASS != kForward) {
-            p.zero();
-            if (active) p.load(static_cast<const T*>(a.own1) + (int64_t)row * a.ld_own1 + j, left);
-#pragma unroll
-            for (int i = 0; i < E; ++i) own1[i] = left > 0 ? p.get(i) : 0.f;
-        }
+    P own0, own1;                                              // zero past the head's end
+    own0.zero();
+    own1.zero();
+    if (active && left > 0) {
+        own0.load(static_cast<const T*>(a.own0) + (int64_t)row * a.ld_own0 + j, left);
+        if (PASS != kForward) own1.load(static_cast<const T*>(a.own1) + (int64_t)row * a.ld_own1 + j, left);
     }
     float m = -CUDART_INF_F, l = 0.f, inv = 0.f, d_sum = 0.f;
     if (PASS == kRowGrad && active) {
@@ -234,111 +259,121 @@ __global__ void __launch_bounds__(kBlock, 2) attend(const __grid_constant__ Atte
         acc0[i] = 0.f;
         if constexpr (PASS != kForward) acc1[i] = 0.f;
     }
-    const T* const far0 = static_cast<const T*>(a.far0) + j;
-    const T* const far1 = static_cast<const T*>(a.far1) + j;
-    const bool with_bias = a.dist != nullptr;
+    const char* const far0 = reinterpret_cast<const char*>(static_cast<const T*>(a.far0) + j);
+    const char* const far1 = reinterpret_cast<const char*>(static_cast<const T*>(a.far1) + j);
+    const float* const bias_h = a.bias + h;
+    const bool with_bias = a.dist != nullptr, capped = a.softcap > 0.f;
 
     const int step = UB << rg.ep_log2;
     const int n_steps = __reduce_max_sync(kFull, (e - b + step - 1) >> (kUbLog2 + rg.ep_log2));
     int32_t next_u[UB], next_r[UB];
-    auto load_entries = [&](int32_t kb) {
+    auto load_entries = [&](int32_t first) {                   // `first`: the group's first entry of the step
 #pragma unroll
         for (int i = 0; i < UB; ++i) {
-            const int32_t kk = kb + (i << rg.ep_log2) + g;
+            const int32_t kk = first + (i << rg.ep_log2);
             next_u[i] = kk < e ? __ldcs(a.col_idx + kk) : -1;
-            next_r[i] = with_bias && kk < e ? __ldcs(a.dist + kk) : 0;
+            if (with_bias) next_r[i] = kk < e ? __ldcs(a.dist + kk) : 0;
         }
     };
-    load_entries(b);
+    load_entries(b + g);
     for (int is = 0; is < n_steps; ++is) {
-        const int32_t kb = b + is * step;
-        P x[UB], y[UB];
-        float bias[UB];
-        float4 stat[UB];
-        bool valid[UB];
+        const int32_t first = b + is * step + g;
+        // one step; FULL: every group of the warp has all its entries
+        auto walk = [&](auto full_tag) {
+            constexpr bool FULL = decltype(full_tag)::value;
+            P x[UB], y[UB];
+            float bias[UB];
+            float4 stat[UB];
+            bool valid[UB];
 #pragma unroll
-        for (int i = 0; i < UB; ++i) {
-            const int32_t u = next_u[i];
-            valid[i] = u >= 0;
-            bias[i] = 0.f;
-            if (valid[i]) {
-                x[i].load(far0 + (int64_t)u * a.ld_far0, left);
-                y[i].load(far1 + (int64_t)u * a.ld_far1, left);
-                if (with_bias) bias[i] = load4(a.bias + (int64_t)min(max(next_r[i], 0), a.buckets - 1) * a.heads + h);
+            for (int i = 0; i < UB; ++i) {
+                valid[i] = FULL || next_u[i] >= 0;
+                // entries past the row's end read vertex 0 instead: they get no weight, and what has none is not added
+                const uint32_t u = FULL ? (uint32_t)next_u[i] : (uint32_t)max(next_u[i], 0);
+                x[i].load(reinterpret_cast<const T*>(far0 + (uint64_t)u * a.pitch_far0), left);
+                y[i].load(reinterpret_cast<const T*>(far1 + (uint64_t)u * a.pitch_far1), left);
+                bias[i] = with_bias ? load4(bias_h + (uint32_t)min(max(next_r[i], 0), a.buckets - 1) * (uint64_t)(uint32_t)a.heads) : 0.f;
                 if (PASS == kColGrad) {
-                    const uint4 w = load16(a.stat + (int64_t)u * a.heads + h);
+                    const uint4 w = load16(a.stat + (u * (uint64_t)(uint32_t)a.heads + h));
                     stat[i] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), 0.f);
                 }
-            } else {
-                x[i].zero();
-                y[i].zero();
-                stat[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
-        }
-        load_entries(kb + step);
-        float s[UB], dp[UB], slope[UB];
-#pragma unroll
-        for (int i = 0; i < UB; ++i) {
-            s[i] = dot(own0, x[i]);
-            if constexpr (PASS != kForward) dp[i] = dot(own1, y[i]);
-        }
-        for (int o = 1; o < lph; o <<= 1) {
+            load_entries(first + step);
+            float s[UB], slope[UB];
+            [[maybe_unused]] float dp[UB];
 #pragma unroll
             for (int i = 0; i < UB; ++i) {
-                s[i] += __shfl_xor_sync(kFull, s[i], o);
-                if constexpr (PASS != kForward) dp[i] += __shfl_xor_sync(kFull, dp[i], o);
+                s[i] = dot(own0, x[i]);
+                if constexpr (PASS != kForward) dp[i] = dot(own1, y[i]);
             }
-        }
+            for (int o = 1; o < lph; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < UB; ++i) {
-            s[i] *= a.scale;
-            slope[i] = 1.f;
-            if (a.softcap > 0.f) {
-                const float t = tanhf(s[i] * a.inv_softcap);
-                s[i] = a.softcap * t;
-                slope[i] = fmaf(-t, t, 1.f);
-            }
-            s[i] += bias[i];
-            // a bias of -inf takes the entry out, whatever its score is
-            if (!valid[i] || bias[i] == -CUDART_INF_F) s[i] = -CUDART_INF_F;
-        }
-        if constexpr (PASS == kForward) {
-            float mx = m;
-#pragma unroll
-            for (int i = 0; i < UB; ++i) mx = fmaxf(mx, s[i]);
-            const float rescale = weight(m, mx);
-            m = mx;
-            l *= rescale;
-#pragma unroll
-            for (int i = 0; i < E; i += 2) mul_pair(acc0[i], acc0[i + 1], rescale, rescale);
-#pragma unroll
-            for (int i = 0; i < UB; ++i) {
-                const float p = weight(s[i], m);
-                l += p;
-                if (p != 0.f) add_scaled(acc0, p, y[i]);       // what stands in masked places does not count, NaN neither
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < UB; ++i) {
-                const float p = PASS == kRowGrad ? weight(s[i], m) * inv : weight(s[i], stat[i].x) * stat[i].y;
-                if constexpr (PASS == kRowGrad) {
-                    if (p != 0.f) {
-                        const float pd = p * dp[i];
-                        d_sum += pd;
-                        add_scaled(acc0, pd * slope[i], x[i]);
-                        add_scaled(acc1, p * slope[i], x[i]);
-                    }
-                } else {
-                    const float ds = p != 0.f ? p * (dp[i] - stat[i].z) : 0.f;
-                    if (p != 0.f) {
-                        add_scaled(acc0, ds * slope[i], x[i]);
-                        add_scaled(acc1, p, y[i]);
-                    }
-                    const int32_t kk = kb + (i << rg.ep_log2) + g;
-                    if (a.ds && col == 0 && head_ok && kk < e) a.ds[(int64_t)kk * a.heads + h] = ds;
+                for (int i = 0; i < UB; ++i) {
+                    s[i] += __shfl_xor_sync(kFull, s[i], o);
+                    if constexpr (PASS != kForward) dp[i] += __shfl_xor_sync(kFull, dp[i], o);
                 }
             }
-        }
+#pragma unroll
+            for (int i = 0; i < UB; ++i) {
+                s[i] *= a.scale;
+                slope[i] = 1.f;
+            }
+            if (capped) {
+#pragma unroll
+                for (int i = 0; i < UB; ++i) {
+                    const float t = tanh_of(s[i] * a.inv_softcap);
+                    s[i] = a.softcap * t;
+                    slope[i] = fmaf(-t, t, 1.f);
+                }
+            }
+            if (with_bias) {
+#pragma unroll
+                for (int i = 0; i < UB; ++i)                   // a bias of -inf takes the entry out, whatever its score is
+                    s[i] = bias[i] == -CUDART_INF_F ? -CUDART_INF_F : s[i] + bias[i];
+            }
+            if (!FULL) {
+#pragma unroll
+                for (int i = 0; i < UB; ++i) s[i] = valid[i] ? s[i] : -CUDART_INF_F;
+            }
+            if constexpr (PASS == kForward) {
+                float mx = m;
+#pragma unroll
+                for (int i = 0; i < UB; ++i) mx = fmaxf(mx, s[i]);
+                const float rescale = weight(m, mx);
+                m = mx;
+                l *= rescale;
+#pragma unroll
+                for (int i = 0; i < E; i += 2) mul_pair(acc0[i], acc0[i + 1], rescale, rescale);
+#pragma unroll
+                for (int i = 0; i < UB; ++i) {
+                    const float p = weight(s[i], m);
+                    l += p;
+                    if (p != 0.f) add_scaled(acc0, p, y[i]);   // what stands in masked places does not count, NaN neither
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < UB; ++i) {
+                    const float p = PASS == kRowGrad ? weight(s[i], m) * inv : weight(s[i], stat[i].x) * stat[i].y;
+                    if constexpr (PASS == kRowGrad) {
+                        if (p != 0.f) {
+                            const float pd = p * dp[i];
+                            d_sum += pd;
+                            add_scaled(acc0, pd * slope[i], x[i]);
+                            add_scaled(acc1, p * slope[i], x[i]);
+                        }
+                    } else {
+                        const float ds = p != 0.f ? p * (dp[i] - stat[i].z) : 0.f;
+                        if (p != 0.f) {
+                            add_scaled(acc0, ds * slope[i], x[i]);
+                            add_scaled(acc1, p, y[i]);
+                        }
+                        if (a.ds && col == 0 && head_ok && valid[i]) a.ds[(int64_t)(first + (i << rg.ep_log2)) * a.heads + h] = ds;
+                    }
+                }
+            }
+        };
+        if (__all_sync(kFull, first + ((UB - 1) << rg.ep_log2) < e)) walk(std::true_type{});
+        else walk(std::false_type{});
     }
 
     // merge the groups of the row, fixed tree
@@ -583,12 +618,16 @@ static HeadLayout head_layout(int size, int32_t dim, bool narrow, const Operand*
     return L;
 }
 
+// ops: the rows' vectors, then the gathered ones (two of the latter, one or two of the former)
 template <int PASS>
 static int launch_attend(const char* name, const char* reduce_name, const gnnfd_csr_t* csr, AttendArgs& a, gnnfd_dtype_t dt, int32_t chunk_heads,
-                         cudaStream_t s)
+                         const Operand (&ops)[4], cudaStream_t s)
 {
     const int size = dt == GNNFD_F32 ? 4 : 2;
-    const Operand ops[4] = {{a.own0, a.ld_own0}, {a.far0, a.ld_far0}, {a.far1, a.ld_far1}, {PASS == kForward ? a.own0 : a.own1, PASS == kForward ? a.ld_own0 : a.ld_own1}};
+    a.own0 = ops[0].p; a.ld_own0 = ops[0].ld;
+    a.own1 = ops[1].p; a.ld_own1 = ops[1].ld;
+    a.far0 = ops[2].p; a.pitch_far0 = (uint32_t)(ops[2].ld * size);
+    a.far1 = ops[3].p; a.pitch_far1 = (uint32_t)(ops[3].ld * size);
     const HeadLayout L = head_layout(size, a.dim, PASS != kForward, ops, 4);
     a.row_ptr = csr->row_ptr; a.col_idx = csr->col_idx; a.row_order = csr->row_order;
     a.seg_row = csr->seg_row; a.seg_begin = csr->seg_begin; a.seg_end = csr->seg_end; a.seg_slot = csr->seg_slot;
@@ -649,6 +688,8 @@ static void carve_attend(Carver& c, const gnnfd_csr_t* csr, const gnnfd_csr_t* c
     g->bias_part = c.take<float>(csr_t && buckets ? (size_t)bias_blocks(csr_t->nnz) * buckets * heads : 0);
 }
 
+constexpr int64_t kMostPitch = 0x3fffffff;       // elements: bytes fit 32 bits
+
 // what the forward call and the backward call ask alike of their arguments
 static int check_attend(const gnnfd_csr_t* csr, gnnfd_dtype_t dt, gnnfd_dtype_t odt, int32_t heads, int32_t dim, float scale, float softcap,
                         const int32_t* d_dist, const float* d_bias, int32_t buckets, int32_t chunk_width, int32_t* chunk_heads)
@@ -689,6 +730,7 @@ int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t l
     const int rc = check_attend(csr, dt, odt, heads, dim, scale, softcap, d_dist, d_bias, buckets, chunk_width, &chunk_heads);
     if (rc) return rc;
     const int64_t f = (int64_t)heads * dim;
+    if (ldq > kMostPitch || ldk > kMostPitch || ldv > kMostPitch) return GNNFD_TOO_LARGE;
     if (!d_q || !d_k || !d_v || !d_out || ldq < f || ldk < f || ldv < f || ldo < f || ((uintptr_t)d_lse & 7u)) return GNNFD_INVALID_ARG;
     if ((uintptr_t)d_scratch & 255u) return GNNFD_INVALID_ARG;
     Carver c(d_scratch, d_scratch ? scratch_bytes : 0);
@@ -696,16 +738,14 @@ int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t l
     carve_attend(c, csr, nullptr, heads, dim, 0, &g);
     if (!c.ok) return GNNFD_WORKSPACE_TOO_SMALL;
     AttendArgs a{};
-    a.own0 = d_q; a.ld_own0 = ldq;
-    a.far0 = d_k; a.ld_far0 = ldk;
-    a.far1 = d_v; a.ld_far1 = ldv;
     a.dist = d_dist; a.bias = d_bias; a.buckets = buckets;
     a.lse = reinterpret_cast<float2*>(d_lse);
     a.out0 = d_out; a.ld_out0 = ldo; a.out_bf16 = odt == GNNFD_BF16;
     a.part0 = g.part0; a.part_ml = g.part_ml;
     a.scale = scale; a.softcap = softcap; a.inv_softcap = softcap > 0.f ? 1.f / softcap : 0.f;
     a.heads = heads; a.dim = dim; a.f = (int32_t)f; a.fpad = (int32_t)align_up((size_t)f, 4);
-    return launch_attend<kForward>("attend", "attend_hub_reduce", csr, a, dt, chunk_heads, static_cast<cudaStream_t>(stream));
+    const Operand ops[4] = {{d_q, ldq}, {d_q, ldq}, {d_k, ldk}, {d_v, ldv}};
+    return launch_attend<kForward>("attend", "attend_hub_reduce", csr, a, dt, chunk_heads, ops, static_cast<cudaStream_t>(stream));
 }
 
 int gnnfd_attention_backward_workspace_bytes(const gnnfd_csr_t* csr, const gnnfd_csr_t* csr_t, int32_t heads, int32_t dim, int32_t buckets,
@@ -733,6 +773,7 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
     if (!csr_t || csr_t->n != csr->n || csr_t->nnz != csr->nnz) return GNNFD_INVALID_ARG;
     if ((d_bias ? !d_dist_t && csr->nnz > 0 : d_dist_t != nullptr) || (d_dbias && !d_bias)) return GNNFD_INVALID_ARG;
     const int64_t f = (int64_t)heads * dim;
+    if (ldq > kMostPitch || ldk > kMostPitch || ldv > kMostPitch || lddo > kMostPitch) return GNNFD_TOO_LARGE;
     if (!d_q || !d_k || !d_v || !d_dout || !d_lse || !d_dq || !d_dk || !d_dv) return GNNFD_INVALID_ARG;
     if (ldq < f || ldk < f || ldv < f || lddo < f || lddq < f || lddk < f || lddv < f || ((uintptr_t)d_lse & 7u)) return GNNFD_INVALID_ARG;
     if (!d_scratch || ((uintptr_t)d_scratch & 255u)) return GNNFD_INVALID_ARG;
@@ -742,10 +783,6 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
     if (!c.ok) return GNNFD_WORKSPACE_TOO_SMALL;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     AttendArgs a{};
-    a.own0 = d_q; a.ld_own0 = ldq;
-    a.own1 = d_dout; a.ld_own1 = lddo;
-    a.far0 = d_k; a.ld_far0 = ldk;
-    a.far1 = d_v; a.ld_far1 = ldv;
     a.dist = d_dist; a.bias = d_bias; a.buckets = buckets;
     a.lse = reinterpret_cast<float2*>(const_cast<float*>(d_lse));
     a.stat = g.stat;
@@ -753,17 +790,14 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
     a.part0 = g.part0; a.part1 = g.part1; a.part_ml = g.part_ml;
     a.scale = scale; a.softcap = softcap; a.inv_softcap = softcap > 0.f ? 1.f / softcap : 0.f;
     a.heads = heads; a.dim = dim; a.f = (int32_t)f; a.fpad = (int32_t)align_up((size_t)f, 4);
-    rc = launch_attend<kRowGrad>("attend_row_grad", "attend_hub_reduce", csr, a, dt, chunk_heads, s);
+    const Operand rows[4] = {{d_q, ldq}, {d_dout, lddo}, {d_k, ldk}, {d_v, ldv}}, cols[4] = {{d_k, ldk}, {d_v, ldv}, {d_q, ldq}, {d_dout, lddo}};
+    rc = launch_attend<kRowGrad>("attend_row_grad", "attend_hub_reduce", csr, a, dt, chunk_heads, rows, s);
     if (rc) return rc;
-    a.own0 = d_k; a.ld_own0 = ldk;
-    a.own1 = d_v; a.ld_own1 = ldv;
-    a.far0 = d_q; a.ld_far0 = ldq;
-    a.far1 = d_dout; a.ld_far1 = lddo;
     a.dist = d_dist_t;
     a.ds = d_dbias ? g.ds : nullptr;
     a.out0 = d_dk; a.ld_out0 = lddk;
     a.out1 = d_dv; a.ld_out1 = lddv;
-    rc = launch_attend<kColGrad>("attend_col_grad", "attend_hub_reduce", csr_t, a, dt, chunk_heads, s);
+    rc = launch_attend<kColGrad>("attend_col_grad", "attend_hub_reduce", csr_t, a, dt, chunk_heads, cols, s);
     if (rc || !d_dbias) return rc;
     const int blocks = bias_blocks(csr_t->nnz);
     const dim3 grid((unsigned)blocks, (unsigned)((heads + kBlock - 1) / kBlock), (unsigned)((buckets + kBiasBuckets - 1) / kBiasBuckets));

@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kEmbedBlock, V == 8 ? 2 : 3) embedding_grad_su
 }
 
 // The first n_blocks blocks: a run that begins in block b of the sums and goes on is added up over the blocks it
-// reaches, in interleaved walks for as many columns as leave four of them or less.  The others: rows that no id names become zero.
+// reaches, in four interleaved walks.  The others: rows that no id names become zero.
 
 template <typename TO>
 __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __grid_constant__ GradArgs a, int vec)
@@ -292,22 +292,23 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
         if (next >= n_valid) return;
         const int64_t key = key_at(next);
         if (key_at(next - 1) != key || (begin > 0 && key_at(begin - 1) == key)) return;      // nothing goes on, or it was begun earlier
-        const int cols = a.f <= 64 ? 64 : a.f <= 128 ? 128 : 256, ways = kEmbedBlock / cols;
+        constexpr int cols = 64, ways = kEmbedBlock / cols;
         const int at_col = threadIdx.x & (cols - 1), way = threadIdx.x / cols;
         for (int c0 = 0; c0 < a.f; c0 += cols) {
             const int c = c0 + at_col;
             float sum = 0.f;
             if (c < a.f) {
                 if (way == 0) sum = a.tail[b * a.fpad + c];
-                constexpr int kAhead = 4;                // blocks of a walk whose words and sums are read together
+                constexpr int kAhead = 8;                // blocks of a walk whose words and sums are read together
                 for (int64_t at = b + 1 + way; at < a.n_blocks && at * a.per_block < n_valid;) {
                     float part[kAhead];
                     bool same[kAhead];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
                         const int64_t block = at + i * ways;
-                        same[i] = block < a.n_blocks && block * a.per_block < n_valid && key_at(block * a.per_block) == key;
-                        part[i] = same[i] ? a.head[block * a.fpad + c] : 0.f;
+                        const bool there = block < a.n_blocks && block * a.per_block < n_valid;
+                        part[i] = there ? a.head[block * a.fpad + c] : 0.f;      // (of another run it is not used)
+                        same[i] = there && key_at(block * a.per_block) == key;
                     }
                     bool on = true;
 #pragma unroll
