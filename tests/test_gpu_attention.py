@@ -2,7 +2,7 @@
 
 The tolerances are first-order bounds, computed entry by entry beside the reference from what the kernels do in fp32 (u = 2^-24 a rounding): a
 dot product of d terms is off by at most (d + 2) u times the sum of its terms' magnitudes; the scaled score takes one rounding more, the capped one
-tanh's (8 u of its value) and two; the weight e^(s - m) carries the score's error, two roundings of its argument and 2 ulp of the exponential; a sum of k
+tanh's (8 u of its value, for 16-bit features of 1) and two; the weight e^(s - m) carries the score's error, two roundings of its argument and 2 ulp of the exponential; a sum of k
 terms (k + 4) u times the sum of their magnitudes; weights below 2^-126 are 0 (with scores of thousands, weights of e^-89 = 2e-39 times gradients and
 a scale of 300 are results of 1e-36 that the kernels leave out).  These are propagated through the formulas; one rounding to the output type comes
 last.  Factor 1.25 for second-order terms and for the few roundings of merging partial results."""
@@ -51,6 +51,7 @@ def reference(row, col, q, k, v, heads, dim, scale, cap, dist=None, bias=None, d
     keep = torch.ones_like(row, dtype=torch.bool)
     res = {}
     outs = {name: [] for name in ("out", "lse", "dq", "dk", "dv", "dbias")}
+    rough = q.dtype != F32
     q, k, v = (t.double().reshape(n, heads, dim) for t in (q, k, v))
     if dout is not None:
         dout = dout.double().reshape(n, heads, dim)
@@ -70,7 +71,7 @@ def reference(row, col, q, k, v, heads, dim, scale, cap, dist=None, bias=None, d
         if cap:
             t = torch.tanh(raw / cap)
             s, slope = cap * t, 1 - t * t
-            e_t = (e_s / cap + 2 * U * (raw / cap).abs()) * slope + 8 * U * t.abs()
+            e_t = (e_s / cap + 2 * U * (raw / cap).abs()) * slope + 8 * U * (1 if rough else t.abs())
             e_s = cap * e_t + U * s.abs()
             e_slope = 2 * t.abs() * e_t + 2 * U
         if bias is not None:
