@@ -22,6 +22,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
+EMBEDDING_FEW_IDS = 8192
 
 _lib = None
 
@@ -1056,9 +1057,8 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
             raise ValueError("out has %d rows, the table has %d" % (out.shape[0], vocab))
         _no_overlap(dout, out, "dout", "out")
         _no_overlap(ids, out, "ids", "out")
-    if scratch is None:
-        need = embedding_backward_workspace_bytes(n, vocab, f)
-        scratch = _new(dout, need, torch.uint8, stream) if need else None
+    if scratch is None and n > EMBEDDING_FEW_IDS:
+        scratch = _new(dout, embedding_backward_workspace_bytes(n, vocab, f), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, dout.device)
     sp = _status_ptr(status, dout.device)
     padding = -1 if padding_idx is None else padding_idx

@@ -1467,7 +1467,7 @@ static int launch_sweep_shape(const char* name, const SweepArgs& a, cudaStream_t
     const auto kernel = radix_sweep<Shape, SOURCE, HAS_VALS, OUT>;
     const int blocks = SOURCE != kBucketWords && a.n_tiles < Shape::kMinBlocks * kSmCount ? a.n_tiles : Shape::kMinBlocks * kSmCount;
     const int smem = (int)(sizeof(SweepSmem<Shape>) + (SOURCE == kBucketWords ? sizeof(BucketTables) : 0));
-    GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (smem > 48 * 1024) GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     GNNFD_LAUNCH(name, s, kernel, (unsigned)blocks, Shape::kThreads, smem, a);
     return GNNFD_OK;
 }

@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
 // A batch of at most kFewIds ids needs no sort: a block that takes an id reads all of them from shared memory, four at a time, leaves where the same id
 // came earlier, and otherwise adds the rows of all places where it occurs, each of its warps those in a share of the places.  That is n^2 comparisons, 4096 ids
 // 4 us of the chip's time; sorting them takes seven launches.
-constexpr int kFewIds = 8192;
+constexpr int kFewIds = GNNFD_EMBEDDING_FEW_IDS;
 constexpr int kFewBlock = 128;
 template <int V> constexpr int few_chunks() { return V == 8 ? 1 : V == 4 ? 2 : 4; }      // column vectors per lane
 
@@ -374,8 +374,23 @@ __global__ void __launch_bounds__(kFewBlock) embedding_grad_few(const __grid_con
     __shared__ float part[kFewBlock / 32 - 1][32][kFewChunks][V];
     const int n = (int)a.n, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n4 = (n + 3) / 4;
     bool bad = false;
+    int from = 0;
+    if (sizeof(IdT) == 4 && (reinterpret_cast<uintptr_t>(a.ids) & 15u) == 0) {        // four ids a load
+        const int whole = n / 4;
+        auto kept = [&](int id) {
+            const bool inside = (uint32_t)id < (uint32_t)a.vocab;
+            bad = bad || !inside;
+            return inside && id != a.padding ? id : -1;
+        };
+#pragma unroll 4
+        for (int i = threadIdx.x; i < whole; i += kFewBlock) {
+            const uint4 v = load16(static_cast<const char*>(a.ids) + (size_t)i * 16);
+            reinterpret_cast<int4*>(few_ids)[i] = make_int4(kept((int)v.x), kept((int)v.y), kept((int)v.z), kept((int)v.w));
+        }
+        from = whole * 4;
+    }
 #pragma unroll 8
-    for (int i = threadIdx.x; i < n4 * 4; i += kFewBlock) few_ids[i] = i < n ? few_id<IdT>(a, i, &bad) : -1;
+    for (int i = from + threadIdx.x; i < n4 * 4; i += kFewBlock) few_ids[i] = i < n ? few_id<IdT>(a, i, &bad) : -1;
     if (bad && blockIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status, 1);
     __syncthreads();
     const int4* const quads = reinterpret_cast<const int4*>(few_ids);
