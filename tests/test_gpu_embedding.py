@@ -101,7 +101,8 @@ def test_ids_outside_the_table_give_zeros_and_set_the_status():
     (0, 9, 5, 5, 0, "even"), (1, 1, 1, 1, 0, "even"), (2, 3, 602, 608, 0, "one"), (31, 40, 8, 8, 1, "even"), (4096, 19_717, 41, 41, 0, "skew"),
     (8192, 100, 64, 64, 0, "one"), (8193, 100, 64, 64, 0, "one"), (8193, 1, 3, 4, 0, "even"), (9000, 30_000, 130, 136, 0, "even"),
     (20_011, 7, 16, 16, 0, "skew"), (60_000, 250, 602, 608, 0, "skew"), (300_000, 232_965, 32, 32, 0, "skew"), (100_001, 3_000, 200, 200, 2, "ascending"),
-    (250_000, 5_000, 1, 1, 0, "skew"), (400_000, 2_100_000, 8, 8, 0, "skew")])
+    (250_000, 5_000, 1, 1, 0, "skew"), (65_536, 16_384, 24, 24, 0, "skew"), (65_536, 16_383, 24, 24, 0, "skew"),
+    (40_000, 60_000, 41, 41, 0, "even"), (12_000, 3_000, 602, 604, 0, "one"), (50_000, 300_000, 9, 12, 1, "skew"), (400_000, 2_100_000, 8, 8, 0, "skew")])
 def test_gradient(ddt, odt, n, vocab, f, ld, offset, kind):
     ids = draw_ids(n, vocab, kind, torch.int64 if n % 2 else torch.int32)
     dout = rand(n, f, ddt, ld, offset) if n else torch.empty((0, f), dtype=ddt, device="cuda")
@@ -182,7 +183,7 @@ def test_captured_and_replayed_and_on_another_stream(n):
 
 @pytest.mark.parametrize("sweep", [0, 1])
 def test_a_sort_that_gives_up_is_reported(sweep):
-    n, vocab = 30_000, 100_000
+    n, vocab = 70_000, 100_000
     ids, dout = draw_ids(n, vocab, "even", torch.int32), rand(n, 4)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     g.debug_build_fault(256, sweep)
