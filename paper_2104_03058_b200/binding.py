@@ -22,7 +22,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
-EMBEDDING_FEW_IDS = 4096
+EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056
 
 _lib = None
 
@@ -1057,7 +1057,7 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
             raise ValueError("out has %d rows, the table has %d" % (out.shape[0], vocab))
         _no_overlap(dout, out, "dout", "out")
         _no_overlap(ids, out, "ids", "out")
-    if scratch is None and n > EMBEDDING_FEW_IDS:
+    if scratch is None and (n > EMBEDDING_FEW_IDS or vocab > EMBEDDING_FEW_ROWS):
         scratch = _new(dout, embedding_backward_workspace_bytes(n, vocab, f), torch.uint8, stream)
     scr, scr_n = _scratch_args(scratch, dout.device)
     sp = _status_ptr(status, dout.device)

@@ -5,6 +5,8 @@
 //
 // Neither does arithmetic worth counting: both are bound by HBM (the lookup reads n rows and writes n rows, the gradient
 // reads n rows and writes `vocab` rows), or by latency on small batches.
+#include <type_traits>
+
 #include "schedule.cuh"
 #include "rows.cuh"
 
@@ -349,132 +351,172 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
     }
 }
 
-// A batch of at most kFewIds ids needs no sort: a block that takes an id reads all of them from shared memory, four at a time, leaves where the same id
-// came earlier, and otherwise adds the rows of all places where it occurs, each of its warps those in a share of the places.  That is n^2 comparisons, 4096 ids
-// 4 us of the chip's time; sorting them takes seven launches.
+// ------------------------------------------------------------------ gradient of few ids
+//
+// One launch in place of the sort's seven (64 columns: 4096 ids 12 to 15 us, 8192 17 to 19, by sorting 27).  Block b has the rows r with r % kClasses == b (a prime number of classes, so that regular ids spread).  It looks through
+// all ids, each warp through a share of their places, and lists its own in order; counts them by row; one warp puts the list in the order of the rows, equal
+// rows in the order of their places; then a warp takes a row, adds up its places or writes zeros.  Rows of more than kCrowd places
+// are added up by the whole block.
 constexpr int kFewIds = GNNFD_EMBEDDING_FEW_IDS;
-constexpr int kFewBlock = 128;
-template <int V> constexpr int few_chunks() { return V == 8 ? 1 : V == 4 ? 2 : 4; }      // column vectors per lane
+constexpr int kClasses = 443;                                          // three blocks on each of 148 SMs
+constexpr int kFewBlock = 512, kFewWarps = kFewBlock / 32;
+constexpr int kClassRows = GNNFD_EMBEDDING_FEW_ROWS / kClasses;        // of one class, at most
+constexpr int kCrowd = 64;
+static_assert(kFewIds <= kFewWarps * 32 * 32, "a lane keeps one vote per step of its warp's share");
+static_assert(kFewIds <= 1 << 16 && kClassRows <= 1 << 16 && GNNFD_EMBEDDING_FEW_ROWS % kClasses == 0, "place and row in one word");
 
-template <typename IdT>
-__device__ __forceinline__ int few_id(const GradArgs& a, int64_t i, bool* bad)
-{
-    const int64_t id = (int64_t) static_cast<const IdT*>(a.ids)[i];
-    const bool inside = (uint64_t)id < (uint64_t)a.vocab;
-    *bad = *bad || !inside;
-    return inside && id != a.padding ? (int)id : -1;
-}
-
-template <typename IdT, typename TI, typename TO, int V>
-__global__ void __launch_bounds__(kFewBlock) embedding_grad_few(const __grid_constant__ GradArgs a)
+template <typename IdT, typename TI, typename TO, int V, int Q>
+__global__ void __launch_bounds__(kFewBlock, 2) embedding_grad_few(const __grid_constant__ GradArgs a, int vec)
 {
     grid_dependency<true>();
-    constexpr int kFewChunks = few_chunks<V>();
-    extern __shared__ __align__(16) int few_ids[];                     // n, rounded up to four
-    __shared__ float part[kFewBlock / 32 - 1][32][kFewChunks][V];
-    const int n = (int)a.n, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n4 = (n + 3) / 4;
+    extern __shared__ uint32_t few_smem[];
+    constexpr unsigned kFull = 0xffffffffu;
+    constexpr int U = V * Q >= 8 ? 4 : 8;
+    const int n = (int)a.n, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, mine = blockIdx.x;
+    const int rows = (int)((a.vocab - mine + kClasses - 1) / kClasses);            // (blocks beyond the last row have none)
+    uint32_t* const listed = few_smem;                                 // [n] row << 16 | place, in the order of the places
+    int* const first = reinterpret_cast<int*>(listed + n);             // [rows + 1] where each row's places start in `order`
+    uint16_t* const order = reinterpret_cast<uint16_t*>(first + rows + 1);         // [n]
+    __shared__ int per_warp[kFewWarps], crowded[kFewIds / kCrowd], n_crowded;
+    __shared__ float part[kFewWarps][32][V * Q];
+    const IdT* const ids = static_cast<const IdT*>(a.ids);
+
+    // the votes of the warp's steps: bit l of step k's vote, which lane k keeps, says that place begin + 32 k + l is this block's
+    const int share = (n + kFewBlock - 1) / kFewBlock * 32, begin = warp * share, steps = share / 32;
+    unsigned votes = 0u;
+    int count = 0;
     bool bad = false;
-    int from = 0;
-    if (sizeof(IdT) == 4 && (reinterpret_cast<uintptr_t>(a.ids) & 15u) == 0) {        // four ids a load
-        const int whole = n / 4;
-        auto kept = [&](int id) {
-            const bool inside = (uint32_t)id < (uint32_t)a.vocab;
-            bad = bad || !inside;
-            return inside && id != a.padding ? id : -1;
-        };
-#pragma unroll 4
-        for (int i = threadIdx.x; i < whole; i += kFewBlock) {
-            const uint4 v = load16(static_cast<const char*>(a.ids) + (size_t)i * 16);
-            reinterpret_cast<int4*>(few_ids)[i] = make_int4(kept((int)v.x), kept((int)v.y), kept((int)v.z), kept((int)v.w));
-        }
-        from = whole * 4;
-    }
-#pragma unroll 8
-    for (int i = from + threadIdx.x; i < n4 * 4; i += kFewBlock) few_ids[i] = i < n ? few_id<IdT>(a, i, &bad) : -1;
-    if (bad && blockIdx.x == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status, 1);
-    __syncthreads();
-    const int4* const quads = reinterpret_cast<const int4*>(few_ids);
-    const int c0 = (int)blockIdx.y * (32 * V * kFewChunks) + lane * V;
-    const int share = (n4 + kFewBlock - 1) / kFewBlock * 32;                           // quads per warp, whole steps of 32
-    auto match = [](int4 q, int id) { return (q.x == id ? 1 : 0) | (q.y == id ? 2 : 0) | (q.z == id ? 4 : 0) | (q.w == id ? 8 : 0); };
-    for (int mine = blockIdx.x; mine < n; mine += gridDim.x) {
-        const int id = few_ids[mine];
-        bool earlier = id < 0;
-        for (int i = threadIdx.x; i * 4 < mine && !earlier; i += kFewBlock)
-            earlier = (match(quads[i], id) & (i * 4 + 4 <= mine ? 15 : (1 << (mine & 3)) - 1)) != 0;
-        if (__syncthreads_or(earlier)) continue;
-        float acc[kFewChunks][V];
+    constexpr int kLook = 8;
+    for (int k0 = 0; k0 < steps; k0 += kLook) {
+        int64_t id[kLook];
 #pragma unroll
-        for (int q = 0; q < kFewChunks; ++q)
+        for (int u = 0; u < kLook; ++u) {
+            const int i = begin + (k0 + u) * 32 + lane;
+            id[u] = k0 + u < steps && i < n ? (int64_t)ids[i] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kLook; ++u) {
+            const int i = begin + (k0 + u) * 32 + lane;
+            const bool there = k0 + u < steps && i < n, inside = (uint64_t)id[u] < (uint64_t)a.vocab;
+            bad = bad || (there && !inside);
+            const unsigned vote = __ballot_sync(kFull, there && inside && id[u] != a.padding && (uint32_t)id[u] % kClasses == (uint32_t)mine);
+            if (lane == k0 + u) votes = vote;
+            count += __popc(vote);
+        }
+    }
+    if (bad && mine == 0 && blockIdx.y == 0 && a.status) atomicOr(a.status, 1);
+    if (lane == 0) per_warp[warp] = count;
+    for (int r = tid; r <= rows; r += kFewBlock) first[r] = 0;
+    if (tid == 0) n_crowded = 0;
+    __syncthreads();
+    int at = 0, total = 0;
+    for (int w = 0; w < kFewWarps; ++w) {
+        at += w < warp ? per_warp[w] : 0;
+        total += per_warp[w];
+    }
+    if (count > 0)
+        for (int k = 0; k < steps; ++k) {
+            const unsigned vote = __shfl_sync(kFull, votes, k);
+            if (vote >> lane & 1u) {
+                const int place = begin + k * 32 + lane;
+                const uint32_t row = (uint32_t)ids[place] / kClasses;
+                listed[at + __popc(vote & ((1u << lane) - 1u))] = row << 16 | (uint32_t)place;
+                atomicAdd(&first[row + 1], 1);
+            }
+            at += __popc(vote);
+        }
+    __syncthreads();
+    // counts to starts, then the list in the order of the rows; both by one warp
+    if (warp == 0) {
+        int sum = 0;
+        for (int r0 = 0; r0 < rows; r0 += 32) {
+            int v = r0 + lane < rows ? first[r0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int t = __shfl_up_sync(kFull, v, o);
+                if (lane >= o) v += t;
+            }
+            if (r0 + lane < rows) first[r0 + lane + 1] = sum + v;
+            sum += __shfl_sync(kFull, v, 31);
+        }
+        __syncwarp();
+        for (int j0 = 0; j0 < total; j0 += 32) {                       // first[row] moves on to the row's end
+            const uint32_t e = j0 + lane < total ? listed[j0 + lane] : 0xffffffffu;
+            const unsigned same = __match_any_sync(kFull, e >> 16 | (j0 + lane < total ? 0u : 0x10000u));
+            int to = 0;
+            if (j0 + lane < total) to = first[e >> 16] + __popc(same & ((1u << lane) - 1u));
+            __syncwarp();
+            if (j0 + lane < total) {
+                order[to] = (uint16_t)(e & 0xffffu);
+                if (lane == __ffs(same) - 1) first[e >> 16] += __popc(same);
+            }
+            __syncwarp();
+        }
+    }
+    __syncthreads();
+
+    const int c = (int)blockIdx.y * (32 * V * Q) + lane * V;
+    float acc[Q][V];
+    auto add_places = [&](int from, int to) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[q][i] = 0.f;
-        const int begin = warp * share, end = min(begin + share, n4);
-        for (int i0 = max(begin, mine / 128 * 32); i0 < end; i0 += 32) {
-            int found = i0 + lane < end ? match(quads[i0 + lane], id) : 0;
-            unsigned lanes = __ballot_sync(0xffffffffu, found != 0);
-            for (int from = 0, bits = 0; lanes | (unsigned)bits;) {    // four places at a time, in order (one at a time, 300 equal ids among 4096 took 35 us)
-                float x[4][kFewChunks][V];
-                int count = 0;
+        for (int j = from; j < to; j += U) {
+            float x[U][Q][V];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    if (!bits && lanes) {
-                        from = __ffs(lanes) - 1;
-                        lanes &= lanes - 1u;
-                        bits = __shfl_sync(0xffffffffu, found, from);
-                    }
-                    if (bits) {
-                        const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)((i0 + from) * 4 + __ffs(bits) - 1) * a.ldd;
-                        bits &= bits - 1;
-                        ++count;
+            for (int u = 0; u < U; ++u)
+                if (j + u < to) {
+                    const TI* const p = static_cast<const TI*>(a.dout) + (int64_t)order[j + u] * a.ldd;
 #pragma unroll
-                        for (int q = 0; q < kFewChunks; ++q)
-                            if (c0 + q * 32 * V < a.f) load_row<TI, V>(p + c0 + q * 32 * V, a.f - c0 - q * 32 * V, x[u][q]);
-                    }
+                    for (int q = 0; q < Q; ++q) load_row<TI, V>(p + c + q * 32 * V, a.f - c - q * 32 * V, x[u][q]);
                 }
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u < count)
+            for (int u = 0; u < U; ++u)
+                if (j + u < to)
 #pragma unroll
-                        for (int q = 0; q < kFewChunks; ++q)
-                            if (c0 + q * 32 * V < a.f)
+                    for (int q = 0; q < Q; ++q)
 #pragma unroll
-                                for (int i = 0; i < V; ++i) acc[q][i] += x[u][q][i];
+                        for (int i = 0; i < V; ++i) acc[q][i] += x[u][q][i];
+        }
+    };
+    auto write = [&](int r) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (c + q * 32 * V < a.f) write_row<TO, V>(a, mine + (int64_t)r * kClasses, c + q * 32 * V, acc[q]);
+    };
+    for (int r = warp; r < rows; r += kFewWarps) {
+        const int from = r > 0 ? first[r - 1] : 0, to = first[r];      // (row r's start is where row r - 1 ended)
+        if (to - from > kCrowd) {
+            if (lane == 0) crowded[atomicAdd(&n_crowded, 1)] = r;
+        } else if (to > from) {
+            add_places(from, to);
+            write(r);
+        } else if (!a.accumulate) {
+            char* const p = reinterpret_cast<char*>(static_cast<TO*>(a.out) + (mine + (int64_t)r * kClasses) * a.ldo);
+            const int begin_byte = (int)blockIdx.y * (32 * V * Q) * (int)sizeof(TO), end_byte = min(begin_byte + 32 * V * Q * (int)sizeof(TO), a.f * (int)sizeof(TO));
+            for (int k = begin_byte + lane * vec; k < end_byte; k += 32 * vec) {
+                if (vec == 16 && k + 16 <= end_byte) __stcs(reinterpret_cast<uint4*>(p + k), make_uint4(0u, 0u, 0u, 0u));
+                else if (vec == 4 && k + 4 <= end_byte) __stcs(reinterpret_cast<unsigned int*>(p + k), 0u);
+                else
+                    for (int m = k; m < k + vec && m < end_byte; m += 2) *reinterpret_cast<unsigned short*>(p + m) = 0;
             }
         }
-        if (warp > 0)
+    }
+    __syncthreads();
+    for (int k = 0; k < n_crowded; ++k) {                              // (in whatever order: each row's sum is its own)
+        const int r = crowded[k], from = r > 0 ? first[r - 1] : 0, length = first[r] - from;
+        add_places(from + (int)((int64_t)length * warp / kFewWarps), from + (int)((int64_t)length * (warp + 1) / kFewWarps));
 #pragma unroll
-            for (int q = 0; q < kFewChunks; ++q)
-#pragma unroll
-                for (int i = 0; i < V; ++i) part[warp - 1][lane][q][i] = acc[q][i];
+        for (int i = 0; i < V * Q; ++i) part[warp][lane][i] = acc[i / V][i % V];
         __syncthreads();
         if (warp == 0) {
-            for (int w = 0; w < kFewBlock / 32 - 1; ++w)
+            for (int w = 1; w < kFewWarps; ++w)
 #pragma unroll
-                for (int q = 0; q < kFewChunks; ++q)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) acc[q][i] += part[w][lane][q][i];
-#pragma unroll
-            for (int q = 0; q < kFewChunks; ++q)
-                if (c0 + q * 32 * V < a.f) write_row<TO, V>(a, id, c0 + q * 32 * V, acc[q]);
+                for (int i = 0; i < V * Q; ++i) acc[i / V][i % V] += part[w][lane][i];
+            write(r);
         }
         __syncthreads();
-    }
-}
-
-// all rows of a gradient that is not added to; four bytes at a time where rows allow it
-template <typename Word>
-__global__ void __launch_bounds__(kEmbedBlock) embedding_grad_clear(void* out, int64_t pitch_words, int64_t rows, int32_t words)
-{
-    grid_dependency<true>();
-    const int64_t total = rows * words, step = (int64_t)gridDim.x * kEmbedBlock;
-    int64_t i = (int64_t)blockIdx.x * kEmbedBlock + threadIdx.x;
-    if (pitch_words == words) {                           // no padding columns
-        for (; i < total; i += step) static_cast<Word*>(out)[i] = Word();
-        return;
-    }
-    for (; i < total; i += step) {
-        const int64_t row = total <= 0x7fffffffll ? (int64_t)((uint32_t)i / (uint32_t)words) : i / words;
-        static_cast<Word*>(out)[row * pitch_words + (i - row * words)] = Word();
     }
 }
 
@@ -537,11 +579,26 @@ static int carve_grad(Carver& c, int64_t n, int64_t vocab, int32_t f, GradScratc
 template <typename TI, typename TO, int V>
 static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool accumulate, cudaStream_t s)
 {
+    const uintptr_t bits = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
+    const int vec = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
     if (few) {
-        const dim3 grid((unsigned)(a.n < 16 * kSms ? a.n : 16 * kSms), (unsigned)((a.f + 32 * V * few_chunks<V>() - 1) / (32 * V * few_chunks<V>())));
-        const size_t smem = (size_t)(a.n + 3) / 4 * 4 * sizeof(int);
-        if (itype == GNNFD_I32) GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<int32_t, TI, TO, V>), grid, kFewBlock, smem, a);
-        else GNNFD_LAUNCH("embedding_grad_few", s, (embedding_grad_few<long long, TI, TO, V>), grid, kFewBlock, smem, a);
+        const int rows = (int)((a.vocab + kClasses - 1) / kClasses);
+        const size_t smem = (size_t)a.n * sizeof(uint32_t) + (size_t)(rows + 1) * sizeof(int) + (size_t)a.n * sizeof(uint16_t);
+        auto launch = [&](auto wide, auto id) -> int {
+            constexpr int Q = decltype(wide)::value;
+            const auto kernel = embedding_grad_few<decltype(id), TI, TO, V, Q>;
+            const dim3 grid((unsigned)(a.vocab < kClasses ? a.vocab : kClasses), (unsigned)((a.f + 32 * V * Q - 1) / (32 * V * Q)));
+            // (static shared memory counts too: beyond 16 KB the limit is raised)
+            if (smem > 16 * 1024) GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            GNNFD_LAUNCH("embedding_grad_few", s, kernel, grid, kFewBlock, smem, a, vec);
+            return GNNFD_OK;
+        };
+        using One = std::integral_constant<int, 1>;
+        using Wide = std::integral_constant<int, wide_lane(V)>;
+        const bool wide = a.f > 32 * V;
+        const int rc = itype == GNNFD_I32 ? (wide ? launch(Wide(), int32_t()) : launch(One(), int32_t()))
+                                          : (wide ? launch(Wide(), (long long)0) : launch(One(), (long long)0));
+        if (rc) return rc;
     } else {
         const int per_tile = (V << a.lpr_log2) * (a.wide ? wide_lane(V) : 1);
         const dim3 sums((unsigned)a.n_blocks, (unsigned)((a.f + per_tile - 1) / per_tile));
@@ -550,8 +607,6 @@ static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool ac
         const int64_t groups = kEmbedBlock >> a.lpr_log2, zero = accumulate ? 0 : (a.vocab + groups - 1) / groups;
         const int64_t grid = (int64_t)a.n_blocks + (zero < 16 * kSms ? zero : 16 * kSms);
         if (grid > 0x7fffffffll) return GNNFD_TOO_LARGE;
-        const uintptr_t bits = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
-        const int vec = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
         GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, vec);
     }
     GNNFD_CUDA_CHECK(cudaGetLastError());
@@ -566,19 +621,7 @@ static int grad_vector(const GradArgs& a, int v, gnnfd_itype_t itype, bool few, 
     return launch_grad<TI, TO, 1>(a, itype, few, accumulate, s);
 }
 
-static int clear_rows(void* out, int64_t ldo, gnnfd_dtype_t odt, int64_t rows, int32_t f, cudaStream_t s)
-{
-    const int64_t size = odt == GNNFD_F32 ? 4 : 2, pitch = ldo * size, bytes = f * size;
-    const uintptr_t bits = (uintptr_t)out | (uintptr_t)pitch | (uintptr_t)bytes;
-    const int64_t word = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2, total = rows * (bytes / word);
-    const int64_t blocks = (total + kEmbedBlock * 4 - 1) / (kEmbedBlock * 4);
-    const unsigned grid = (unsigned)(blocks < 16 * kSms ? blocks : 16 * kSms);
-    if (word == 16) GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint4>, grid, kEmbedBlock, 0, out, pitch / 16, rows, (int32_t)(bytes / 16));
-    else if (word == 4) GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint32_t>, grid, kEmbedBlock, 0, out, pitch / 4, rows, (int32_t)(bytes / 4));
-    else GNNFD_LAUNCH("embedding_grad_clear", s, embedding_grad_clear<uint16_t>, grid, kEmbedBlock, 0, out, pitch / 2, rows, (int32_t)(bytes / 2));
-    GNNFD_CUDA_CHECK(cudaGetLastError());
-    return GNNFD_OK;
-}
+static bool few_ids(int64_t n, int64_t vocab) { return n <= kFewIds && vocab <= GNNFD_EMBEDDING_FEW_ROWS; }
 
 static bool known(gnnfd_dtype_t t) { return t == GNNFD_F32 || t == GNNFD_BF16; }
 
@@ -610,7 +653,7 @@ int gnnfd_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int32_t f
     if (n < 0 || vocab <= 0 || f <= 0 || !scratch_bytes) return GNNFD_INVALID_ARG;
     if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
     *scratch_bytes = 0;
-    if (n <= kFewIds) return GNNFD_OK;
+    if (few_ids(n, vocab)) return GNNFD_OK;
     Carver c(nullptr, ~size_t(0));
     GradScratch g;
     const int rc = carve_grad(c, n, vocab, f, &g);
@@ -629,7 +672,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
     if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
     if (n > 0 && (!d_ids || !d_dout)) return GNNFD_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool few = n <= kFewIds;
+    const bool few = few_ids(n, vocab);
     if (few && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
     int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
     // a group reads eight words at a time at least: rows narrower than eight vectors are taken in narrower ones
@@ -642,13 +685,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
     a.lpr_log2 = lanes_log2(f, v);
     if (a.lpr_log2 < 3) a.lpr_log2 = 3;
     a.wide = f > v << a.lpr_log2 && v < 8;
-    if (few) {
-        if (!accumulate) {
-            const int rc = clear_rows(d_grad, ldg, gdt, vocab, f, s);
-            if (rc) return rc;
-        }
-        if (n == 0) return GNNFD_OK;
-    } else {
+    if (!few) {
         if (!d_scratch || ((uintptr_t)d_scratch & 255u)) return GNNFD_INVALID_ARG;
         Carver c(d_scratch, scratch_bytes);
         GradScratch g;

@@ -68,8 +68,7 @@ __device__ __forceinline__ float reciprocal_fast(float x)             // 1 ulp; 
 }
 constexpr float kL2e = 1.4426950408889634f;
 
-// Two neighbouring elements in one instruction each (the same roundings as one by one): x + c, and x * m + c.
-__device__ __forceinline__ void shift_pair(float& x, float& y, float c, float d) { add_pair(x, y, c, d); }
+// Two neighbouring elements in one instruction (the same roundings as one by one): x * m + c.
 __device__ __forceinline__ void scale_shift_pair(float& x, float& y, float m, float n, float c, float d)
 {
     asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%0, %1};\n\t"
@@ -88,7 +87,7 @@ __device__ __forceinline__ void add_minus(float (&x)[V], const float (&c)[CS])
     if constexpr (V == 1) x[0] -= c[0];
     else
 #pragma unroll
-        for (int i = 0; i < V; i += 2) shift_pair(x[i], x[i + 1], -c[CS == 1 ? 0 : i], -c[CS == 1 ? 0 : i + 1]);
+        for (int i = 0; i < V; i += 2) add_pair(x[i], x[i + 1], -c[CS == 1 ? 0 : i], -c[CS == 1 ? 0 : i + 1]);
 }
 template <int V>
 __device__ __forceinline__ void add_all(float (&s)[V], const float (&x)[V])
@@ -302,7 +301,11 @@ __device__ __forceinline__ void each_piece(const NormArgs& a, int64_t s, F work)
     int64_t r = begin;
     for (int64_t b = a.first_long ? a.first_long[s] : graph_of(a, r); b < a.graphs && r < end; ++b) {
         const int64_t g0 = offset_at(a, b), g1 = offset_at(a, b + 1), first = max(g0, r), last = min(g1, end);
-        if (first >= last) continue;         // an empty graph, or one whose offsets go back
+        if (first >= last) {                 // an empty graph, or one whose offsets go back: on to the one that has row r, over all empty ones
+            const int64_t next = graph_of(a, r);
+            if (next > b + 1) b = next - 1;
+            continue;
+        }
         if (!is_small(a, g1 - g0)) work(b, first, last);
         r = last;
     }
@@ -1177,7 +1180,7 @@ static int check_norm(int64_t n, int32_t f, int32_t groups, int64_t graphs, cons
     if ((xdt != GNNFD_F32 && xdt != GNNFD_BF16) || (odt != GNNFD_F32 && odt != GNNFD_BF16)) return GNNFD_UNSUPPORTED;
     if (d_ptr && itype != GNNFD_I32 && itype != GNNFD_I64) return GNNFD_UNSUPPORTED;
     if (act < kNone || act > kGelu || f > kMaxColumns) return GNNFD_UNSUPPORTED;
-    if (n > 0x7fffffffll || graphs > 0x7fffffffll) return GNNFD_TOO_LARGE;
+    if (n > 0x7fffffffll || graphs > 0x7f000000ll) return GNNFD_TOO_LARGE;
     return GNNFD_OK;
 }
 

@@ -216,6 +216,6 @@ def test_refusals():
     with pytest.raises(ValueError, match="rows"):
         g.embedding_backward(ids, rand(3, 8), 10)
     with pytest.raises(g.GnnfdError) as err:
-        many = torch.zeros(9000, dtype=torch.int32, device="cuda")
-        g.embedding_backward(many, rand(9000, 8), 10, scratch=torch.empty(256, dtype=torch.uint8, device="cuda"))
+        many = torch.zeros(17_000, dtype=torch.int32, device="cuda")
+        g.embedding_backward(many, rand(17_000, 8), 10, scratch=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert err.value.status == g.WORKSPACE_TOO_SMALL

@@ -168,6 +168,14 @@ def test_batches_of_graphs(itype, n, graphs, f, groups, last):
     both_ways(x.bfloat16(), groups, rand(1, f, seed=2)[0].contiguous(), None, ptr, "none", dout.bfloat16(), out_dtype=BF16, rms=False)
 
 
+@pytest.mark.parametrize("n,empties", [(900, 40), (900, 5000), (70_000, 3000), (400_000, 5000)])
+def test_long_graphs_between_many_empty_ones(n, empties):
+    third = n // 3
+    ptr = torch.cat([torch.full((empties,), at, device="cuda") for at in (0, third, third + 1, 2 * third)] + [torch.full((3,), n, device="cuda")]).int()
+    x, dout = rand(n, 12, scale=2.0), rand(n, 12, seed=1)
+    both_ways(x, 3, None, None, ptr, "elu", dout, rms=False)
+
+
 def test_values_far_from_zero_and_an_outlier_in_the_first_row():
     x = rand(3000, 32, scale=1.0, mean=1000.0)
     both_ways(x, 4, None, None, offsets(3000, 3), "none", rand(3000, 32, seed=1), rms=False)

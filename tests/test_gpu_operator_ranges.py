@@ -29,8 +29,8 @@ def test_rows_more_than_four_gigabytes_apart():
     picked = torch.arange(1099, -1, -1, device="cuda", dtype=torch.int32)
     emb.check_grad(g.embedding_backward(picked % 7, x, 7), picked % 7, x, 7, 1.0)                      # few ids
     out = far_rows(1100, 24, pitch, F32, 1)
-    many = emb.draw_ids(5000, 1100, "even", torch.int32)
-    dout = emb.rand(5000, 24)
+    many = emb.draw_ids(20_000, 1100, "even", torch.int32)
+    dout = emb.rand(20_000, 24)
     emb.check_grad(g.embedding_backward(many, dout, 1100, out=out), many, dout, 1100, 1.0)             # sorted, into rows far apart
     y = g.group_norm(x, 4, activation="silu", out=out)
     norm.check(y, norm.reference(x, 4, None, None, None, "silu", norm.EPS)["out"], "out")

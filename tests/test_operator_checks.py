@@ -56,7 +56,7 @@ def test_the_c_calls_refuse_bad_arguments_without_a_device():
     assert emb(n=-1) == emb(vocab=0) == emb(f=0) == emb(ldt=7) == emb(ldo=7) == emb(ids=None) == emb(table=None) == emb(out=None) == g.INVALID_ARG
     assert emb(itype=2) == emb(tdt=2) == emb(odt=5) == g.UNSUPPORTED
     assert emb(n=1 << 31) == emb(vocab=1 << 31) == g.TOO_LARGE
-    grad = lambda n=9000, itype=0, vocab=5, ldd=8, ddt=0, f=8, ldg=8, gdt=0, ids=p, dout=p, out=p, scr=p, size=1 << 40: (      # noqa: E731
+    grad = lambda n=19_000, itype=0, vocab=5, ldd=8, ddt=0, f=8, ldg=8, gdt=0, ids=p, dout=p, out=p, scr=p, size=1 << 40: (      # noqa: E731
         L.gnnfd_embedding_backward(n, ids, itype, dout, ldd, ddt, vocab, f, 1.0, -1, 0, out, ldg, gdt, scr, size, None, None))
     assert grad(n=-1) == grad(vocab=0) == grad(f=0) == grad(ldd=7) == grad(ldg=7) == grad(ids=None) == grad(dout=None) == grad(out=None) == g.INVALID_ARG
     assert grad(ldd=1 << 31) == grad(scr=None) == grad(scr=p + 8) == g.INVALID_ARG
@@ -80,9 +80,9 @@ def test_the_c_calls_refuse_bad_arguments_without_a_device():
 
 
 def test_workspaces_grow_with_what_they_are_for():
-    sizes = [g.embedding_backward_workspace_bytes(n, 1000, 64) for n in (0, 4096, 4097, 10_000, 100_000, 1_000_000, 30_000_000)]
+    sizes = [g.embedding_backward_workspace_bytes(n, 1000, 64) for n in (0, 16_384, 16_385, 20_000, 100_000, 1_000_000, 30_000_000)]
     assert sizes[:2] == [0, 0] and sizes == sorted(sizes)
-    assert g.embedding_backward_workspace_bytes(10_000, 1000, 64) <= g.embedding_backward_workspace_bytes(10_000, 1_000_000, 64)
+    assert g.embedding_backward_workspace_bytes(10_000, 3_629_056, 64) == 0 < g.embedding_backward_workspace_bytes(10_000, 3_629_057, 64)
     assert g.group_norm_workspace_bytes(0, 8, 2) > 0
     for backward in (False, True):
         sizes = [g.group_norm_workspace_bytes(n, 64, 8, 1, backward) for n in (1, 100, 10_000, 1_000_000)]
@@ -97,5 +97,6 @@ def test_workspaces_grow_with_what_they_are_for():
 def test_constants_of_the_header():
     text = open(os.path.join(ROOT, "include", "gnnfd.h")).read()
     assert int(re.search(r"#define GNNFD_EMBEDDING_FEW_IDS (\d+)", text).group(1)) == g.EMBEDDING_FEW_IDS
+    assert int(re.search(r"#define GNNFD_EMBEDDING_FEW_ROWS (\d+)", text).group(1)) == g.EMBEDDING_FEW_ROWS
     for name, code in g.ACTIVATIONS.items():
         assert int(re.search(r"GNNFD_ACT_%s = (\d+)" % name.upper(), text).group(1)) == code
