@@ -382,6 +382,7 @@ int gnnfd_layer_gat(const gnnfd_csr_t* csr, const void* d_x, int64_t ldx, gnnfd_
  * d_lse (may be NULL): [n, heads, 2] fp32, 8-byte aligned, receives each row's largest score and the sum of e^(s - largest): the
  * logarithm of the softmax's denominator in two parts, as the gradient needs it ((-infinity, 0) for rows without entries).
  * chunk_width: as for the other aggregations, but a multiple of dim (or >= heads * dim): a chunk holds whole heads.
+ * GNNFD_TOO_LARGE: more than 4,194,240 columns, 2^31 - 65536 entries or a pitch of 2^30; for d_dbias also more than 2,621,400 buckets.
  * d_scratch: gnnfd_attention_workspace_bytes(csr, heads, dim) bytes, 256-byte aligned (0 and NULL where the graph has no hub row).  fp32 sums and
  * softmax; the call only enqueues work. */
 int gnnfd_attention_workspace_bytes(const gnnfd_csr_t* csr, int32_t heads, int32_t dim, size_t* scratch_bytes);

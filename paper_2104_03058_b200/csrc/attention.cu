@@ -701,15 +701,16 @@ static void carve_attend(Carver& c, const gnnfd_csr_t* csr, const gnnfd_csr_t* c
 }
 
 constexpr int64_t kMostPitch = 0x3fffffff;       // elements: bytes fit 32 bits
+constexpr int64_t kMostColumns = 65535ll * kReduceCols, kMostBuckets = 65535ll * kBiasBuckets, kMostBiasSums = 0x7fffffffll * (kBlock / 32);   // grids
 
 // what the forward call and the backward call ask alike of their arguments
 static int check_attend(const gnnfd_csr_t* csr, gnnfd_dtype_t dt, gnnfd_dtype_t odt, int32_t heads, int32_t dim, float scale, float softcap,
                         const int32_t* d_dist, const float* d_bias, int32_t buckets, int32_t chunk_width, int32_t* chunk_heads)
 {
     if (!csr || heads <= 0 || dim <= 0 || chunk_width <= 0 || !(softcap >= 0.f) || softcap > 3.4e38f || scale != scale) return GNNFD_INVALID_ARG;
-    if ((int64_t)heads * dim > 0x7fffffffll) return GNNFD_INVALID_ARG;
+    if ((int64_t)heads * dim > kMostColumns) return GNNFD_TOO_LARGE;
     if ((dt != GNNFD_F32 && dt != GNNFD_BF16) || (odt != GNNFD_F32 && odt != GNNFD_BF16)) return GNNFD_UNSUPPORTED;
-    if (csr->nnz > 0x7fffff00ll) return GNNFD_TOO_LARGE;          // a walk looks up to 256 entries ahead
+    if (csr->nnz > 0x7fff0000ll) return GNNFD_TOO_LARGE;          // a short row's walk counts on as long as the longest beside it (2048 entries)
     if (dim > (dt == GNNFD_F32 ? 256 : 512)) return GNNFD_UNSUPPORTED;
     if ((d_bias != nullptr) != (buckets > 0) || buckets < 0) return GNNFD_INVALID_ARG;
     if (d_bias ? !d_dist && csr->nnz > 0 : d_dist != nullptr) return GNNFD_INVALID_ARG;
@@ -780,6 +781,7 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
 {
     using namespace gnnfd;
     int32_t chunk_heads;
+    if (d_dbias && (buckets > kMostBuckets || (int64_t)buckets * heads > kMostBiasSums)) return GNNFD_TOO_LARGE;
     int rc = check_attend(csr, dt, gdt, heads, dim, scale, softcap, d_dist, d_bias, buckets, chunk_width, &chunk_heads);
     if (rc) return rc;
     if (!csr_t || csr_t->n != csr->n || csr_t->nnz != csr->nnz) return GNNFD_INVALID_ARG;

@@ -100,3 +100,13 @@ def test_constants_of_the_header():
     assert int(re.search(r"#define GNNFD_EMBEDDING_FEW_ROWS (\d+)", text).group(1)) == g.EMBEDDING_FEW_ROWS
     for name, code in g.ACTIVATIONS.items():
         assert int(re.search(r"GNNFD_ACT_%s = (\d+)" % name.upper(), text).group(1)) == code
+
+
+def test_attention_refuses_what_its_grids_do_not_hold():
+    """Columns beyond 65535 blocks of 64 and buckets beyond 65535 blocks of 40 are refused before the graph is looked at."""
+    L, p = g.lib(), 4096
+    fwd = lambda heads, dim: L.gnnfd_aggregate_attention(p, p, 8, p, 8, p, 8, 0, heads, dim, 1.0, 0.0, None, None, 0, p, 8, 0, None, 8, None, 0, None)      # noqa: E731
+    back = lambda heads, buckets: L.gnnfd_aggregate_attention_backward(      # noqa: E731
+        p, p, p, 8, p, 8, p, 8, p, 8, 0, p, heads, 8, 1.0, 0.0, p, p, p, buckets, p, 8, p, 8, p, 8, 0, p, 8, p, 0, None)
+    assert fwd(65_536, 64) == fwd((1 << 31) - 1, 256) == g.TOO_LARGE
+    assert back(1, 65_535 * 40 + 1) == back((1 << 31) - 1, 9) == g.TOO_LARGE
