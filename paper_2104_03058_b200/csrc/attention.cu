@@ -363,7 +363,9 @@ __global__ void __launch_bounds__(kBlock, PASS == kForward ? 3 : 2) attend(const
             } else {
 #pragma unroll
                 for (int i = 0; i < UB; ++i) {
-                    const float p = PASS == kRowGrad ? weight(s[i], m) * inv : weight(s[i], stat[i].x) * stat[i].y;
+                    float p = PASS == kRowGrad ? weight(s[i], m) * inv : weight(s[i], stat[i].x) * stat[i].y;
+                    // exactly 0 for what is taken out: the row whose statistics these are (vertex 0's, past the end) may hold NaN
+                    if (PASS == kColGrad && MASKED) p = s[i] == -CUDART_INF_F ? 0.f : p;
                     if constexpr (PASS == kRowGrad) {
                         if (!MASKED || p != 0.f) {
                             const float pd = p * dp[i];

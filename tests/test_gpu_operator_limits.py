@@ -1,0 +1,66 @@
+"""The lookup, attention and group norm calls where one bad row stands among good ones, at extreme caps and sizes, and from two host
+threads at once.  References and bounds are those of the operators' own tests, unless a test derives its own."""
+import threading
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2104_03058_b200 as g  # noqa: E402
+import test_gpu_attention as att  # noqa: E402
+import test_gpu_embedding as emb  # noqa: E402
+import test_gpu_group_norm as norm  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24
+INF = float("inf")
+
+
+# ---------------------------------------------------------------- attention: bad rows
+
+def with_bad_row(p, row, name, bad):
+    """gradients and sums as they are, and with `bad` in row `row` of one operand"""
+    clean = p.backward(p.forward(with_lse=True)[1])
+    getattr(p, name)[row] = bad
+    return clean, p.backward(p.forward(with_lse=True)[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name,bad", [("q", float("nan")), ("q", INF), ("dout", float("nan"))])
+@pytest.mark.parametrize("row,hub", [(0, 0), (0, 2500), (9, 0)])
+def test_a_bad_row_changes_the_gradients_of_what_it_attends_to_alone(row, hub, name, bad, dtype):
+    n = 400
+    p = att.Problem(n, *att.edges(n, 3000, hub), 2, 8, dtype, cap=6.0)
+    attended = torch.zeros(n, dtype=torch.bool, device="cuda")
+    attended[p.col[p.row == row]] = True
+    assert 0 < int(attended.sum()) < n
+    clean, got = with_bad_row(p, row, name, bad)
+    others = torch.arange(n, device="cuda") != row
+    assert torch.equal(clean[0][others], got[0][others])                                  # dq
+    for was, now in zip(clean[1:3], got[1:3]):                                            # dk, dv
+        assert torch.equal(was[~attended], now[~attended])
+    assert torch.isnan(got[1][attended]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name,bad", [("q", float("nan")), ("q", INF), ("dout", float("nan"))])
+def test_a_bad_row_does_not_reach_what_the_bias_hides_from_it(name, bad, dtype):
+    """Row 7 attends to the vertices of even number; a bias of -infinity hides the others from it, from other rows some."""
+    n, row = 300, 7
+    src, dst = att.edges(n, 6000)
+    p = att.Problem(n, src, dst, 2, 16, dtype, cap=4.0, buckets=4)
+    p.bias[1] = -INF
+    dist = torch.randint(0, 4, src.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").int()
+    dist[dst == row] = torch.where(src[dst == row] % 2 == 1, 1, 2).int()
+    p.dist, p.dist_t = g.edge_values(p.csr, dist), g.edge_values(p.csr_t, dist)
+    here = p.row == row
+    attended, hidden = (torch.zeros(n, dtype=torch.bool, device="cuda") for _ in range(2))
+    attended[p.col[here & (p.col % 2 == 0)]] = True
+    hidden[p.col[here & (p.col % 2 == 1)]] = True
+    assert int(attended.sum()) > 3 and int(hidden.sum()) > 3
+    clean, got = with_bad_row(p, row, name, bad)
+    for was, now in zip(clean[1:3], got[1:3]):
+        assert torch.equal(was[~attended], now[~attended])
+    assert (got[3][1] == 0).all() and torch.equal(clean[3][[0, 3]], got[3][[0, 3]]) and torch.isnan(got[3][2]).all()
+    assert torch.isnan(got[1][attended]).all()
