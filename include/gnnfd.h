@@ -384,7 +384,8 @@ int gnnfd_layer_gat(const gnnfd_csr_t* csr, const void* d_x, int64_t ldx, gnnfd_
  * chunk_width: as for the other aggregations, but a multiple of dim (or >= heads * dim): a chunk holds whole heads.
  * GNNFD_TOO_LARGE: more than 4,194,240 columns, 2^31 - 65536 entries or a pitch of 2^30; for d_dbias also more than 2,621,400 buckets.
  * d_scratch: gnnfd_attention_workspace_bytes(csr, heads, dim) bytes, 256-byte aligned (0 and NULL where the graph has no hub row).  fp32 sums and
- * softmax; the call only enqueues work. */
+ * softmax; tanh is within 8 * 2^-24 of its value, for bf16 features and results of a call without d_lse and a cap of up to 64 within as much
+ * of 1 (a weight is then off by 2^-14 of itself at most).  The call only enqueues work. */
 int gnnfd_attention_workspace_bytes(const gnnfd_csr_t* csr, int32_t heads, int32_t dim, size_t* scratch_bytes);
 
 int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v,

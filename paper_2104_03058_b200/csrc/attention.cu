@@ -69,8 +69,11 @@ __device__ __forceinline__ float weight(float s, float m) { return ex2((s - (m =
 // capped at a few tens lie mostly in the first part, where an absolute error would be as large as the score.  tanhf, which is within 2 ulp, branches, and took a
 // quarter of the forward walk's instructions.
 //
-// ROUGH, for 16-bit features: the second part alone, within 8 * 2^-24 of 1.  The score is then off by so much of the cap (3e-5 of a weight at a cap of 50), a
-// hundredth of what the output's rounding takes; it saves 13 of the forward walk's 90 instructions per entry and head.
+// ROUGH: the second part alone, within 8 * 2^-24 of 1, so the score is off by so much of the cap.  Only where nothing is left of that in what the call
+// gives: the forward pass of bf16 features into bf16, without the sums that a gradient would go on with, and caps up to kRoughCap, where a weight is
+// off by 2 * 3e-5 of itself, a sixtieth of the output's half step of 2^-8.  It saves 13 of the forward walk's instructions per entry and head.
+constexpr float kRoughCap = 64.f;
+
 template <bool ROUGH>
 __device__ __forceinline__ float tanh_of(float x)
 {
@@ -198,7 +201,7 @@ __device__ __forceinline__ void store_head(void* out, int out_bf16, bool vec_ok,
 template <int WORDS> constexpr int in_flight() { return WORDS == 8 ? 2 : 4; }
 
 // The row's lanes: 2^lpr_log2 cover its columns, 2^lph_log2 of them a head, E elements each; 2^ep_log2 such groups walk interleaved entries.
-template <int PASS, typename T, int E, int LOAD>
+template <int PASS, typename T, int E, int LOAD, bool ROUGH>
 __global__ void __launch_bounds__(kBlock, PASS == kForward ? 3 : 2) attend(const __grid_constant__ AttendArgs a)
 {
     grid_dependency<false>();
@@ -331,7 +334,7 @@ __global__ void __launch_bounds__(kBlock, PASS == kForward ? 3 : 2) attend(const
             if (capped) {
 #pragma unroll
                 for (int i = 0; i < UB; ++i) {
-                    const float t = tanh_of<sizeof(T) == 2>(s[i] * a.inv_softcap);
+                    const float t = tanh_of<ROUGH>(s[i] * a.inv_softcap);
                     s[i] = a.softcap * t;
                     slope[i] = fmaf(-t, t, 1.f);
                 }
@@ -601,10 +604,12 @@ __global__ void __launch_bounds__(kBlock) attend_bias_join(const float* part, in
 
 typedef void (*AttendKernel)(const AttendArgs);
 
-template <int PASS, typename T, int E>
-static AttendKernel pick_load(int load)
+template <int PASS, typename T, int E, bool ROUGH = false>
+static AttendKernel pick_load(int load, bool rough)
 {
-    return load == kWide ? attend<PASS, T, E, kWide> : load == kVectors ? attend<PASS, T, E, kVectors> : attend<PASS, T, E, kScalars>;
+    if constexpr (PASS == kForward && sizeof(T) == 2 && !ROUGH)
+        if (rough) return pick_load<PASS, T, E, true>(load, rough);
+    return load == kWide ? attend<PASS, T, E, kWide, ROUGH> : load == kVectors ? attend<PASS, T, E, kVectors, ROUGH> : attend<PASS, T, E, kScalars, ROUGH>;
 }
 
 struct Operand { const void* p; int64_t ld; };
@@ -635,7 +640,7 @@ static HeadLayout head_layout(int size, int32_t dim, const Operand* ops, int n_o
 // ops: the rows' vectors, then the gathered ones (two of the latter, one or two of the former)
 template <int PASS>
 static int launch_attend(const char* name, const char* reduce_name, const gnnfd_csr_t* csr, AttendArgs& a, gnnfd_dtype_t dt, int32_t chunk_heads,
-                         const Operand (&ops)[4], cudaStream_t s)
+                         const Operand (&ops)[4], cudaStream_t s, bool rough = false)
 {
     const int size = dt == GNNFD_F32 ? 4 : 2;
     a.own0 = ops[0].p; a.ld_own0 = ops[0].ld;
@@ -661,8 +666,8 @@ static int launch_attend(const char* name, const char* reduce_name, const gnnfd_
     const int64_t grid_x = blocks * a.n_htiles;
     if (grid_x > 0x7fffffffll) return GNNFD_TOO_LARGE;
     AttendKernel kernel;
-    if (dt == GNNFD_F32) kernel = words == 8 ? pick_load<PASS, float, 8>(L.load) : pick_load<PASS, float, 4>(L.load);
-    else kernel = words == 8 ? pick_load<PASS, __nv_bfloat16, 16>(L.load) : pick_load<PASS, __nv_bfloat16, 8>(L.load);
+    if (dt == GNNFD_F32) kernel = words == 8 ? pick_load<PASS, float, 8>(L.load, rough) : pick_load<PASS, float, 4>(L.load, rough);
+    else kernel = words == 8 ? pick_load<PASS, __nv_bfloat16, 16>(L.load, rough) : pick_load<PASS, __nv_bfloat16, 8>(L.load, rough);
     for (int c0 = 0; grid_x > 0 && c0 < n_chunks; c0 += kMaxGridY) {
         a.chunk_base = c0;
         const dim3 grid((unsigned)grid_x, (unsigned)(n_chunks - c0 < kMaxGridY ? n_chunks - c0 : kMaxGridY));
@@ -759,8 +764,9 @@ int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t l
     a.part0 = g.part0; a.part_ml = g.part_ml;
     a.scale = scale; a.softcap = softcap; a.inv_softcap = softcap > 0.f ? 1.f / softcap : 0.f;
     a.heads = heads; a.dim = dim; a.f = (int32_t)f; a.fpad = (int32_t)align_up((size_t)f, 4);
+    const bool rough = softcap > 0.f && softcap <= kRoughCap && odt == GNNFD_BF16 && !d_lse;
     const Operand ops[4] = {{d_q, ldq}, {d_q, ldq}, {d_k, ldk}, {d_v, ldv}};
-    return launch_attend<kForward>("attend", "attend_hub_reduce", csr, a, dt, chunk_heads, ops, static_cast<cudaStream_t>(stream));
+    return launch_attend<kForward>("attend", "attend_hub_reduce", csr, a, dt, chunk_heads, ops, static_cast<cudaStream_t>(stream), rough);
 }
 
 int gnnfd_attention_backward_workspace_bytes(const gnnfd_csr_t* csr, const gnnfd_csr_t* csr_t, int32_t heads, int32_t dim, int32_t buckets,

@@ -64,3 +64,33 @@ def test_a_bad_row_does_not_reach_what_the_bias_hides_from_it(name, bad, dtype):
         assert torch.equal(was[~attended], now[~attended])
     assert (got[3][1] == 0).all() and torch.equal(clean[3][[0, 3]], got[3][[0, 3]]) and torch.isnan(got[3][2]).all()
     assert torch.isnan(got[1][attended]).all()
+
+
+# ---------------------------------------------------------------- attention: caps
+
+def check_capped(p, odt):
+    """Against the bounds for a tanh that is within 8 u of its own value."""
+    ref = att.reference(p.row, p.col, p.q.float(), p.k, p.v, p.heads, p.dim, p.scale, p.cap, p.dist, p.bias, p.dout)
+    out, lse = p.forward(with_lse=True, out_dtype=odt)
+    grads = p.backward(lse, out_dtype=odt)
+    assert torch.equal(out, p.forward(with_lse=True, out_dtype=odt)[0])
+    att.check(p.forward(out_dtype=odt), ref["out"], "out alone")
+    want, bound = ref["lse"]
+    some = want > -INF
+    assert ((att.lse_of(lse) - want).abs() <= 1.25 * bound)[some].all()
+    for name, got in zip(("out", "dq", "dk", "dv", "dbias"), (out, *grads)):
+        if got is not None:
+            att.check(got, ref[name], name)
+
+
+@pytest.mark.parametrize("dtype,odt,cap", [(BF16, F32, 0.5), (BF16, F32, 30.0), (BF16, BF16, 1e3), (BF16, F32, 1e4), (BF16, BF16, 1e4), (BF16, F32, 1e7),
+                                           (BF16, BF16, 1e7), (BF16, F32, 1e30), (F32, F32, 1e7)])
+def test_caps_of_any_size(dtype, odt, cap):
+    """A large cap is nearly none: scores as exact as without one, whatever the type of the features."""
+    for hub in (0, 2300):
+        check_capped(att.Problem(500, *att.edges(500, 6000, hub), 3, 16, dtype, cap=cap, buckets=4), odt)
+
+
+def test_gradients_of_small_caps_are_exact_to_the_features_type():
+    """Sums over the graph (the bias's gradient) stay fp32, so the capped scores behind them are as exact as for fp32 features."""
+    check_capped(att.Problem(800, *att.edges(800, 20_000), 4, 8, BF16, cap=20.0, buckets=5), F32)
