@@ -710,6 +710,9 @@ static void carve_attend(Carver& c, const gnnfd_csr_t* csr, const gnnfd_csr_t* c
 constexpr int64_t kMostPitch = 0x3fffffff;       // elements: bytes fit 32 bits
 constexpr int64_t kMostColumns = 65535ll * kReduceCols, kMostBuckets = 65535ll * kBiasBuckets, kMostBiasSums = 0x7fffffffll * (kBlock / 32);   // grids
 
+// 1 / cap, of caps below 2^-128 the largest number there is: a score of 0 stays 0, others reach such a cap anyway
+static float reciprocal_cap(float cap) { return cap > 0.f ? fminf(1.f / cap, 3.402823466e38f) : 0.f; }
+
 // what the forward call and the backward call ask alike of their arguments
 static int check_attend(const gnnfd_csr_t* csr, gnnfd_dtype_t dt, gnnfd_dtype_t odt, int32_t heads, int32_t dim, float scale, float softcap,
                         const int32_t* d_dist, const float* d_bias, int32_t buckets, int32_t chunk_width, int32_t* chunk_heads)
@@ -762,7 +765,7 @@ int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t l
     a.lse = reinterpret_cast<float2*>(d_lse);
     a.out0 = d_out; a.ld_out0 = ldo; a.out_bf16 = odt == GNNFD_BF16;
     a.part0 = g.part0; a.part_ml = g.part_ml;
-    a.scale = scale; a.softcap = softcap; a.inv_softcap = softcap > 0.f ? 1.f / softcap : 0.f;
+    a.scale = scale; a.softcap = softcap; a.inv_softcap = reciprocal_cap(softcap);
     a.heads = heads; a.dim = dim; a.f = (int32_t)f; a.fpad = (int32_t)align_up((size_t)f, 4);
     const bool rough = softcap > 0.f && softcap <= kRoughCap && odt == GNNFD_BF16 && !d_lse;
     const Operand ops[4] = {{d_q, ldq}, {d_q, ldq}, {d_k, ldk}, {d_v, ldv}};
@@ -810,7 +813,7 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
     a.stat = g.stat;
     a.out0 = d_dq; a.ld_out0 = lddq; a.out_bf16 = gdt == GNNFD_BF16;
     a.part0 = g.part0; a.part1 = g.part1; a.part_ml = g.part_ml;
-    a.scale = scale; a.softcap = softcap; a.inv_softcap = softcap > 0.f ? 1.f / softcap : 0.f;
+    a.scale = scale; a.softcap = softcap; a.inv_softcap = reciprocal_cap(softcap);
     a.heads = heads; a.dim = dim; a.f = (int32_t)f; a.fpad = (int32_t)align_up((size_t)f, 4);
     const Operand rows[4] = {{d_q, ldq}, {d_dout, lddo}, {d_k, ldk}, {d_v, ldv}}, cols[4] = {{d_k, ldk}, {d_v, ldv}, {d_q, ldq}, {d_dout, lddo}};
     rc = launch_attend<kRowGrad>("attend_row_grad", "attend_hub_reduce", csr, a, dt, chunk_heads, rows, s);

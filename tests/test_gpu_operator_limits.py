@@ -94,3 +94,17 @@ def test_caps_of_any_size(dtype, odt, cap):
 def test_gradients_of_small_caps_are_exact_to_the_features_type():
     """Sums over the graph (the bias's gradient) stay fp32, so the capped scores behind them are as exact as for fp32 features."""
     check_capped(att.Problem(800, *att.edges(800, 20_000), 4, 8, BF16, cap=20.0, buckets=5), F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_caps_whose_reciprocal_is_beyond_fp32(dtype):
+    """softcap = 1e-39: every score is within 1e-39 of 0, those of exactly 0 among them, so all entries weigh the same."""
+    n = 200
+    p = att.Problem(n, *att.edges(n, 2000), 2, 8, dtype, cap=1e-39)
+    p.q[::2] = 0
+    ref = att.reference(p.row, p.col, torch.zeros(n, 16, device="cuda"), p.k, p.v, 2, 8, 1.0, 0.0, dout=p.dout)
+    out, lse = p.forward(with_lse=True)
+    att.check(out, ref["out"], "out")
+    dq, dk, dv, _ = p.backward(lse)
+    att.check(dv, ref["dv"], "dv")
+    assert torch.isfinite(dq).all() and torch.isfinite(dk).all()
