@@ -362,6 +362,9 @@ constexpr int kClasses = 443;                                          // three 
 constexpr int kFewBlock = 512, kFewWarps = kFewBlock / 32;
 constexpr int kClassRows = GNNFD_EMBEDDING_FEW_ROWS / kClasses;        // of one class, at most
 constexpr int kCrowd = 64;
+// shared memory of a block with n ids and so many rows, and the most there can be
+constexpr size_t few_bytes(size_t n, size_t rows) { return n * sizeof(uint32_t) + (rows + 1) * sizeof(int) + n * sizeof(uint16_t); }
+constexpr int kFewSmem = (int)few_bytes(kFewIds, kClassRows);
 static_assert(kFewIds <= kFewWarps * 32 * 32, "a lane keeps one vote per step of its warp's share");
 static_assert(kFewIds <= 1 << 16 && kClassRows <= 1 << 16 && GNNFD_EMBEDDING_FEW_ROWS % kClasses == 0, "place and row in one word");
 
@@ -582,14 +585,13 @@ static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool ac
     const uintptr_t bits = (uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(TO));
     const int vec = bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
     if (few) {
-        const int rows = (int)((a.vocab + kClasses - 1) / kClasses);
-        const size_t smem = (size_t)a.n * sizeof(uint32_t) + (size_t)(rows + 1) * sizeof(int) + (size_t)a.n * sizeof(uint16_t);
+        const size_t smem = few_bytes((size_t)a.n, (size_t)((a.vocab + kClasses - 1) / kClasses));
         auto launch = [&](auto wide, auto id) -> int {
             constexpr int Q = decltype(wide)::value;
             const auto kernel = embedding_grad_few<decltype(id), TI, TO, V, Q>;
             const dim3 grid((unsigned)(a.vocab < kClasses ? a.vocab : kClasses), (unsigned)((a.f + 32 * V * Q - 1) / (32 * V * Q)));
-            // (static shared memory counts too: beyond 16 KB the limit is raised)
-            if (smem > 16 * 1024) GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            // Static shared memory counts too: beyond 16 KB the limit is raised, to the same for every call, since it is one for all host threads.
+            if (smem > 16 * 1024) GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
             GNNFD_LAUNCH("embedding_grad_few", s, kernel, grid, kFewBlock, smem, a, vec);
             return GNNFD_OK;
         };

@@ -108,3 +108,56 @@ def test_caps_whose_reciprocal_is_beyond_fp32(dtype):
     dq, dk, dv, _ = p.backward(lse)
     att.check(dv, ref["dv"], "dv")
     assert torch.isfinite(dq).all() and torch.isfinite(dk).all()
+
+
+# ---------------------------------------------------------------- gradient of the lookup
+
+@pytest.mark.parametrize("f,itype", [(1, torch.int32), (5, torch.int64), (40, torch.int32)])
+def test_the_largest_gradient_of_one_launch(f, itype):
+    """As many ids and rows as the one-launch path takes, all of its shared memory in use; beside it one of each more."""
+    for n, vocab in ((g.EMBEDDING_FEW_IDS, g.EMBEDDING_FEW_ROWS), (g.EMBEDDING_FEW_IDS + 1, g.EMBEDDING_FEW_ROWS), (g.EMBEDDING_FEW_IDS, g.EMBEDDING_FEW_ROWS + 1)):
+        ids = emb.draw_ids(n, vocab, "skew", itype)
+        ids[:3] = torch.tensor([vocab - 1, 0, vocab - 1], device="cuda")
+        dout = emb.rand(n, f)
+        emb.check_grad(g.embedding_backward(ids, dout, vocab, scale=0.7), ids, dout, vocab, 0.7)
+
+
+def from_two_threads(calls, turns):
+    """what went wrong in `turns` calls of each of two functions, made by two host threads at once"""
+    wrong, start = [], threading.Barrier(2)
+
+    def work(call):
+        start.wait()
+        try:
+            for _ in range(turns):
+                call()
+        except Exception as err:                                                          # noqa: BLE001
+            wrong.append(err)
+    threads = [threading.Thread(target=work, args=(call,)) for call in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    return wrong
+
+
+def test_gradients_of_different_sizes_from_two_threads():
+    """Through the C call, so that the threads spend their time in it; each waits for its stream now and then, lest a full queue holds it up."""
+    vocab, f, calls, jobs = 443, 8, [], []
+    for n in (16_384, 9_000):
+        ids, dout, out = emb.draw_ids(n, vocab, "even", torch.int32, n), emb.rand(n, f, seed=n), torch.empty((vocab, f), device="cuda")
+        stream = torch.cuda.Stream()
+        args = (n, ids.data_ptr(), g.I32, dout.data_ptr(), f, g.F32, vocab, f, 1.0, -1, 0, out.data_ptr(), f, g.F32, None, 0, None, stream.cuda_stream)
+        jobs.append((ids, dout, out))
+
+        def call(args=args, stream=stream, gradient=g.lib().gnnfd_embedding_backward):
+            for _ in range(100):
+                if gradient(*args) != g.OK:
+                    raise RuntimeError("the call of %d ids failed" % args[0])
+            stream.synchronize()
+        calls.append(call)
+    torch.cuda.synchronize()
+    assert not from_two_threads(calls, 100)
+    for ids, dout, out in jobs:
+        emb.check_grad(out, ids, dout, vocab, 1.0)
