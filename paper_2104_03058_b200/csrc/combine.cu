@@ -678,25 +678,20 @@ int combine_impl(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
     if (a.tmem_cols == 256 && smem < 80 * 1024) smem = 80 * 1024;
     if (a.tmem_cols == 512 && smem < 120 * 1024) smem = 120 * 1024;
 
+    // (Ahead of the tensor maps: those are made by the driver, which asks for a context that a thread has from its first runtime call on.)
+    const void* const kernel = bf16 ? (const void*)combine_mma<true, false> : !split ? (const void*)combine_mma<false, false>
+                               : xt ? (const void*)combine_mma<false, true, true> : (const void*)combine_mma<false, true>;
+    GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     CUtensorMap map_x, map_w;
     if (!make_map(&map_x, d_x, bf16, n, f_in, ldx, kTileM) || !make_map(&map_w, d_w_t, bf16, f_out, f_in, ldw, a.tile_n)) {
         set_cuda_error(cudaErrorInvalidValue);
         return GNNFD_CUDA_ERROR;
     }
     const dim3 grid((unsigned)((n + kTileM - 1) / kTileM), (unsigned)((f_out + a.tile_n - 1) / a.tile_n));
-    if (bf16) {
-        GNNFD_CUDA_CHECK(cudaFuncSetAttribute(combine_mma<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        GNNFD_LAUNCH("combine_bf16", s, (combine_mma<true, false>), grid, kCombineThreads, smem, map_x, map_w, a);
-    } else if (split && xt) {
-        GNNFD_CUDA_CHECK(cudaFuncSetAttribute(combine_mma<false, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        GNNFD_LAUNCH("combine_fp32_3xtf32", s, (combine_mma<false, true, true>), grid, kSplitThreads, smem, map_x, map_w, a);
-    } else if (split) {
-        GNNFD_CUDA_CHECK(cudaFuncSetAttribute(combine_mma<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        GNNFD_LAUNCH("combine_fp32_3xtf32", s, (combine_mma<false, true>), grid, kSplitThreads, smem, map_x, map_w, a);
-    } else {
-        GNNFD_CUDA_CHECK(cudaFuncSetAttribute(combine_mma<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        GNNFD_LAUNCH("combine_tf32", s, (combine_mma<false, false>), grid, kCombineThreads, smem, map_x, map_w, a);
-    }
+    if (bf16) GNNFD_LAUNCH("combine_bf16", s, (combine_mma<true, false>), grid, kCombineThreads, smem, map_x, map_w, a);
+    else if (split && xt) GNNFD_LAUNCH("combine_fp32_3xtf32", s, (combine_mma<false, true, true>), grid, kSplitThreads, smem, map_x, map_w, a);
+    else if (split) GNNFD_LAUNCH("combine_fp32_3xtf32", s, (combine_mma<false, true>), grid, kSplitThreads, smem, map_x, map_w, a);
+    else GNNFD_LAUNCH("combine_tf32", s, (combine_mma<false, false>), grid, kCombineThreads, smem, map_x, map_w, a);
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
 }

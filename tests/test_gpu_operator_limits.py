@@ -122,9 +122,9 @@ def test_the_largest_gradient_of_one_launch(f, itype):
         emb.check_grad(g.embedding_backward(ids, dout, vocab, scale=0.7), ids, dout, vocab, 0.7)
 
 
-def from_two_threads(calls, turns):
-    """what went wrong in `turns` calls of each of two functions, made by two host threads at once"""
-    wrong, start = [], threading.Barrier(2)
+def from_threads(calls, turns):
+    """what went wrong in `turns` calls of each function, made by host threads at once"""
+    wrong, start = [], threading.Barrier(len(calls))
 
     def work(call):
         start.wait()
@@ -142,7 +142,7 @@ def from_two_threads(calls, turns):
     return wrong
 
 
-def test_gradients_of_different_sizes_from_two_threads():
+def test_gradients_of_different_sizes_from_threads():
     """Through the C call, so that the threads spend their time in it; each waits for its stream now and then, lest a full queue holds it up."""
     vocab, f, calls, jobs = 443, 8, [], []
     for n in (16_384, 9_000):
@@ -158,6 +158,14 @@ def test_gradients_of_different_sizes_from_two_threads():
             stream.synchronize()
         calls.append(call)
     torch.cuda.synchronize()
-    assert not from_two_threads(calls, 100)
+    assert not from_threads(calls, 100)
     for ids, dout, out in jobs:
         emb.check_grad(out, ids, dout, vocab, 1.0)
+
+
+def test_a_transform_as_the_first_call_of_a_thread():
+    """A thread that has made no other call yet, the result's memory given."""
+    x, w, out = emb.rand(300, 64), emb.rand(16, 64, seed=1), torch.empty((300, 16), device="cuda")
+    want = g.combine(x, w)
+    assert not from_threads([lambda: g.combine(x, w, out=out)], 1)
+    assert torch.equal(out, want)
