@@ -681,7 +681,8 @@ int combine_impl(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
     // (Ahead of the tensor maps: those are made by the driver, which asks for a context that a thread has from its first runtime call on.)
     const void* const kernel = bf16 ? (const void*)combine_mma<true, false> : !split ? (const void*)combine_mma<false, false>
                                : xt ? (const void*)combine_mma<false, true, true> : (const void*)combine_mma<false, true>;
-    GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    // The limit is one for all host threads, so every call sets the same.
+    GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudgetMax + 1024));
     CUtensorMap map_x, map_w;
     if (!make_map(&map_x, d_x, bf16, n, f_in, ldx, kTileM) || !make_map(&map_w, d_w_t, bf16, f_out, f_in, ldw, a.tile_n)) {
         set_cuda_error(cudaErrorInvalidValue);

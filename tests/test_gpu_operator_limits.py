@@ -169,3 +169,23 @@ def test_a_transform_as_the_first_call_of_a_thread():
     want = g.combine(x, w)
     assert not from_threads([lambda: g.combine(x, w, out=out)], 1)
     assert torch.equal(out, want)
+
+
+def test_transforms_of_different_sizes_from_threads():
+    """One stream, so that the transforms run one after the other; only the calls meet."""
+    calls, jobs = [], []
+    for f_in, f_out in ((8, 240), (8, 16), (16, 8)):
+        x, w = emb.rand(300, f_in, seed=f_in), emb.rand(f_out, f_in, seed=f_out)
+        out = torch.empty((300, f_out), device="cuda")
+        args = (300, x.data_ptr(), f_in, g.F32, f_in, w.data_ptr(), f_in, f_out, out.data_ptr(), f_out, g.F32, None, 0)
+        jobs.append((out, g.combine(x, w, mode="tf32")))
+
+        def call(args=args, transform=g.lib().gnnfd_combine):
+            for _ in range(100):
+                if transform(*args) != g.OK:
+                    raise RuntimeError("the transform of %d columns failed" % args[4])
+            torch.cuda.synchronize()
+        calls.append(call)
+    assert not from_threads(calls, 200)
+    for out, want in jobs:
+        assert torch.equal(out, want)
