@@ -178,7 +178,7 @@ def test_transforms_of_different_sizes_from_threads():
         x, w = emb.rand(300, f_in, seed=f_in), emb.rand(f_out, f_in, seed=f_out)
         out = torch.empty((300, f_out), device="cuda")
         args = (300, x.data_ptr(), f_in, g.F32, f_in, w.data_ptr(), f_in, f_out, out.data_ptr(), f_out, g.F32, None, 0)
-        jobs.append((out, g.combine(x, w, mode="tf32")))
+        jobs.append((out, g.combine(x, w, mode="tf32"), x, w))
 
         def call(args=args, transform=g.lib().gnnfd_combine):
             for _ in range(100):
@@ -187,5 +187,5 @@ def test_transforms_of_different_sizes_from_threads():
             torch.cuda.synchronize()
         calls.append(call)
     assert not from_threads(calls, 200)
-    for out, want in jobs:
+    for out, want, _, _ in jobs:
         assert torch.equal(out, want)
