@@ -459,7 +459,7 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * (-1: none) take no part: their row is treated as one that no id names.  Ids outside [0, vocab) take no part and set bit 0 of *d_status;
  * bit 1 is set if a block of the sort gave up waiting for another one (grad is then incomplete).  d_dout [n, ldd] of type ddt;
  * d_grad [vocab, ldg], not overlapping it.  d_scratch: gnnfd_embedding_backward_workspace_bytes(n, vocab, f) bytes, 256-byte
- * aligned (0 bytes up to GNNFD_EMBEDDING_FEW_IDS ids of a table of up to GNNFD_EMBEDDING_FEW_ROWS rows, NULL is then accepted).  Both
+ * aligned (0 bytes for no ids, and up to GNNFD_EMBEDDING_FEW_IDS ids of a table of up to GNNFD_EMBEDDING_FEW_ROWS rows; NULL is then accepted).  Both
  * calls only enqueue work. */
 #define GNNFD_EMBEDDING_FEW_IDS 16384
 #define GNNFD_EMBEDDING_FEW_ROWS 3629056

@@ -104,7 +104,7 @@ struct GradArgs {
     const unsigned long long* words;       // sorted: id << val_bits | position + 1; ids out of range last
     const BuildCounts* counts;
     float *head, *tail;                    // [blocks, fpad] partial sums of the run that a block starts / ends inside of
-    uint8_t* mark;                         // [vocab] rows that get a sum, zeroed (null where the gradient is added to what is there)
+    uint8_t* mark;                         // [vocab] rows that get a sum, zeroed (null where the gradient is added to what is there, or nothing is)
     int32_t* status;
     float scale;
     int32_t f, fpad, lpr_log2, val_bits, per_block, n_blocks, wide, accumulate;
@@ -281,14 +281,14 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
 {
     grid_dependency<true>();
     __shared__ float sums[kEmbedBlock];
-    if (a.counts->sort_failed) {
+    const int64_t join_blocks = a.n_blocks;                  // 0 where there were no ids, and then no sort
+    if (join_blocks > 0 && a.counts->sort_failed) {
         if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, 2);
         return;
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status && a.counts->bad_index) atomicOr(a.status, 1);
-    const int64_t n_valid = a.counts->n_valid;
-    const int64_t join_blocks = a.n_blocks;
+    if (join_blocks > 0 && blockIdx.x == 0 && threadIdx.x == 0 && a.status && a.counts->bad_index) atomicOr(a.status, 1);
     if (blockIdx.x < join_blocks) {
+        const int64_t n_valid = a.counts->n_valid;
         const int64_t b = blockIdx.x, begin = b * a.per_block, next = begin + a.per_block;
         auto key_at = [&](int64_t i) { return (int64_t)(a.words[i] >> a.val_bits); };
         if (next >= n_valid) return;
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kEmbedBlock) embedding_grad_finish(const __gri
     const int lpr = 1 << a.lpr_log2, lane = threadIdx.x & (lpr - 1), groups = kEmbedBlock >> a.lpr_log2;
     const int64_t stride = ((int64_t)gridDim.x - join_blocks) * groups;
     for (int64_t row = (blockIdx.x - join_blocks) * groups + (threadIdx.x >> a.lpr_log2); row < a.vocab; row += stride) {
-        if (a.mark[row]) continue;
+        if (a.mark && a.mark[row]) continue;
         char* const p = reinterpret_cast<char*>(static_cast<TO*>(a.out) + row * a.ldo);
         const int bytes = a.f * (int)sizeof(TO);
         int at = lane * vec;
@@ -604,12 +604,13 @@ static int launch_grad(const GradArgs& a, gnnfd_itype_t itype, bool few, bool ac
     } else {
         const int per_tile = (V << a.lpr_log2) * (a.wide ? wide_lane(V) : 1);
         const dim3 sums((unsigned)a.n_blocks, (unsigned)((a.f + per_tile - 1) / per_tile));
-        if (a.wide) GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V, wide_lane(V)>), sums, kEmbedBlock, 0, a);
+        if (a.n_blocks == 0) {}                                        // no ids
+        else if (a.wide) GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V, wide_lane(V)>), sums, kEmbedBlock, 0, a);
         else GNNFD_LAUNCH("embedding_grad_sums", s, (embedding_grad_sums<TI, TO, V, 1>), sums, kEmbedBlock, 0, a);
         const int64_t groups = kEmbedBlock >> a.lpr_log2, zero = accumulate ? 0 : (a.vocab + groups - 1) / groups;
         const int64_t grid = (int64_t)a.n_blocks + (zero < 16 * kSms ? zero : 16 * kSms);
         if (grid > 0x7fffffffll) return GNNFD_TOO_LARGE;
-        GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, vec);
+        if (grid > 0) GNNFD_LAUNCH("embedding_grad_finish", s, (embedding_grad_finish<TO>), (unsigned)grid, kEmbedBlock, 0, a, vec);
     }
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
@@ -655,7 +656,7 @@ int gnnfd_embedding_backward_workspace_bytes(int64_t n, int64_t vocab, int32_t f
     if (n < 0 || vocab <= 0 || f <= 0 || !scratch_bytes) return GNNFD_INVALID_ARG;
     if (n > 0x7ffffff0ll || vocab > 0x7ffffff0ll) return GNNFD_TOO_LARGE;
     *scratch_bytes = 0;
-    if (few_ids(n, vocab)) return GNNFD_OK;
+    if (n == 0 || few_ids(n, vocab)) return GNNFD_OK;
     Carver c(nullptr, ~size_t(0));
     GradScratch g;
     const int rc = carve_grad(c, n, vocab, f, &g);
@@ -675,7 +676,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
     if (n > 0 && (!d_ids || !d_dout)) return GNNFD_INVALID_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool few = few_ids(n, vocab);
-    if (few && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
+    if ((few || n == 0) && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
     int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
     // a group reads eight words at a time at least: rows narrower than eight vectors are taken in narrower ones
     if (!few && v > 2 && (f + v - 1) / v < kInFlight) v = 2;
@@ -687,7 +688,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
     a.lpr_log2 = lanes_log2(f, v);
     if (a.lpr_log2 < 3) a.lpr_log2 = 3;
     a.wide = f > v << a.lpr_log2 && v < 8;
-    if (!few) {
+    if (!few && n > 0) {
         if (!d_scratch || ((uintptr_t)d_scratch & 255u)) return GNNFD_INVALID_ARG;
         Carver c(d_scratch, scratch_bytes);
         GradScratch g;

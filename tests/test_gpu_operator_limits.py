@@ -189,3 +189,17 @@ def test_transforms_of_different_sizes_from_threads():
     assert not from_threads(calls, 200)
     for out, want, _, _ in jobs:
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("odt", [F32, BF16])
+@pytest.mark.parametrize("vocab", [1000, g.EMBEDDING_FEW_ROWS, g.EMBEDDING_FEW_ROWS + 1, 5_000_000])
+def test_the_gradient_of_no_ids(vocab, odt):
+    ids, dout = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty((0, 3), device="cuda")
+    buf = torch.full((vocab, 5), 7.0, device="cuda", dtype=odt)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    g.embedding_backward(ids, dout, vocab, accumulate=True, out=buf[:, :3], status=status)
+    assert (buf == 7.0).all()
+    g.embedding_backward(ids, dout, vocab, out=buf[:, :3], status=status)
+    assert (buf[:, :3] == 0).all() and (buf[:, 3:] == 7.0).all() and int(status) == 0
+    fresh = g.embedding_backward(ids, torch.empty((0, 8), device="cuda"), vocab, out_dtype=odt)
+    assert fresh.shape == (vocab, 8) and (fresh == 0).all()
