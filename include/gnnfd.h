@@ -459,8 +459,9 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * (-1: none) take no part: their row is treated as one that no id names.  Ids outside [0, vocab) take no part and set bit 0 of *d_status;
  * bit 1 is set if a block of the sort gave up waiting for another one (grad is then incomplete).  d_dout [n, ldd] of type ddt;
  * d_grad [vocab, ldg], not overlapping it.  d_scratch: gnnfd_embedding_backward_workspace_bytes(n, vocab, f) bytes, 256-byte
- * aligned (0 bytes for no ids, and up to GNNFD_EMBEDDING_FEW_IDS ids of a table of up to GNNFD_EMBEDDING_FEW_ROWS rows; NULL is then accepted).  Both
- * calls only enqueue work. */
+ * aligned (0 bytes for no ids, and up to GNNFD_EMBEDDING_FEW_IDS ids of a table of up to GNNFD_EMBEDDING_FEW_ROWS rows; NULL is then accepted).  GNNFD_TOO_LARGE:
+ * 2^31 - 15 or more ids or rows (2^31 in the lookup), more than 65535 * 256 columns in the gradient (65535 * 128 where rows do not all start on two
+ * elements of their type), 2^31 - 4096 in the lookup.  Both calls only enqueue work. */
 #define GNNFD_EMBEDDING_FEW_IDS 16384
 #define GNNFD_EMBEDDING_FEW_ROWS 3629056
 int gnnfd_embedding(int64_t n, const void* d_ids, gnnfd_itype_t itype, int64_t vocab, const void* d_table, int64_t ldt,

@@ -34,6 +34,8 @@ static int lanes_log2(int f, int v)
 
 // ------------------------------------------------------------------ lookup
 
+constexpr int32_t kMostLookup = 0x7ffff000;      // columns: a row's walk counts on for up to 32 vectors, in 32 bits
+
 struct LookupArgs {
     const void *ids, *table;
     void* out;
@@ -638,7 +640,7 @@ int gnnfd_embedding(int64_t n, const void* d_ids, gnnfd_itype_t itype, int64_t v
     using namespace gnnfd;
     if (n < 0 || vocab <= 0 || f <= 0 || ldt < f || ldo < f) return GNNFD_INVALID_ARG;
     if (!known(tdt) || !known(odt) || (itype != GNNFD_I32 && itype != GNNFD_I64)) return GNNFD_UNSUPPORTED;
-    if (n > 0x7fffffffll || vocab > 0x7fffffffll) return GNNFD_TOO_LARGE;
+    if (n > 0x7fffffffll || vocab > 0x7fffffffll || f > kMostLookup) return GNNFD_TOO_LARGE;
     if (n == 0) return GNNFD_OK;
     if (!d_ids || !d_table || !d_out) return GNNFD_INVALID_ARG;
     const int v = embed_vector(d_table, ldt, tdt, d_out, ldo, odt);
@@ -678,6 +680,7 @@ int gnnfd_embedding_backward(int64_t n, const void* d_ids, gnnfd_itype_t itype, 
     const bool few = few_ids(n, vocab);
     if ((few || n == 0) && drill.sweep >= 0) return GNNFD_INVALID_ARG;             // no sort to drill
     int v = embed_vector(d_dout, ldd, ddt, d_grad, ldg, gdt);
+    if ((f - 1) / (32 * v * wide_lane(v)) >= 65535) return GNNFD_TOO_LARGE;      // column tiles are a grid's rows
     // a group reads eight words at a time at least: rows narrower than eight vectors are taken in narrower ones
     if (!few && v > 2 && (f + v - 1) / v < kInFlight) v = 2;
     if (!few && (f + v - 1) / v < kInFlight) v = 1;

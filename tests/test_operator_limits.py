@@ -5,7 +5,27 @@ torch = pytest.importorskip("torch")
 
 import paper_2104_03058_b200 as g  # noqa: E402
 
+P = 4096                                             # an aligned address that nothing reads
+
+
+def lookup(f, n=1, vocab=5):
+    return g.lib().gnnfd_embedding(n, P, 0, vocab, P, f, 0, f, 1.0, P, f, 0, None, None)
+
+
+def gradient(f, n=19_000, vocab=5, out=P):
+    return g.lib().gnnfd_embedding_backward(n, P, 0, P, f, 0, vocab, f, 1.0, -1, 0, out, f, 0, P, 1 << 60, None, None)
+
 
 def test_no_ids_need_no_workspace():
     for vocab in (1, g.EMBEDDING_FEW_ROWS, g.EMBEDDING_FEW_ROWS + 1, 100_000_000):
         assert g.embedding_backward_workspace_bytes(0, vocab, 64) == 0
+
+
+def test_rows_wider_than_the_grids():
+    """65535 column tiles: of 256 columns, of 128 where rows can only be read element by element."""
+    for n in (100, 19_000):
+        assert gradient(65_535 * 256 + 8, n) == g.TOO_LARGE                       # rows start on 16 bytes
+        assert gradient(65_535 * 256 + 2, n) == g.TOO_LARGE                       # on 8
+        assert gradient(65_535 * 128 + 1, n) == gradient(65_535 * 128 + 8, n, out=P + 4) == g.TOO_LARGE
+        assert gradient((1 << 31) - 1, n) == g.TOO_LARGE
+    assert lookup((1 << 31) - 1) == lookup((1 << 31) - 1024) == g.TOO_LARGE       # column counters are 32 bits
