@@ -233,10 +233,11 @@ def _scratch_args(scratch, device):
 class Csr:
     """Handle of a built CSR; keeps the persistent device buffer alive."""
 
-    def __init__(self, handle, persistent: torch.Tensor, device):
+    def __init__(self, handle, persistent: torch.Tensor, device, e: int | None = None):
         self._h = handle
         self._persistent = persistent
         self.device = device
+        self.e = e                                 # edges of the list that the graph was built from
         # one array of 64-bit words takes every result: n, nnz, max degree, segments, five bin counts, twelve pointers
         r = (ctypes.c_int64 * 21)()
         at = [ctypes.addressof(r) + 8 * i for i in range(21)]
@@ -310,7 +311,7 @@ def build_csr(n: int, src: torch.Tensor, dst: torch.Tensor, flags: int = 0, stre
                                persistent.data_ptr(), persistent.numel(), scratch.data_ptr(), scratch.numel(),
                                _stream_ptr(stream), ctypes.byref(handle))
     _check(st, "gnnfd_build_csr")
-    return Csr(handle, persistent, src.device)
+    return Csr(handle, persistent, src.device, e)
 
 
 def aggregate_workspace_bytes(csr: Csr, f: int) -> int:
@@ -753,11 +754,13 @@ def _status_ptr(status, device):
 
 
 def edge_values(csr: Csr, values: torch.Tensor, loop=0) -> torch.Tensor:
-    """The values [e] of the input edges in CSR slot order: a reverse edge that the build added has its edge's value, an added
-    self-loop the value ``loop``."""
+    """The values [e] of the input edges, one for each edge of the list that the graph was built from, in CSR slot order: a reverse edge
+    that the build added has its edge's value, an added self-loop the value ``loop``."""
     if values.dim() != 1 or values.device != csr.device:
         raise ValueError("values must be a 1-D tensor on %s" % csr.device)
-    perm, e = csr.perm.long(), values.shape[0]
+    if values.shape[0] != csr.e:
+        raise ValueError("values has %d entries, the graph was built from %d edges" % (values.shape[0], csr.e))
+    perm, e = csr.perm.long(), csr.e
     if e == 0:
         return torch.full((csr.nnz,), loop, dtype=values.dtype, device=csr.device)
     return torch.where(perm < 0, torch.full((), loop, dtype=values.dtype, device=csr.device), values[perm.clamp_min(0) % e])

@@ -1,9 +1,12 @@
 """What the lookup, attention and group norm calls refuse or accept at their limits: host logic, before any launch."""
+from types import SimpleNamespace
+
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import paper_2104_03058_b200 as g  # noqa: E402
+from paper_2104_03058_b200 import binding as b  # noqa: E402
 
 P = 4096                                             # an aligned address that nothing reads
 
@@ -29,3 +32,11 @@ def test_rows_wider_than_the_grids():
         assert gradient(65_535 * 128 + 1, n) == gradient(65_535 * 128 + 8, n, out=P + 4) == g.TOO_LARGE
         assert gradient((1 << 31) - 1, n) == g.TOO_LARGE
     assert lookup((1 << 31) - 1) == lookup((1 << 31) - 1024) == g.TOO_LARGE       # column counters are 32 bits
+
+
+def test_edge_values_want_one_value_for_each_edge():
+    csr = SimpleNamespace(device=torch.device("cpu"), nnz=6, e=3, perm=torch.tensor([0, 4, 2, 3, -1, 1], dtype=torch.int32))
+    assert b.edge_values(csr, torch.tensor([10, 20, 30]), loop=7).tolist() == [10, 20, 30, 10, 7, 20]
+    for count in (0, 1, 2, 4, 6):
+        with pytest.raises(ValueError, match="3 edges"):
+            b.edge_values(csr, torch.zeros(count))
