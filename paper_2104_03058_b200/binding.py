@@ -705,7 +705,7 @@ def layer(csr: Csr, model: str, x: torch.Tensor, w_t: torch.Tensor, f_in: int | 
 
 # Kernels are launched on the current device, so the entry points below make that of their tensors current where it is another one: they call
 # themselves once more inside _elsewhere.
-_current_device = torch._C._cuda_getDevice
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (a torch without CUDA lacks it)
 
 
 def _elsewhere(device, stream, again, *args, **kwargs):

@@ -1,4 +1,7 @@
 """What the lookup, attention and group norm calls refuse or accept at their limits: host logic, before any launch."""
+import os
+import subprocess
+import sys
 from types import SimpleNamespace
 
 import pytest
@@ -40,3 +43,14 @@ def test_edge_values_want_one_value_for_each_edge():
     for count in (0, 1, 2, 4, 6):
         with pytest.raises(ValueError, match="3 edges"):
             b.edge_values(csr, torch.zeros(count))
+
+
+def test_the_package_imports_where_torch_has_no_cuda():
+    code = ("import torch\n"
+            "for name in [n for n in dir(torch._C) if n.startswith('_cuda')]: delattr(torch._C, name)\n"
+            "import paper_2104_03058_b200 as g\n"
+            "try: g.group_norm(torch.zeros(4, 8), 2)\n"
+            "except ValueError as err: assert 'CUDA tensor' in str(err)\n"
+            "else: raise AssertionError\n")
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0, done.stderr
