@@ -291,7 +291,8 @@ __device__ __forceinline__ int64_t graph_of(const NormArgs& a, int64_t r)
     }
     return count == 1 && offset_at(a, lo + 1) <= r ? lo + 1 : lo;
 }
-__device__ __forceinline__ bool is_small(const NormArgs& a, int64_t rows) { return rows <= a.small_rows; }
+// (a graph whose offsets go back counts as empty)
+__device__ __forceinline__ bool is_small(const NormArgs& a, int64_t rows) { return max(rows, (int64_t)0) <= a.small_rows; }
 
 // work(graph, first row, one past the last row) for every piece inside slab s of a graph that no warp takes; uniform over the block
 template <typename F>

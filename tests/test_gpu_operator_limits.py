@@ -203,3 +203,19 @@ def test_the_gradient_of_no_ids(vocab, odt):
     assert (buf[:, :3] == 0).all() and (buf[:, 3:] == 7.0).all() and int(status) == 0
     fresh = g.embedding_backward(ids, torch.empty((0, 8), device="cuda"), vocab, out_dtype=odt)
     assert fresh.shape == (vocab, 8) and (fresh == 0).all()
+
+
+# ---------------------------------------------------------------- group norm
+
+@pytest.mark.parametrize("n,f,groups", [(3000, 16, 2), (200_000, 64, 32)])
+def test_statistics_of_graphs_whose_offsets_go_back(n, f, groups):
+    """They count as empty: mean 0 and rstd eps^-1/2, in calls of few pieces and of many."""
+    x, eps = norm.rand(n, f), 1e-5
+    ptr = torch.tensor([0, n // 2, n // 4, n], dtype=torch.int32, device="cuda")
+    out, mean, rstd = torch.zeros_like(x), *(torch.full((3, groups), float("nan"), device="cuda") for _ in range(2))
+    scratch = torch.empty(g.group_norm_workspace_bytes(n, f, groups, 3), dtype=torch.uint8, device="cuda")
+    status = g.lib().gnnfd_group_norm(n, x.data_ptr(), f, g.F32, f, groups, 3, ptr.data_ptr(), g.I32, None, None, eps, 0, out.data_ptr(), f, g.F32,
+                                      mean.data_ptr(), rstd.data_ptr(), scratch.data_ptr(), scratch.numel(), torch.cuda.current_stream().cuda_stream)
+    assert status == g.OK
+    assert (mean[1] == 0).all() and torch.allclose(rstd[1], torch.full_like(rstd[1], eps ** -0.5), rtol=4 * U)
+    assert torch.isfinite(mean[0]).all() and torch.isfinite(rstd[0]).all()
