@@ -219,3 +219,23 @@ def test_statistics_of_graphs_whose_offsets_go_back(n, f, groups):
     assert status == g.OK
     assert (mean[1] == 0).all() and torch.allclose(rstd[1], torch.full_like(rstd[1], eps ** -0.5), rtol=4 * U)
     assert torch.isfinite(mean[0]).all() and torch.isfinite(rstd[0]).all()
+
+
+def test_gelu_is_exact_relative_to_itself():
+    """With a weight of 0 the norm's output is act(bias) and, of one row, the gradient of the bias act'(bias).  With Phi the normal distribution's
+    integral: Phi(-|z|) is a polynomial, off by 13 u (2 u its fit, 5 its evaluation, 6 the reciprocal in it), times e^(-z^2/2): its argument carries
+    three roundings, an error of 3 u z^2/2, and the exponential 2 ulp; two products more: 19 + 1.5 z^2, taken as (20 + 2 z^2) u of Phi.  For z > 0 it is
+    1 - Phi(-z), one rounding more of results between a half and 1.  Below 2^-126 the exponential is 0.  The slope Phi + z phi adds (8 + 2 z^2) u of its
+    second term and 2 u of the sum of both."""
+    z = torch.cat([torch.linspace(-13, 13, 8000), torch.tensor([0.0, -0.0, -1e-20, 1e-20, 40.0, -40.0])]).cuda()
+    z = torch.cat([z, torch.zeros(8192 - z.numel(), device="cuda")])
+    x, w = norm.rand(1, z.numel(), seed=4), torch.zeros_like(z)
+    out, mean, rstd = g.group_norm(x, 1, w, z, activation="gelu", with_stats=True)
+    db = g.group_norm_backward(torch.ones_like(x), x, 1, mean, rstd, w, z, activation="gelu")[2]
+    z = z.double()
+    cdf, far = 0.5 * torch.special.erfc(-z / 2 ** 0.5), 0.5 * torch.special.erfc(z.abs() / 2 ** 0.5)
+    e_cdf = (20 + 2 * z * z) * U * far + 2 ** -126 + torch.where(z > 0, 2 * U, 0.0)
+    assert ((out[0].double() - z * cdf).abs() <= z.abs() * e_cdf + U * (z * cdf).abs() + 1e-37).all()
+    part = z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    tol = e_cdf + (8 + 2 * z * z) * U * part.abs() + 2 * U * (cdf + part.abs()) + 2 ** -126 * z.abs() + 1e-37
+    assert ((db.double() - (cdf + part)).abs() <= tol).all()
