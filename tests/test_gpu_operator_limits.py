@@ -239,3 +239,16 @@ def test_gelu_is_exact_relative_to_itself():
     part = z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
     tol = e_cdf + (8 + 2 * z * z) * U * part.abs() + 2 * U * (cdf + part.abs()) + 2 ** -126 * z.abs() + 1e-37
     assert ((db.double() - (cdf + part)).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_batches_of_small_graphs_in_the_root_mean_square(act):
+    """Graphs of a warp each.  An output carries about ten roundings, half a step each at most; the statistics' errors average out over
+    the 400 values or more of a group."""
+    sizes = torch.randint(25, 60, (1500,), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    ptr = torch.cat([sizes.new_zeros(1), sizes.cumsum(0)])
+    n = int(ptr[-1])
+    for f, groups in ((128, 8), (64, 1), (48, 3)):
+        x, dout = norm.rand(n, f, scale=2.0, mean=0.5), norm.rand(n, f, seed=1)
+        w, b = norm.rand(1, f, seed=2)[0].contiguous(), norm.rand(1, f, seed=3)[0].contiguous()
+        norm.both_ways(x, groups, w, b, ptr, act, dout, rms=True)
