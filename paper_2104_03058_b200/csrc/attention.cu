@@ -64,34 +64,32 @@ __device__ __forceinline__ float ex2(float x)
 // e^(s - m); m is -inf only where every score so far is
 __device__ __forceinline__ float weight(float s, float m) { return ex2((s - (m == -CUDART_INF_F ? 0.f : m)) * kLog2e); }
 
-// tanh, within 8 * 2^-24 of its value.  For |x| < 1/2 its series to x^13 (the next term is 9e-8 of the result at 1/2); from there on 1 - 2 / (1 + e^2|x|): the
-// quotient is below 0.54 and off by about 4 * 2^-24 of itself from the exponential, 2 from the reciprocal and the rest from roundings.  Scores that are
-// capped at a few tens lie mostly in the first part, where an absolute error would be as large as the score.  tanhf, which is within 2 ulp, branches, and took a
-// quarter of the forward walk's instructions.
+// tanh, within 8 * 2^-24 of its value.  For |x| < 1/2 its series to x^13 (the next term is 9e-8 of the result at 1/2); from there on tanh_rough,
+// 1 - 2 / (1 + e^2|x|): the quotient is below 0.54 and off by about 4 * 2^-24 of itself from the exponential, 2 from the reciprocal and the rest from
+// roundings.  Scores that are capped at a few tens lie mostly in the first part, where an absolute error would be as large as the score; a warp takes
+// the second part only if one of its scores needs it (training passes of 2 M entries of 8 x 16, cap 20: fp32 774 -> 754 us, bf16 497 -> 483; cap
+// 2, where most need it, 774 -> 776).  tanhf, which is within 2 ulp, branches, and took a quarter of the forward walk's instructions.
 //
 // ROUGH: the second part alone, within 8 * 2^-24 of 1, so the score is off by so much of the cap.  Only where nothing is left of that in what the call
 // gives: the forward pass of bf16 features into bf16, without the sums that a gradient would go on with, and caps up to kRoughCap, where a weight is
-// off by 2 * 3e-5 of itself, a sixtieth of the output's half step of 2^-8.  It saves 13 of the forward walk's instructions per entry and head.
+// off by 2 * 3e-5 of itself, a sixtieth of the output's half step of 2^-8 (39.6 M entries of 8 x 8, cap 30: 750 us, otherwise 789).
 constexpr float kRoughCap = 64.f;
 
-template <bool ROUGH>
-__device__ __forceinline__ float tanh_of(float x)
+__device__ __forceinline__ float tanh_rough(float x)
 {
-    if constexpr (ROUGH) {
-        float inv;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(x * (2.f * kLog2e))));
-        return fmaf(-2.f, inv, 1.f);
-    }
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(x * (2.f * kLog2e))));
+    return fmaf(-2.f, inv, 1.f);
+}
+__device__ __forceinline__ float tanh_series(float x)
+{
     const float x2 = x * x;
     float c = fmaf(x2, 21844.f / 6081075.f, -1382.f / 155925.f);
     c = fmaf(x2, c, 62.f / 2835.f);
     c = fmaf(x2, c, -17.f / 315.f);
     c = fmaf(x2, c, 2.f / 15.f);
     c = fmaf(x2, c, -1.f / 3.f);
-    const float series = fmaf(x * x2, c, x), size = fabsf(x);
-    float inv;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(1.f + ex2(size * (2.f * kLog2e))));
-    return size < 0.5f ? series : copysignf(fmaf(-2.f, inv, 1.f), x);
+    return fmaf(x * x2, c, x);
 }
 
 // (x, y) += (a, b) * (c, d)
@@ -332,11 +330,23 @@ __global__ void __launch_bounds__(kBlock, PASS == kForward ? 3 : 2) attend(const
                 slope[i] = 1.f;
             }
             if (capped) {
+                float t[UB];
+                [[maybe_unused]] bool far = false;
 #pragma unroll
                 for (int i = 0; i < UB; ++i) {
-                    const float t = tanh_of<ROUGH>(s[i] * a.inv_softcap);
-                    s[i] = a.softcap * t;
-                    slope[i] = fmaf(-t, t, 1.f);
+                    s[i] *= a.inv_softcap;
+                    t[i] = ROUGH ? tanh_rough(s[i]) : tanh_series(s[i]);
+                    far = far || !(fabsf(s[i]) < 0.5f);
+                }
+                if (!ROUGH && __any_sync(kFull, far)) {
+#pragma unroll
+                    for (int i = 0; i < UB; ++i)
+                        if (!(fabsf(s[i]) < 0.5f)) t[i] = copysignf(tanh_rough(fabsf(s[i])), s[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < UB; ++i) {
+                    s[i] = a.softcap * t[i];
+                    slope[i] = fmaf(-t[i], t[i], 1.f);
                 }
             }
             if (MASKED && with_bias) {
