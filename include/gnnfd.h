@@ -397,7 +397,8 @@ int gnnfd_aggregate_attention(const gnnfd_csr_t* csr, const void* d_q, int64_t l
  * d_dbias [buckets, heads] fp32.  csr_t: the CSR of the reversed edges, gnnfd_build_csr of the same edge list with d_src and d_dst exchanged and
  * the same flags; d_dist_t: the buckets in csr_t's slot order.  d_lse as written by the forward call with the same arguments.  Nothing is
  * added with atomics: gradients of vertices that many edges share are sums over the rows of csr_t.
- * d_scratch: gnnfd_attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets) bytes (buckets may be 0 there where d_dbias is NULL). */
+ * d_scratch: gnnfd_attention_backward_workspace_bytes(csr, csr_t, heads, dim, buckets) bytes (buckets may be 0 there where d_dbias is NULL;
+ * with it, nnz * heads floats of it and up to 740 * buckets * heads more). */
 int gnnfd_attention_backward_workspace_bytes(const gnnfd_csr_t* csr, const gnnfd_csr_t* csr_t, int32_t heads, int32_t dim, int32_t buckets,
                                              size_t* scratch_bytes);
 
@@ -418,7 +419,7 @@ int gnnfd_aggregate_attention_backward(const gnnfd_csr_t* csr, const gnnfd_csr_t
  * from 0; NULL: one graph of n rows (graphs = 1).  Rows behind the last offset are left as they are; graphs may be empty (mean 0,
  * rstd eps^-1/2).  Offsets outside [0, n] or not ascending are cut to what is inside: nothing outside of the arrays is touched.  d_weight, d_bias [f] fp32,
  * either may be NULL (1 and 0).  d_mean, d_rstd [graphs, groups] fp32 receive the statistics; both may be NULL.  f up to 8192.
- * Statistics, sums and the activation are fp32 or wider; the result is rounded once.  d_scratch:
+ * Statistics, sums and the activation are fp32 or wider, squares of distances from the mean included; the result is rounded once.  d_scratch:
  * gnnfd_group_norm_workspace_bytes(n, f, groups, graphs, 0) bytes, 256-byte aligned.  The call only enqueues work. */
 typedef enum {
     GNNFD_ACT_NONE = 0,
@@ -454,7 +455,7 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * *d_status (d_status may be NULL; the caller has set it to 0).
  *
  * gnnfd_embedding_backward: grad[r, :] = scale * sum of dout[i, :] over the i with ids[i] == r, for all vocab rows; rows that no id
- * names become 0.  Sums are fp32 in an order that depends on the ids alone: equal inputs give equal bits.  With accumulate != 0 the
+ * names become 0.  Sums are fp32 in an order that depends on the ids, the sizes, and the operands' alignment and pitches: equal calls give equal bits.  With accumulate != 0 the
  * sums are added to what d_grad holds (of type gdt, rounded once) and rows that no id names are left as they are.  Ids equal to `padding`
  * (-1: none) take no part: their row is treated as one that no id names.  Ids outside [0, vocab) take no part and set bit 0 of *d_status;
  * bit 1 is set if a block of the sort gave up waiting for another one (grad is then incomplete).  d_dout [n, ldd] of type ddt;

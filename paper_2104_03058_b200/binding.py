@@ -1038,7 +1038,8 @@ def embedding_backward(ids: torch.Tensor, dout: torch.Tensor, vocab: int, scale:
                        accumulate: bool = False, f: int | None = None, out: torch.Tensor | None = None, out_dtype=None, scratch=None,
                        status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """gnnfd_embedding_backward: the gradient [vocab, f] of a table from the gradients of the rows looked up.  ``accumulate`` adds to
-    ``out`` (which must then be given); ids equal to ``padding_idx`` take no part; ``status``: see the header."""
+    ``out`` (which must then be given); ids equal to ``padding_idx`` take no part (a negative one is no row of the table: none, not one
+    counted from the end); ``status``: see the header."""
     index = dout.get_device()
     if index >= 0 and index != _current_device():
         return _elsewhere(dout.device, stream, embedding_backward, ids, dout, vocab, scale, padding_idx, accumulate, f, out, out_dtype, scratch,

@@ -671,6 +671,8 @@ static int launch_attend(const char* name, const char* reduce_name, const gnnfd_
     a.out_vec_ok = a.dim % 4 == 0 && out_bits % (4 * osize) == 0;
     const int lpr = 1 << a.lpr_log2, words = L.elems * size / 4;
     const int per_step = (words == 8 ? in_flight<8>() : in_flight<4>()) * (32 / lpr);
+    // (blocks per SM counted as the gradients' two in the forward pass as well, which has three: counted as three, eight graphs of 40,000 to 2 M entries
+    // were within 3 % either way)
     const int64_t limit = walk_limit(csr, per_step, a.n_htiles, 16, 2);
     const int64_t blocks = plan_ranges(csr, gather_groups(), lpr, per_step, limit, a.range, &a.n_ranges);
     const int64_t grid_x = blocks * a.n_htiles;

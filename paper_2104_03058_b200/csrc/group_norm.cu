@@ -1162,7 +1162,10 @@ static NormPlan plan_norm(int64_t n, int32_t f, int32_t groups, int64_t graphs)
     p.inst = groups == f;
     const int lanes = (f + 3) / 4 < kNormBlock ? (f + 3) / 4 : kNormBlock;
     const int batch = kNormBlock / lanes * 4;                          // four rows a thread
-    // Warps take the graphs of up to kSmallRows rows of a batch that has enough of them to fill the chip, and whose average graph is well below.
+    // Warps take the graphs of up to kSmallRows rows of a batch that has enough of them to fill the chip, and whose average graph is well below.  128 bf16
+    // columns in 8 groups, warps against slabs: 600 graphs of 25 rows 18 us against 38, 6000 of 64 77 against 158; where a fifth of the graphs is longer than
+    // kSmallRows, so that both run, 6000 of 100 rows 210 against 189.  Fewer graphs would gain from warps as well (100 of 25 rows 18 against 25, 300 of 64 25
+    // against 30, gradients 35 against 27 and 41 against 39): for a forward pass alone the border is drawn high.
     p.small_rows = graphs >= 4 * kNormSms && n <= graphs * (kSmallRows / 2) ? kSmallRows : -1;
     // Slabs of whole batches: about six slabs per SM, so that a block's fixed costs (the search for its graph, the meetings of its threads) are small
     // beside its rows, up to 512 rows a slab (see kShiftRows) and from one batch up.  Sixteen per SM: gradients of 133 k x 256 bf16 137 us, six 109.  Beside small
