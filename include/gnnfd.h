@@ -445,6 +445,87 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
                               const float* d_bias, const float* d_mean, const float* d_rstd, int activation, void* d_dx, int64_t lddx,
                               gnnfd_dtype_t gdt, float* d_dweight, float* d_dbias, void* d_scratch, size_t scratch_bytes, void* stream);
 
+/* ------------------------------------------------------------------ layer norm
+ *
+ * Every row by itself, where gnnfd_group_norm takes the rows of a graph together: a vertex's result does not depend on the vertices beside
+ * it, nor a token's on its batch.  (Like that call a step between layers, which the paper leaves to the user.)  Over the f columns of a row
+ *   out = (x - mean) * rstd * weight + bias,   rstd = (variance + eps)^-1/2  (not corrected)
+ * d_x [n, ldx] of type xdt, d_out [n, ldo] of type odt (may be d_x itself, with ldo = ldx and odt = xdt).  d_weight, d_bias [f] fp32, either may be NULL (1 and 0).
+ * d_mean, d_rstd [n] fp32 receive the statistics; both may be NULL.  f up to 8192.  Sums and statistics are fp32, the variance is the mean of squared
+ * distances from the mean; the result is rounded once.  Rows that hold an infinity or NaN give NaN, others are not touched by them.
+ *
+ * gnnfd_layer_norm_backward: for d_dout [n, ldd] of type xdt, d_dx [n, lddx] of type gdt (may be d_dout itself: same pitch and type) and d_dweight,
+ * d_dbias [f] fp32, sums over all rows (both NULL: not wanted; d_scratch may then be NULL).  d_mean, d_rstd as the forward call gave them.  d_scratch:
+ * gnnfd_layer_norm_backward_workspace_bytes(n, f) bytes, 256-byte aligned.  The calls only enqueue work. */
+int gnnfd_layer_norm(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f, const float* d_weight, const float* d_bias,
+                     float eps, void* d_out, int64_t ldo, gnnfd_dtype_t odt, float* d_mean, float* d_rstd, void* stream);
+
+int gnnfd_layer_norm_backward_workspace_bytes(int64_t n, int32_t f, size_t* scratch_bytes);
+
+int gnnfd_layer_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f,
+                              const float* d_weight, const float* d_mean, const float* d_rstd, void* d_dx, int64_t lddx, gnnfd_dtype_t gdt,
+                              float* d_dweight, float* d_dbias, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* ------------------------------------------------------------------ rotary positions
+ *
+ * Ahead of gnnfd_aggregate_attention: queries and keys are turned by angles that grow with their vertices' positions (in a document, along a
+ * path), so that a score depends on how far apart the positions are.  (The paper's models know no positions.)  In each of `heads` heads of `dim` columns the first rotary_dim
+ * columns (even, up to dim, up to 4096) are turned in pairs,
+ *   angle = position[row] * freq[i],   (u, v) -> scale * (u cos(angle) - v sin(angle), u sin(angle) + v cos(angle)),   i < rotary_dim / 2
+ * with (u, v) the columns (i, i + rotary_dim / 2) of the head or, with interleaved != 0, (2 i, 2 i + 1).  The other columns are copied.  inverse != 0 turns by the
+ * opposite angle (the scale stays): this is the gradient, out's for x's.  A matrix that holds queries, keys and values side by side is turned in one call: `heads` counts
+ * those of the queries and keys, and ldx goes on to the values.
+ * d_positions [n] of type itype, any value (fractions of a turn are exact to 2^-52 of the angle); NULL: the row's number.  d_freq [rotary_dim / 2] fp64, radians per position:
+ * gnnfd_rotary_frequencies or any other.  d_x [n, ldx] of type xdt, d_out [n, ldo] of type odt (d_x itself with ldo = ldx and odt = xdt; columns of
+ * heads that are not turned and columns past heads * dim then stay as they are).  fp32 arithmetic on cosines and sines within 2 * 2^-24; one rounding at the end.
+ * GNNFD_TOO_LARGE: more than 2^20 columns.  The call only enqueues work.
+ *
+ * gnnfd_rotary_frequencies (host memory, no device): freq[i] = base^(-2 i / rotary_dim), for contexts beyond the length that a model was trained on
+ *   GNNFD_ROTARY_POSITION  divided by factor (positions are squeezed),
+ *   GNNFD_ROTARY_BASE      with base * factor^(rotary_dim / (rotary_dim - 2)): the last frequency is divided by factor, the first stays (rotary_dim > 2),
+ *   GNNFD_ROTARY_RAMP      divided by factor where a frequency makes fewer than low_turns turns over `length` positions, kept where it makes more than
+ *                          high_turns, in between kept * freq + (1 - kept) * freq / factor with kept = (turns - low_turns) / (high_turns - low_turns). */
+typedef enum { GNNFD_ROTARY_NONE = 0, GNNFD_ROTARY_POSITION = 1, GNNFD_ROTARY_BASE = 2, GNNFD_ROTARY_RAMP = 3 } gnnfd_rotary_scaling_t;
+
+int gnnfd_rotary_frequencies(int32_t rotary_dim, double base, int scaling, double factor, int64_t length, double low_turns, double high_turns,
+                             double* freq);
+
+int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t heads, int32_t dim, int32_t rotary_dim, int interleaved,
+                 const void* d_positions, gnnfd_itype_t itype, const double* d_freq, float scale, int inverse, void* d_out, int64_t ldo,
+                 gnnfd_dtype_t odt, void* stream);
+
+/* ------------------------------------------------------------------ gated linear recurrence over the rows of a graph
+ *
+ * A mixer of linear cost beside the attention, for vertices that have an order (the tokens of a document, a walk): every column keeps a state that decays by a
+ * gate of its own from row to row.  (An aggregation over the rows ahead with weights that are products of gates; not in the paper.)  Per column
+ *   h[t] = a[t] * h[t - 1] + b[t],   out[t] = h[t]        GNNFD_GATE_FACTOR: a = gate, b = x (gates of -1 to 1 are meant)
+ *                                                         GNNFD_GATE_SIGMOID: a = 1 / (1 + e^-gate), b = (1 - a) * x
+ * Rows graph_ptr[b] .. graph_ptr[b + 1] - 1 are graph b, in order; its first row's h[t - 1] is d_initial[b] (fp32 [graphs, f]; NULL: 0).  d_graph_ptr [graphs + 1]
+ * of type itype, ascending from 0; NULL: graphs of n / graphs rows each (n must be a multiple), so graphs = n is one token for each of n sequences.  Rows
+ * behind the last offset are left as they are; graphs may be empty (their last state is the first one).  Offsets outside [0, n] or not ascending are cut to what is
+ * inside: nothing outside of the arrays is touched.  d_x, d_gate [n, ld] of type dt, d_out [n, ldo] of type odt, not overlapping them.  d_final (fp32
+ * [graphs, f], may be NULL) receives the last state of each graph; it may be d_initial itself where graphs = n and d_graph_ptr is NULL, and does not overlap it otherwise.  d_states
+ * (may be NULL): fp32 [(n + 15) / 16, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
+ * d_scratch: gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, d_graph_ptr == NULL, 0) bytes, 256-byte aligned (0 and NULL for few rows).
+ *
+ * gnnfd_linear_recurrence_backward: for d_dout [n, ldd] of type dt and d_dfinal (fp32 [graphs, f]; NULL: 0), the gradients of out and the last states, d_dx and
+ * d_dgate [n, ld*] of type gdt and d_dinitial (fp32 [graphs, f]; NULL: not wanted).  d_states as written by the forward call with the same arguments.  Rows
+ * behind the last offset are left as they are.  Scratch: the same query with backward = 1.
+ * GNNFD_TOO_LARGE: more than 2^31 - 65536 rows or 2^20 columns.  The calls only enqueue work. */
+typedef enum { GNNFD_GATE_FACTOR = 0, GNNFD_GATE_SIGMOID = 1 } gnnfd_gate_t;
+
+int gnnfd_linear_recurrence_workspace_bytes(int64_t n, int32_t f, int64_t graphs, int equal_lengths, int backward, size_t* scratch_bytes);
+
+int gnnfd_linear_recurrence(int64_t n, const void* d_x, int64_t ldx, const void* d_gate, int64_t ldg, gnnfd_dtype_t dt, int32_t f, int form,
+                            int64_t graphs, const void* d_graph_ptr, gnnfd_itype_t itype, const float* d_initial, void* d_out, int64_t ldo,
+                            gnnfd_dtype_t odt, float* d_final, float* d_states, void* d_scratch, size_t scratch_bytes, void* stream);
+
+int gnnfd_linear_recurrence_backward(int64_t n, const void* d_dout, int64_t ldd, const void* d_x, int64_t ldx, const void* d_gate, int64_t ldg,
+                                     gnnfd_dtype_t dt, int32_t f, int form, int64_t graphs, const void* d_graph_ptr, gnnfd_itype_t itype,
+                                     const float* d_initial, const float* d_states, const float* d_dfinal, void* d_dx, int64_t lddx,
+                                     void* d_dgate, int64_t lddg, gnnfd_dtype_t gdt, float* d_dinitial, void* d_scratch, size_t scratch_bytes,
+                                     void* stream);
+
 /* ------------------------------------------------------------------ learned vertex features
  *
  * For graphs whose vertices have no features of their own (or a type, a degree, a name instead): a table with a learned row per

@@ -20,6 +20,9 @@ OK, INVALID_ARG, BAD_INDEX, TOO_LARGE, WORKSPACE_TOO_SMALL, UNSUPPORTED, CUDA_ER
 STATIC_SCRATCH_EXCEEDED = -7
 COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
+ROTARY_SCALINGS = {"none": 0, "position": 1, "base": 2, "ramp": 3}
+GATES = {"factor": 0, "sigmoid": 1}
+STATE_ROWS = 16
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056
@@ -95,6 +98,15 @@ def lib() -> ctypes.CDLL:
         L.gnnfd_group_norm.argtypes = [i64, vp, i64, i32, i32, i32, i64, vp, i32, vp, vp, fl, ctypes.c_int, vp, i64, i32, vp, vp, vp, sz, vp]
         L.gnnfd_group_norm_backward.argtypes = [i64, vp, i64, vp, i64, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, ctypes.c_int, vp, i64,
                                                 i32, vp, vp, vp, sz, vp]
+        L.gnnfd_layer_norm.argtypes = [i64, vp, i64, i32, i32, vp, vp, fl, vp, i64, i32, vp, vp, vp]
+        L.gnnfd_layer_norm_backward_workspace_bytes.argtypes = [i64, i32, pp(sz)]
+        L.gnnfd_layer_norm_backward.argtypes = [i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.gnnfd_rotary_frequencies.argtypes = [i32, ctypes.c_double, ctypes.c_int, ctypes.c_double, i64, ctypes.c_double, ctypes.c_double, vp]
+        L.gnnfd_rotary.argtypes = [i64, vp, i64, i32, i32, i32, i32, ctypes.c_int, vp, i32, vp, fl, ctypes.c_int, vp, i64, i32, vp]
+        L.gnnfd_linear_recurrence_workspace_bytes.argtypes = [i64, i32, i64, ctypes.c_int, ctypes.c_int, pp(sz)]
+        L.gnnfd_linear_recurrence.argtypes = [i64, vp, i64, vp, i64, i32, i32, ctypes.c_int, i64, vp, i32, vp, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.gnnfd_linear_recurrence_backward.argtypes = [i64, vp, i64, vp, i64, vp, i64, i32, i32, ctypes.c_int, i64, vp, i32, vp, vp, vp, vp, i64,
+                                                       vp, i64, i32, vp, vp, sz, vp]
         L.gnnfd_embedding.argtypes = [i64, vp, i32, i64, vp, i64, i32, i32, fl, vp, i64, i32, vp, vp]
         L.gnnfd_embedding_backward_workspace_bytes.argtypes = [i64, i64, i32, pp(sz)]
         L.gnnfd_embedding_backward.argtypes = [i64, vp, i32, vp, i64, i32, i64, i32, fl, i64, ctypes.c_int, vp, i64, i32, vp, sz, vp, vp]
@@ -994,6 +1006,247 @@ def group_norm_backward(dout: torch.Tensor, x: torch.Tensor, groups: int, mean: 
     _check(lib().gnnfd_group_norm_backward(n, dp, ldd, xp, ldx, xdt, f, groups, graphs, pp, itype, wp, bp, mean.data_ptr(), rstd.data_ptr(), act,
                                            op, ldo, odt, dwp, dbp, scr, scr_n, _stream_handle(index, stream)), "gnnfd_group_norm_backward")
     return out, dweight, dbias
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5, f: int | None = None,
+               out: torch.Tensor | None = None, out_dtype=None, with_stats: bool = False, stream=None):
+    """gnnfd_layer_norm: every row of x by itself normalised over its columns, scaled and shifted.  ``out`` may be x itself.  With
+    ``with_stats`` the call returns (out, mean, rstd), each [n], for layer_norm_backward."""
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, layer_norm, x, weight, bias, eps, f, out, out_dtype, with_stats)
+    n, width = x.shape
+    f = width if f is None else f
+    xp, ldx = _matrix(x, f, "x")
+    wp, bp = _column_values(x, f, "weight", weight), _column_values(x, f, "bias", bias)
+    if out is None:
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        if not _same_place(x, out):
+            _no_overlap(x, out, "x", "out")
+    op, ldo = _matrix(out, f, "out")
+    mean = rstd = mp = rp = None
+    if with_stats:
+        mean, rstd = _new(x, (2, n), torch.float32, stream)
+        mp, rp = mean.data_ptr(), rstd.data_ptr()
+    _check(lib().gnnfd_layer_norm(n, xp, ldx, _dtype_code(x), f, wp, bp, eps, op, ldo, _dtype_code(out), mp, rp, _stream_handle(index, stream)),
+           "gnnfd_layer_norm")
+    return (out, mean, rstd) if with_stats else out
+
+
+def _column_values(x, f: int, name: str, t):
+    """Pointer of a row of f fp32 values beside x, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != f or not t.is_contiguous() or t.device != x.device:
+        raise ValueError("%s must be a contiguous float32 tensor of %d values on %s" % (name, f, x.device))
+    return t.data_ptr()
+
+
+def layer_norm_backward_workspace_bytes(n: int, f: int) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_layer_norm_backward_workspace_bytes(n, f, ctypes.byref(s)), "gnnfd_layer_norm_backward_workspace_bytes")
+    return s.value
+
+
+def layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None,
+                        f: int | None = None, out: torch.Tensor | None = None, out_dtype=None, with_params: bool = True, scratch=None, stream=None):
+    """gnnfd_layer_norm_backward: (dx, dweight, dbias) for the gradient ``dout`` of layer_norm's result, of the type of x; dweight and dbias
+    are None where ``with_params`` is false.  ``mean`` and ``rstd`` are what the forward call returned; ``out`` receives dx and may be dout itself."""
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, layer_norm_backward, dout, x, mean, rstd, weight, f, out, out_dtype, with_params, scratch)
+    n, width = x.shape
+    f = width if f is None else f
+    xp, ldx = _matrix(x, f, "x")
+    dp, ldd = _matrix(dout, f, "dout")
+    if dout.dtype != x.dtype:
+        raise TypeError("dout must have the dtype of x")
+    _need_rows_of(dout, n, "dout")
+    _same_device(x.device, dout=dout)
+    wp = _column_values(x, f, "weight", weight)
+    mp, rp = _column_values(x, n, "mean", mean), _column_values(x, n, "rstd", rstd)
+    if out is None:
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        _no_overlap(x, out, "x", "out")
+        if not _same_place(dout, out):
+            _no_overlap(dout, out, "dout", "out")
+    op, ldo = _matrix(out, f, "out")
+    dweight = dbias = dwp = dbp = None
+    if with_params:
+        dweight, dbias = _new(x, (2, f), torch.float32, stream)
+        dwp, dbp = dweight.data_ptr(), dbias.data_ptr()
+        if scratch is None and n:
+            scratch = _new(x, layer_norm_backward_workspace_bytes(n, f), torch.uint8, stream)
+    scr, scr_n = _scratch_args(scratch, x.device)
+    _check(lib().gnnfd_layer_norm_backward(n, dp, ldd, xp, ldx, _dtype_code(x), f, wp, mp, rp, op, ldo, _dtype_code(out), dwp, dbp, scr, scr_n,
+                                           _stream_handle(index, stream)), "gnnfd_layer_norm_backward")
+    return out, dweight, dbias
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, length: int = 0, turns=(1.0, 32.0),
+                       device="cuda") -> torch.Tensor:
+    """gnnfd_rotary_frequencies: float64 [rotary_dim / 2] radians per position for rotary, made once.  ``scaling`` ("none", "position", "base",
+    "ramp") stretches contexts beyond ``length`` positions by ``factor``; "ramp" keeps frequencies of more than turns[1] turns over ``length``
+    and divides those of fewer than turns[0]."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError("scaling must be one of %s" % ", ".join(ROTARY_SCALINGS))
+    freq = torch.empty(max(0, rotary_dim) // 2, dtype=torch.float64)
+    _check(lib().gnnfd_rotary_frequencies(rotary_dim, base, ROTARY_SCALINGS[scaling], factor, length, turns[0], turns[1], freq.data_ptr()),
+           "gnnfd_rotary_frequencies")
+    return freq.to(device)
+
+
+def rotary(x: torch.Tensor, freq: torch.Tensor, heads: int, dim: int, positions: torch.Tensor | None = None, interleaved: bool = False,
+           scale: float = 1.0, inverse: bool = False, out: torch.Tensor | None = None, out_dtype=None, stream=None) -> torch.Tensor:
+    """gnnfd_rotary: the first 2 * len(freq) columns of each of ``heads`` heads of ``dim`` columns turned in pairs by positions[row] * freq
+    (``positions`` None: the row's number), halves of the head against each other or ``interleaved`` neighbours.  ``inverse`` turns back: the
+    gradient of x for that of the result.  ``out`` may be x itself; other columns than those of the heads then stay as they are."""
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, rotary, x, freq, heads, dim, positions, interleaved, scale, inverse, out, out_dtype)
+    f = heads * dim
+    xp, ldx = _matrix(x, f, "x")
+    n = x.shape[0]
+    if freq.dtype != torch.float64 or freq.dim() != 1 or freq.device != x.device or not freq.is_contiguous():
+        raise ValueError("freq must be a contiguous float64 tensor on %s" % x.device)
+    if not 0 < 2 * freq.shape[0] <= dim:
+        raise ValueError("%d frequencies do not fit heads of %d columns" % (freq.shape[0], dim))
+    pp, itype = None, I32
+    if positions is not None:
+        pp, count, itype = _index_list(positions, "positions")
+        if count != n or positions.device != x.device:
+            raise ValueError("positions must hold a position for each of the %d rows, on %s" % (n, x.device))
+    if out is None:
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        if not _same_place(x, out):
+            _no_overlap(x, out, "x", "out")
+    op, ldo = _matrix(out, f, "out")
+    _check(lib().gnnfd_rotary(n, xp, ldx, _dtype_code(x), heads, dim, 2 * freq.shape[0], int(interleaved), pp, itype, freq.data_ptr(), scale,
+                              int(inverse), op, ldo, _dtype_code(out), _stream_handle(index, stream)), "gnnfd_rotary")
+    return out
+
+
+def linear_recurrence_workspace_bytes(n: int, f: int, graphs: int = 1, equal_lengths: bool = False, backward: bool = False) -> int:
+    s = ctypes.c_size_t()
+    _check(lib().gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, int(equal_lengths), int(backward), ctypes.byref(s)),
+           "gnnfd_linear_recurrence_workspace_bytes")
+    return s.value
+
+
+def _recurrence_operands(x, gate, form: str, graph_ptr, graphs: int, f: int, **states):
+    """(pointer of x, pitch, pointer of the gates, pitch, form, graphs, offsets pointer, offsets type, pointers of the [graphs, f] states)"""
+    xp, ldx = _matrix(x, f, "x")
+    gp, ldg = _matrix(gate, f, "gate")
+    if gate.dtype != x.dtype:
+        raise TypeError("gate must have the dtype of x")
+    if gate.device != x.device:
+        _same_device(x.device, gate=gate)
+    n = x.shape[0]
+    _need_rows_of(gate, n, "gate")
+    if form not in GATES:
+        raise ValueError("form must be one of %s" % ", ".join(GATES))
+    pp, itype = None, I32
+    if graph_ptr is not None:
+        pp, count, itype = _index_list(graph_ptr, "graph_ptr")
+        if count < 2 or graph_ptr.device != x.device:
+            raise ValueError("graph_ptr must hold graphs + 1 >= 2 offsets on %s" % x.device)
+        if graphs is not None and graphs != count - 1:
+            raise ValueError("graph_ptr holds the offsets of %d graphs, not of %d" % (count - 1, graphs))
+        graphs = count - 1
+    else:
+        graphs = 1 if graphs is None else graphs
+        if graphs < 1 or n % graphs:
+            raise ValueError("%d rows do not make %d graphs of one length" % (n, graphs))
+    pointers = []
+    for name, t in states.items():
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (graphs, f) or not t.is_contiguous() or t.device != x.device):
+            raise ValueError("%s must be a contiguous float32 [graphs = %d, %d] tensor on %s" % (name, graphs, f, x.device))
+        pointers.append(None if t is None else t.data_ptr())
+    return xp, ldx, gp, ldg, GATES[form], graphs, pp, itype, pointers
+
+
+def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid", graph_ptr: torch.Tensor | None = None, graphs: int | None = None,
+                      initial: torch.Tensor | None = None, f: int | None = None, out: torch.Tensor | None = None, out_dtype=None,
+                      final: torch.Tensor | None = None, with_final: bool = False, with_states: bool = False, scratch=None, stream=None):
+    """gnnfd_linear_recurrence: h[t] = a[t] h[t - 1] + b[t] down the rows of each graph of a batch, per column; ``form`` "factor": a = gate,
+    b = x, "sigmoid": a = 1 / (1 + exp(-gate)), b = (1 - a) x.  ``graph_ptr`` [graphs + 1] holds the graphs' row offsets; without it the rows are
+    ``graphs`` (1) graphs of one length, so graphs = n is a single token for each of n sequences.  ``initial`` [graphs, f]: states ahead of the
+    first rows.  Rows behind the last offset keep what ``out`` holds (undefined where the call allocates it).  Returns out, with ``with_final`` or
+    ``final`` (filled; for single tokens it may be ``initial``) also the last states, with ``with_states`` also what linear_recurrence_backward takes."""
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, linear_recurrence, x, gate, form, graph_ptr, graphs, initial, f, out, out_dtype, final, with_final,
+                          with_states, scratch)
+    n, width = x.shape
+    f = width if f is None else f
+    xp, ldx, gp, ldg, code, graphs, pp, itype, (ip, fp) = _recurrence_operands(x, gate, form, graph_ptr, graphs, f, initial=initial, final=final)
+    if out is None:
+        out = _new(x, (n, f), out_dtype or torch.float32, stream)
+    else:
+        _same_device(x.device, out=out)
+        _need_rows_of(out, n, "out")
+        _no_overlap(x, out, "x", "out")
+        _no_overlap(gate, out, "gate", "out")
+    op, ldo = _matrix(out, f, "out")
+    if final is not None:
+        if initial is not None and not (ip == fp and graph_ptr is None and graphs == n):
+            _no_overlap(initial, final, "initial", "final")
+        for name, t in (("x", x), ("gate", gate), ("out", out)):
+            _no_overlap(t, final, name, "final")
+    elif with_final:
+        final = _new(x, (graphs, f), torch.float32, stream)
+        fp = final.data_ptr()
+    states = _new(x, (-(-n // STATE_ROWS), f), torch.float32, stream) if with_states else None
+    if scratch is None:
+        need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None)
+        scratch = _new(x, need, torch.uint8, stream) if need else None
+    scr, scr_n = _scratch_args(scratch, x.device)
+    _check(lib().gnnfd_linear_recurrence(n, xp, ldx, gp, ldg, _dtype_code(x), f, code, graphs, pp, itype, ip, op, ldo, _dtype_code(out), fp,
+                                         states.data_ptr() if with_states else None, scr, scr_n, _stream_handle(index, stream)),
+           "gnnfd_linear_recurrence")
+    got = [out] + ([final] if final is not None else []) + ([states] if with_states else [])
+    return tuple(got) if len(got) > 1 else out
+
+
+def linear_recurrence_backward(dout: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, states: torch.Tensor, form: str = "sigmoid",
+                               graph_ptr: torch.Tensor | None = None, graphs: int | None = None, initial: torch.Tensor | None = None,
+                               dfinal: torch.Tensor | None = None, f: int | None = None, out_dtype=None, scratch=None, stream=None):
+    """gnnfd_linear_recurrence_backward: (dx, dgate, dinitial) for the gradients ``dout`` of linear_recurrence's result, of the type of x, and
+    ``dfinal`` of its last states; dinitial is None where there was no ``initial``.  ``states`` is what the forward call with the same arguments returned."""
+    index = x.get_device()
+    if index >= 0 and index != _current_device():
+        return _elsewhere(x.device, stream, linear_recurrence_backward, dout, x, gate, states, form, graph_ptr, graphs, initial, dfinal, f,
+                          out_dtype, scratch)
+    n, width = x.shape
+    f = width if f is None else f
+    xp, ldx, gp, ldg, code, graphs, pp, itype, (ip, dfp) = _recurrence_operands(x, gate, form, graph_ptr, graphs, f, initial=initial, dfinal=dfinal)
+    dp, ldd = _matrix(dout, f, "dout")
+    if dout.dtype != x.dtype:
+        raise TypeError("dout must have the dtype of x")
+    _same_device(x.device, dout=dout)
+    _need_rows_of(dout, n, "dout")
+    if states.dtype != torch.float32 or tuple(states.shape) != (-(-n // STATE_ROWS), f) or not states.is_contiguous() or states.device != x.device:
+        raise ValueError("states must be the contiguous float32 [%d, %d] tensor of the forward call, on %s" % (-(-n // STATE_ROWS), f, x.device))
+    dx, dgate = (_new(x, (n, f), out_dtype or torch.float32, stream) for _ in range(2))
+    dinitial = _new(x, (graphs, f), torch.float32, stream) if initial is not None else None
+    if scratch is None:
+        need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None, True)
+        scratch = _new(x, need, torch.uint8, stream) if need else None
+    scr, scr_n = _scratch_args(scratch, x.device)
+    _check(lib().gnnfd_linear_recurrence_backward(
+        n, dp, ldd, xp, ldx, gp, ldg, _dtype_code(x), f, code, graphs, pp, itype, ip, states.data_ptr(), dfp, dx.data_ptr(), f, dgate.data_ptr(), f,
+        _dtype_code(dx), None if dinitial is None else dinitial.data_ptr(), scr, scr_n, _stream_handle(index, stream)),
+        "gnnfd_linear_recurrence_backward")
+    return dx, dgate, dinitial
 
 
 def embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, f: int | None = None, out: torch.Tensor | None = None,

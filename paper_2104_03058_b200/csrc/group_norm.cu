@@ -1286,18 +1286,6 @@ static int launch_apply(NormArgs& a, bool grad, cudaStream_t s)
     return GNNFD_OK;
 }
 
-// f(elements per vector) for the widths there are; TI: float or __nv_bfloat16
-template <typename TI, typename F>
-static int with_vector(int v, F f)
-{
-    switch (v) {
-        case 8: if constexpr (sizeof(TI) == 2) return f(std::integral_constant<int, 8>());
-        case 4: return f(std::integral_constant<int, 4>());
-        case 2: return f(std::integral_constant<int, 2>());
-        default: return f(std::integral_constant<int, 1>());
-    }
-}
-
 template <typename TI>
 static int run_norm(NormArgs& a, int sums, int apply, bool inst, bool grad, cudaStream_t s)
 {

@@ -2,6 +2,8 @@
 // vector is inside the row.
 #pragma once
 
+#include <type_traits>
+
 #include "vec.cuh"
 
 namespace gnnfd {
@@ -25,6 +27,11 @@ struct Raw {
             asm("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
             w[0] = h;
         }
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < (kBytes < 4 ? 1 : kBytes / 4); ++i) w[i] = 0u;
     }
     __device__ __forceinline__ void get(float (&x)[V]) const
     {
@@ -77,6 +84,14 @@ __device__ __forceinline__ void store_packed(T* p, const float (&x)[V])
     }
 }
 
+// a vector into fp32 or bf16, as the flag says
+template <int V>
+__device__ __forceinline__ void store_row(void* out, int bf16, int64_t at, const float (&x)[V])
+{
+    if (bf16) store_packed<__nv_bfloat16, V>(static_cast<__nv_bfloat16*>(out) + at, x);
+    else store_packed<float, V>(static_cast<float*>(out) + at, x);
+}
+
 // the same where the row may end inside the vector (`left` columns from its first element on); columns past the end read as 0
 template <typename T, int V>
 __device__ __forceinline__ void load_row(const T* p, int left, float (&x)[V])
@@ -92,4 +107,26 @@ __device__ __forceinline__ void load_row(const T* p, int left, float (&x)[V])
         x[i] = one[0];
     }
 }
+
+// ---- host side
+
+// whether rows of elements of `size` bytes, `ld` apart, can be read and written in vectors of v elements (accesses have 16 bytes at most)
+inline bool rows_fit(const void* p, int64_t ld, int size, int v)
+{
+    const int bytes = v * size < 16 ? v * size : 16;
+    return (uintptr_t)p % bytes == 0 && ld * size % bytes == 0;
+}
+
+// f(elements per vector) for the widths there are; TI: float or __nv_bfloat16
+template <typename TI, typename F>
+inline int with_vector(int v, F f)
+{
+    switch (v) {
+        case 8: if constexpr (sizeof(TI) == 2) return f(std::integral_constant<int, 8>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 2: return f(std::integral_constant<int, 2>());
+        default: return f(std::integral_constant<int, 1>());
+    }
+}
+
 }  // namespace gnnfd
