@@ -95,6 +95,14 @@ inline void launch_early(void (*kernel)(Params...), dim3 grid, dim3 block, size_
     cudaLaunchKernelEx(&config, kernel, std::forward<Args>(args)...);      // errors are picked up by cudaGetLastError
 }
 
+// Blocks of a kernel that an SM has room for: of kernels whose blocks stay and take work in turn as many are launched as the chip holds, once found out.
+template <typename... Params>
+inline int blocks_per_sm(void (*kernel)(Params...), int threads, size_t smem)
+{
+    int blocks = 0;
+    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, smem) == cudaSuccess && blocks > 0 ? blocks : 1;
+}
+
 template <bool LET_NEXT_START>
 __device__ __forceinline__ void grid_dependency()
 {

@@ -68,78 +68,6 @@ __device__ __forceinline__ float reciprocal_fast(float x)             // 1 ulp; 
 }
 constexpr float kL2e = 1.4426950408889634f;
 
-// Two neighbouring elements in one instruction (the same roundings as one by one): x * m + c.
-__device__ __forceinline__ void scale_shift_pair(float& x, float& y, float m, float n, float c, float d)
-{
-    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%0, %1};\n\t"
-        "fma.rn.f32x2 r, r, p, q;\n\tmov.b64 {%0, %1}, r;\n\t}" : "+f"(x), "+f"(y) : "f"(m), "f"(n), "f"(c), "f"(d));
-}
-// (x, y) += (a, b) * (c, d)
-__device__ __forceinline__ void fma_pairs(float& x, float& y, float a, float b, float c, float d)
-{
-    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%0, %1};\n\t"
-        "fma.rn.f32x2 r, p, q, r;\n\tmov.b64 {%0, %1}, r;\n\t}" : "+f"(x), "+f"(y) : "f"(a), "f"(b), "f"(c), "f"(d));
-}
-// x[i] += c[i], x[i] = x[i] * m[i] + c[i], x[i] *= m[i] and s[i] += x[i] * y[i]; CS: one c for all
-template <int V, int CS>
-__device__ __forceinline__ void add_minus(float (&x)[V], const float (&c)[CS])
-{
-    if constexpr (V == 1) x[0] -= c[0];
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) add_pair(x[i], x[i + 1], -c[CS == 1 ? 0 : i], -c[CS == 1 ? 0 : i + 1]);
-}
-template <int V>
-__device__ __forceinline__ void add_all(float (&s)[V], const float (&x)[V])
-{
-    if constexpr (V == 1) s[0] += x[0];
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) add_pair(s[i], s[i + 1], x[i], x[i + 1]);
-}
-template <int V>
-__device__ __forceinline__ void scale_shift(float (&x)[V], const float (&m)[V], const float (&c)[V])
-{
-    if constexpr (V == 1) x[0] = fmaf(x[0], m[0], c[0]);
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) scale_shift_pair(x[i], x[i + 1], m[i], m[i + 1], c[i], c[i + 1]);
-}
-template <int V>
-__device__ __forceinline__ void multiply(float (&x)[V], const float (&m)[V])
-{
-    if constexpr (V == 1) x[0] *= m[0];
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) mul_pair(x[i], x[i + 1], m[i], m[i + 1]);
-}
-template <int V>
-__device__ __forceinline__ void add_products(float (&s)[V], const float (&x)[V], const float (&y)[V])
-{
-    if constexpr (V == 1) s[0] = fmaf(x[0], y[0], s[0]);
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) fma_pairs(s[i], s[i + 1], x[i], x[i + 1], y[i], y[i + 1]);
-}
-
-// x[i] = m * x[i], x[i] = m * x[i] + c for constants
-template <int V>
-__device__ __forceinline__ void scale(float (&x)[V], float m)
-{
-    if constexpr (V == 1) x[0] *= m;
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) mul_pair(x[i], x[i + 1], m, m);
-}
-template <int V>
-__device__ __forceinline__ void scale_shift(float (&x)[V], float m, float c)
-{
-    if constexpr (V == 1) x[0] = fmaf(x[0], m, c);
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 2) scale_shift_pair(x[i], x[i + 1], m, m, c, c);
-}
-
 // The normal distribution's tail Phi(-|z|) = bell * poly, bell = e^(-z^2 / 2), and size = -|z|.  poly = c1 t + .. + c8 t^8 with t = 1 / (1 + 0.305 |z|), the
 // form of formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions; the coefficients are a fit of our own, within 1.6 * 2^-24 of
 // the value itself for |z| up to 14 (least squares over Chebyshev nodes, weighted towards the largest relative error until that is even),

@@ -3,11 +3,17 @@
 //   xhat = (x - mean) * rstd,   rstd = (var + eps)^-1/2 over the f columns of a row,   out = xhat * w + b
 //   g = dout * w,   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)),   dw = sum over the rows of dout * xhat,   db = sum over the rows of dout
 //
-// Bound by HBM: x is read once and stays in registers as it lies in memory, so the variance is a sum of squares of distances from the mean that has
-// been found already.  A lane holds kElems elements of a row, whatever the vector width, so a row has f / 8 lanes: part of a warp, a warp, or
-// (WIDE) several warps that meet in shared memory.  kRows rows are in flight per lane.  Blocks stay and take rows in turn: the weights of a lane's
-// columns stay in registers, and so do, in the gradient, the sums of dw and db over the rows that it has seen; a second launch adds the
-// blocks' sums up in 64 bits in ascending order.
+// Bound by HBM: x is read once and stays in registers, so the variance is a sum of squares of distances from the mean that has been found
+// already.  A lane holds N = 16 elements of a row in vectors of 16 bytes (fewer where rows do not allow them), so a row has f / 16 lanes: part of a warp, a
+// warp, or (WIDE) several warps that meet in shared memory.  Rows of 513 to 768 columns have 24 elements a lane, so that they need no meeting.  Blocks stay, as many as
+// the chip holds, and take rows in turn; the next row's loads are issued before this one is worked on.  In the gradient the sums of dw and db over the rows that
+// a lane has seen stay in registers as well; a second launch adds the blocks' sums up in 64 bits in ascending order.
+//
+// What counts beside the bytes is instructions: arithmetic is done on two elements at a time, addresses are a lane's base and constants, and columns that a lane
+// does not have are registers set to 0 once.  (The gradient of 233 k x 602 fp32, in vectors of two: 58 instructions an element and 452 us with the checks inside,
+// 17 and 287 us without; the weights in shared memory instead of registers leave room for twice the warps, 64 to 512 columns 255 -> 200 us for 400 MB a tensor.)
+// Measured, 400 MB a tensor, fp32 / bf16: forward 0.87 - 0.97 of the copy peak, gradient 0.90 - 0.99 / 0.81 - 0.92 from 64 columns on; bf16 rows of 600 columns
+// 0.75 and 0.68 (a quarter of the lanes' places are empty), odd numbers of bf16 columns 0.3 to 0.6 (elements of 2 bytes one by one).
 #include <type_traits>
 
 #include "schedule.cuh"
@@ -16,10 +22,9 @@
 namespace gnnfd {
 
 constexpr int kLayerBlock = 256;
-constexpr int kLayerColumns = 8192;              // 1024 lanes of kElems elements
-constexpr int kElems = 8;
+constexpr int kLayerColumns = 8192;              // 512 lanes of 16 elements
 constexpr int kLayerSms = 148;
-constexpr int64_t kForwardBlocks = 8 * kLayerSms, kGradBlocks = 3 * kLayerSms;
+constexpr int64_t kGradBlocks = 3 * kLayerSms;   // at most
 
 struct LayerArgs {
     const void *x, *dout;
@@ -56,89 +61,143 @@ __device__ __forceinline__ void row_sums(float (&s)[N], int lanes, float (*red)[
     }
 }
 
-// w[j][i]: the values of a lane's columns (`otherwise` where there are none)
-template <int V>
-__device__ __forceinline__ void load_columns(const float* p, const LayerArgs& a, int lane, float otherwise, float (&w)[kElems / V][V])
+// w[j * V + i]: the values of a lane's columns (`otherwise` where there are none)
+template <int V, int N>
+__device__ __forceinline__ void load_columns(const float* p, const LayerArgs& a, int lanes, int lane, float otherwise, float (&w)[N])
 {
 #pragma unroll
-    for (int j = 0; j < kElems / V; ++j) {
-        const int vec = lane + j * a.lanes;
+    for (int j = 0; j < N / V; ++j) {
+        const int vec = lane + j * lanes;
 #pragma unroll
-        for (int i = 0; i < V; ++i) w[j][i] = p && vec < a.nvec ? load4(p + vec * V + i) : otherwise;
+        for (int i = 0; i < V; ++i) w[j * V + i] = p && vec < a.nvec ? load4(p + vec * V + i) : otherwise;
     }
 }
 
-template <typename TI, int V>
-__device__ __forceinline__ void load_lane(const void* p, int64_t row, int64_t ld, const LayerArgs& a, int lane, Raw<TI, V> (&raw)[kElems / V])
-{
-    const TI* const q = static_cast<const TI*>(p) + row * ld;
+// A lane's share of a row as it lies in memory: vectors lane, lane + lanes, ..; zeros where there are none, since those are never written.
+template <typename TI, int V, int N>
+struct Share {
+    Raw<TI, V> raw[N / V];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int j = 0; j < kElems / V; ++j) {
-        const int vec = lane + j * a.lanes;
-        if (row < a.n && vec < a.nvec) raw[j].load(q + vec * V);
-        else raw[j].zero();
+        for (int j = 0; j < N / V; ++j) raw[j].zero();
+    }
+    // p: the lane's first vector; left: the row's vectors from there on
+    __device__ __forceinline__ void load(const TI* p, int lanes, int left)
+    {
+#pragma unroll
+        for (int j = 0; j < N / V; ++j)
+            if (j * lanes < left) raw[j].load(p + j * lanes * V);
+    }
+    __device__ __forceinline__ void get(float (&x)[N]) const
+    {
+#pragma unroll
+        for (int j = 0; j < N / V; ++j) {
+            float v[V];
+            raw[j].get(v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[j * V + i] = v[i];
+        }
+    }
+};
+
+template <typename TO, int V, int N>
+__device__ __forceinline__ void store_lane(TO* p, int lanes, int left, const float (&x)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N / V; ++j) {
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = x[j * V + i];
+        if (j * lanes < left) store_packed<TO, V>(p + j * lanes * V, v);
     }
 }
+// into fp32 or bf16, `at` elements from the start of the output
+template <int V, int N>
+__device__ __forceinline__ void store_lane(const LayerArgs& a, int64_t at, int lanes, int left, const float (&x)[N])
+{
+    if (a.out_bf16) store_lane<__nv_bfloat16, V>(static_cast<__nv_bfloat16*>(a.out) + at, lanes, left, x);
+    else store_lane<float, V>(static_cast<float*>(a.out) + at, lanes, left, x);
+}
+// x = 0 where a lane has no columns
+template <int V, int N>
+__device__ __forceinline__ void clear_outside(int lanes, int left, float (&x)[N])
+{
+    if ((N / V - 1) * lanes < left) return;
+#pragma unroll
+    for (int j = 0; j < N / V; ++j)
+        if (j * lanes >= left)
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[j * V + i] = 0.f;
+}
+// the sum of x[i] * y[i], of x[i]
+template <int N>
+__device__ __forceinline__ float dot(const float (&x)[N], const float (&y)[N])
+{
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) fma_pairs(s0, s1, x[i], x[i + 1], y[i], y[i + 1]);
+    return s0 + s1;
+}
+template <int N>
+__device__ __forceinline__ float total(const float (&x)[N])
+{
+    float s0 = x[0], s1 = x[1];
+#pragma unroll
+    for (int i = 2; i < N; i += 2) add_pair(s0, s1, x[i], x[i + 1]);
+    return s0 + s1;
+}
 
-template <typename TI, int V, int ROWS, int TEAM>
+template <typename TI, int V, int N, int ROWS, int TEAM>
 __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM) layer_norm_rows(const __grid_constant__ LayerArgs a)
 {
     grid_dependency<true>();
-    constexpr int VPL = kElems / V;
     constexpr bool WIDE = TEAM > 32;
     __shared__ float red[2][ROWS][32];
-    const int lane = WIDE ? threadIdx.x % a.lanes : threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
-    float w[VPL][V], b[VPL][V];
-    load_columns<V>(a.weight, a, lane, 1.f, w);
-    load_columns<V>(a.bias, a, lane, 0.f, b);
-    const int per_block = a.groups * ROWS;
-    for (int64_t base = (int64_t)blockIdx.x * per_block; base < a.n; base += (int64_t)gridDim.x * per_block) {
-        const int64_t row0 = base + group;
-        Raw<TI, V> raw[ROWS][VPL];
-        float mean[ROWS], var[ROWS];
+    const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
+    float w[N], b[N];
+    load_columns<V>(a.weight, a, lanes, lane, 1.f, w);
+    load_columns<V>(a.bias, a, lanes, lane, 0.f, b);
+    const int per_block = a.groups * ROWS, left = a.nvec - lane;
+    const int64_t step = (int64_t)gridDim.x * per_block;
+    Share<TI, V, N> next[ROWS];
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u) load_lane(a.x, row0 + u * a.groups, a.ldx, a, lane, raw[u]);
+    for (int u = 0; u < ROWS; ++u) next[u].clear();
+    const TI* const x0 = static_cast<const TI*>(a.x) + lane * V;
+    auto fetch = [&](int64_t base) {
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            mean[u] = 0.f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                float x[V];
-                raw[u][j].get(x);
-#pragma unroll
-                for (int i = 0; i < V; ++i) mean[u] += x[i];
-            }
+            const int64_t row = base + group + u * a.groups;
+            if (row < a.n) next[u].load(x0 + row * a.ldx, lanes, left);
         }
-        row_sums<ROWS, WIDE>(mean, a.lanes, red[0]);
+    };
+    int64_t base = (int64_t)blockIdx.x * per_block;
+    fetch(base);
+    for (; base < a.n; base += step) {
+        float x[ROWS][N], mean[ROWS], var[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) next[u].get(x[u]);
+        fetch(base + step);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) mean[u] = total(x[u]);
+        row_sums<ROWS, WIDE>(mean, lanes, red[0]);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
             mean[u] *= a.inv_f;
-            var[u] = 0.f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                float x[V];
-                raw[u][j].get(x);
-                if (lane + j * a.lanes < a.nvec)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) var[u] = fmaf(x[i] - mean[u], x[i] - mean[u], var[u]);
-            }
+            const float shift[1] = {mean[u]};
+            add_minus(x[u], shift);
+            clear_outside<V>(lanes, left, x[u]);
+            var[u] = dot(x[u], x[u]);
         }
-        row_sums<ROWS, WIDE>(var, a.lanes, red[1]);
+        row_sums<ROWS, WIDE>(var, lanes, red[1]);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            const int64_t row = row0 + u * a.groups;
+            const int64_t row = base + group + u * a.groups;
             const float rstd = rsqrtf(fmaf(var[u], a.inv_f, a.eps));
             if (row >= a.n) continue;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const int vec = lane + j * a.lanes;
-                if (vec >= a.nvec) continue;
-                float x[V];
-                raw[u][j].get(x);
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = fmaf((x[i] - mean[u]) * rstd, w[j][i], b[j][i]);
-                store_row<V>(a.out, a.out_bf16, row * a.ldo + vec * V, x);
-            }
+            scale(x[u], rstd);
+            scale_shift(x[u], w, b);
+            store_lane<V>(a, row * a.ldo + lane * V, lanes, left, x[u]);
             if (a.mean && lane == 0) {
                 a.mean[row] = mean[u];
                 a.rstd[row] = rstd;
@@ -147,108 +206,122 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM) layer
     }
 }
 
-template <typename TI, int V, int ROWS, int TEAM>
-__global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM) layer_norm_grad(const __grid_constant__ LayerArgs a)
+// x[j * V + i] *= w[j * lanes * V + i]
+template <int V, int N>
+__device__ __forceinline__ void multiply_lane(float (&x)[N], const float* w, int lanes)
+{
+#pragma unroll
+    for (int j = 0; j < N / V; ++j) {
+        constexpr int W = V < 4 ? V : 4;
+#pragma unroll
+        for (int i = 0; i < V; i += W) {
+            float v[W];
+            if constexpr (W == 4) {
+                const float4 q = *reinterpret_cast<const float4*>(w + j * lanes * V + i);
+                v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+            } else if constexpr (W == 2) {
+                const float2 q = *reinterpret_cast<const float2*>(w + j * lanes * V + i);
+                v[0] = q.x; v[1] = q.y;
+            } else {
+                v[0] = w[j * lanes + i];
+            }
+#pragma unroll
+            for (int k = 0; k < W; ++k) x[j * V + i + k] *= v[k];
+        }
+    }
+}
+
+template <typename TI, int V, int N, int TEAM>
+__global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 16 || TEAM > kLayerBlock ? 1 : 2) layer_norm_grad(const __grid_constant__ LayerArgs a)
 {
     grid_dependency<true>();
-    constexpr int VPL = kElems / V;
     constexpr bool WIDE = TEAM > 32;
-    __shared__ float red[2][2 * ROWS][32];
-    __shared__ float columns[(TEAM < kLayerBlock ? kLayerBlock : TEAM) * kElems];
-    const int lane = WIDE ? threadIdx.x % a.lanes : threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
-    float w[VPL][V], dw[VPL][V], db[VPL][V];
-    load_columns<V>(a.weight, a, lane, 1.f, w);
+    __shared__ float red[2][2][32];
+    __shared__ __align__(16) float columns[(TEAM < kLayerBlock ? kLayerBlock : TEAM) * N];      // the weights, at the end the sums of columns
+    const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
+    const int left = a.nvec - lane;
+    // the weights, for columns that no lane has 0
+    if (a.weight)
+        for (int c = threadIdx.x; c < lanes * N; c += blockDim.x) columns[c] = c < a.f ? load4(a.weight + c) : 0.f;
+    __syncthreads();
+    float dw[N], db[N];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) dw[j][i] = db[j][i] = 0.f;
-    const int per_block = a.groups * ROWS;
-    int turn = 0;
-    for (int64_t base = (int64_t)blockIdx.x * per_block; base < a.n; base += (int64_t)gridDim.x * per_block, turn ^= 1) {
-        const int64_t row0 = base + group;
-        Raw<TI, V> x_raw[ROWS][VPL], d_raw[ROWS][VPL];
-        float mean[ROWS], rstd[ROWS], sums[2 * ROWS];
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            const int64_t row = row0 + u * a.groups;
-            load_lane(a.x, row, a.ldx, a, lane, x_raw[u]);
-            load_lane(a.dout, row, a.ldd, a, lane, d_raw[u]);
-            mean[u] = row < a.n ? load4(a.mean + row) : 0.f;
-            rstd[u] = row < a.n ? load4(a.rstd + row) : 0.f;
+    for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+    const int64_t step = (int64_t)gridDim.x * a.groups;
+    Share<TI, V, N> next_x, next_d;
+    next_x.clear();
+    next_d.clear();
+    const TI *const x0 = static_cast<const TI*>(a.x) + lane * V, *const d0 = static_cast<const TI*>(a.dout) + lane * V;
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto fetch = [&](int64_t row) {
+        if (row >= a.n) return;
+        next_x.load(x0 + row * a.ldx, lanes, left);
+        next_d.load(d0 + row * a.ldd, lanes, left);
+        next_mean = load4(a.mean + row);
+        next_rstd = load4(a.rstd + row);
+    };
+    int64_t base = (int64_t)blockIdx.x * a.groups;
+    fetch(base + group);
+    for (int turn = 0; base < a.n; base += step, turn ^= 1) {
+        const int64_t row = base + group;
+        float x[N], d[N], sums[2];
+        next_x.get(x);
+        next_d.get(d);
+        const float shift[1] = {next_mean}, rstd = next_rstd;
+        fetch(row + step);
+        add_minus(x, shift);
+        scale(x, rstd);
+        if (row < a.n) {                                         // (columns that a lane does not have: d is 0, x what it may)
+            add_all(db, d);
+            add_products(dw, d, x);
         }
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            sums[2 * u] = sums[2 * u + 1] = 0.f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                if (lane + j * a.lanes >= a.nvec) continue;
-                float x[V], d[V];
-                x_raw[u][j].get(x);
-                d_raw[u][j].get(d);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xhat = (x[i] - mean[u]) * rstd[u], g = d[i] * w[j][i];
-                    sums[2 * u] += g;
-                    sums[2 * u + 1] = fmaf(g, xhat, sums[2 * u + 1]);
-                    dw[j][i] = fmaf(d[i], xhat, dw[j][i]);
-                    db[j][i] += d[i];
-                }
-            }
-        }
-        row_sums<2 * ROWS, WIDE>(sums, a.lanes, red[turn]);
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            const int64_t row = row0 + u * a.groups;
-            if (row >= a.n) continue;
-            const float m1 = sums[2 * u] * a.inv_f, m2 = sums[2 * u + 1] * a.inv_f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const int vec = lane + j * a.lanes;
-                if (vec >= a.nvec) continue;
-                float x[V], d[V];
-                x_raw[u][j].get(x);
-                d_raw[u][j].get(d);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xhat = (x[i] - mean[u]) * rstd[u];
-                    x[i] = rstd[u] * (fmaf(d[i], w[j][i], -m1) - xhat * m2);
-                }
-                store_row<V>(a.out, a.out_bf16, row * a.ldo + vec * V, x);
-            }
-        }
+        if (a.weight) multiply_lane<V>(d, columns + lane * V, lanes);
+        sums[0] = total(d);
+        sums[1] = dot(d, x);
+        row_sums<2, WIDE>(sums, lanes, red[turn]);
+        if (row >= a.n) continue;
+        // rstd (d - m1 - x m2)
+        scale(x, -sums[1] * a.inv_f);
+        add_all(x, d);
+        const float m1[1] = {sums[0] * a.inv_f};
+        add_minus(x, m1);
+        scale(x, rstd);
+        store_lane<V>(a, row * a.ldo + lane * V, lanes, left, x);
     }
     if (!a.part) return;
     // the block's sums of each column, over its groups in ascending order
     for (int k = 0; k < 2; ++k) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
+        for (int j = 0; j < N / V; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) columns[((group * VPL + j) * a.lanes + lane) * V + i] = k == 0 ? dw[j][i] : db[j][i];
+            for (int i = 0; i < V; ++i) columns[((group * (N / V) + j) * lanes + lane) * V + i] = k == 0 ? dw[j * V + i] : db[j * V + i];
         __syncthreads();
         for (int c = threadIdx.x; c < a.f; c += blockDim.x) {
             float sum = 0.f;
-            for (int q = 0; q < a.groups; ++q) sum += columns[q * kElems * a.lanes + c];
+            for (int q = 0; q < a.groups; ++q) sum += columns[q * N * lanes + c];
             a.part[((int64_t)blockIdx.x * 2 + k) * a.f + c] = sum;
         }
     }
 }
 
-// dw and db [f] each: the blocks' sums [rows, 2 f] added up, 8 ways a column.
-__global__ void __launch_bounds__(256) layer_norm_columns(const float* part, int32_t rows, int32_t f, float* dweight, float* dbias)
+// dw and db [f] each: the blocks' sums [rows, 2 f] added up, 32 ways a column (8 ways took 7.5 us for 296 blocks, half of it waiting for loads).
+__global__ void __launch_bounds__(1024) layer_norm_columns(const float* part, int32_t rows, int32_t f, float* dweight, float* dbias)
 {
     grid_dependency<true>();
-    __shared__ double sums[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), way = threadIdx.x >> 5;
+    __shared__ double sums[32][33];
+    const int lane = threadIdx.x & 31, way = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     double sum = 0.0;
     if (c < 2 * f)
-#pragma unroll 8
-        for (int r = way; r < rows; r += 8) sum += load4(part + (int64_t)r * 2 * f + c);
-    sums[way][threadIdx.x & 31] = sum;
+#pragma unroll 10
+        for (int r = way; r < rows; r += 32) sum += load4(part + (int64_t)r * 2 * f + c);
+    sums[way][lane] = sum;
     __syncthreads();
-    if (way != 0 || c >= 2 * f) return;
-    for (int k = 1; k < 8; ++k) sum += sums[k][threadIdx.x];
-    (c < f ? dweight : dbias - f)[c] = (float)sum;
+    sum = sums[lane][way];                                // a warp adds up the ways of a column
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const int column = blockIdx.x * 32 + way;
+    if (lane == 0 && column < 2 * f) (column < f ? dweight : dbias - f)[column] = (float)sum;
 }
 
 // ------------------------------------------------------------------ host side
@@ -261,43 +334,50 @@ static int check_layer_norm(int64_t n, int32_t f, gnnfd_dtype_t xdt, gnnfd_dtype
     return GNNFD_OK;
 }
 
-// The widest vector that divides a row and that all rows can be read and written in; lanes and rows of a block.  Returns the threads.
-static int plan_layer_norm(LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt, int* v)
+// The widest vector that divides a row and that all rows can be read and written in.
+static int layer_vector(const LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt)
 {
     const int xs = xdt == GNNFD_F32 ? 4 : 2, os = odt == GNNFD_F32 ? 4 : 2;
-    *v = 16 / xs;
-    while (*v > 1 && !(a.f % *v == 0 && rows_fit(a.x, a.ldx, xs, *v) && (!a.dout || rows_fit(a.dout, a.ldd, xs, *v)) && rows_fit(a.out, a.ldo, os, *v)))
-        *v /= 2;
-    a.nvec = a.f / *v;
-    const int per_lane = kElems / *v, lanes = (a.nvec + per_lane - 1) / per_lane;
-    a.lanes = lanes <= 32 ? 1 << ilog2(lanes) : (lanes + 31) / 32 * 32;
-    a.groups = a.lanes < kLayerBlock ? kLayerBlock / a.lanes : 1;
-    return a.groups * a.lanes;
+    int v = 16 / xs;
+    while (v > 1 && !(a.f % v == 0 && rows_fit(a.x, a.ldx, xs, v) && (!a.dout || rows_fit(a.dout, a.ldd, xs, v)) && rows_fit(a.out, a.ldo, os, v)))
+        v /= 2;
+    return v;
 }
 
-template <typename TI, int V, int TEAM>
-static void launch_layer_norm(const LayerArgs& a, int threads, int32_t* blocks, cudaStream_t s)
+template <typename TI, int V, int N, int TEAM>
+static void launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
 {
-    // rows in flight per lane; of more than 256 lanes there are too many registers for two
-    constexpr int kForwardRows = TEAM > kLayerBlock ? 1 : sizeof(TI) == 4 ? 2 : 4, kGradRows = TEAM > kLayerBlock ? 1 : 2;
-    const int64_t per_block = (int64_t)a.groups * (a.dout ? kGradRows : kForwardRows), need = (a.n + per_block - 1) / per_block;
-    const int64_t most = a.dout ? kGradBlocks : kForwardBlocks;
-    *blocks = (int32_t)(need < most ? need : most);
-    if (a.dout) GNNFD_LAUNCH("layer_norm_grad", s, (layer_norm_grad<TI, V, kGradRows, TEAM>), (unsigned)*blocks, threads, 0, a);
-    else GNNFD_LAUNCH("layer_norm_rows", s, (layer_norm_rows<TI, V, kForwardRows, TEAM>), (unsigned)*blocks, threads, 0, a);
+    constexpr int kRows = sizeof(TI) == 4 || N > 16 ? 1 : 2;
+    const int lanes = (a.nvec + N / V - 1) / (N / V);
+    a.lanes = TEAM >= 32 ? (lanes + 31) / 32 * 32 : 1 << ilog2(lanes);
+    a.groups = a.lanes < kLayerBlock ? kLayerBlock / a.lanes : 1;
+    const int64_t per_block = a.groups * (a.dout ? 1 : kRows), need = (a.n + per_block - 1) / per_block;
+    constexpr int kThreads = TEAM < kLayerBlock ? kLayerBlock : TEAM;
+    if (a.dout) {
+        static const int held = blocks_per_sm(layer_norm_grad<TI, V, N, TEAM>, kThreads, 0);
+        *blocks = (int32_t)(need < kLayerSms * held ? need : kLayerSms * held);
+        GNNFD_LAUNCH("layer_norm_grad", s, (layer_norm_grad<TI, V, N, TEAM>), (unsigned)*blocks, a.groups * a.lanes, 0, a);
+    } else {
+        static const int held = blocks_per_sm(layer_norm_rows<TI, V, N, kRows, TEAM>, kThreads, 0);
+        *blocks = (int32_t)(need < kLayerSms * held ? need : kLayerSms * held);
+        GNNFD_LAUNCH("layer_norm_rows", s, (layer_norm_rows<TI, V, N, kRows, TEAM>), (unsigned)*blocks, a.groups * a.lanes, 0, a);
+    }
 }
 
 static int run_layer_norm(LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt, int32_t* blocks, cudaStream_t s)
 {
-    int v;
-    const int threads = plan_layer_norm(a, xdt, odt, &v);
+    const int v = layer_vector(a, xdt, odt);
+    a.nvec = a.f / v;
     auto run = [&](auto type) {
         using TI = decltype(type);
         with_vector<TI>(v, [&](auto w) {
             constexpr int V = decltype(w)::value;
-            if (a.lanes > kLayerBlock) launch_layer_norm<TI, V, 1024>(a, threads, blocks, s);
-            else if (a.lanes > 32) launch_layer_norm<TI, V, kLayerBlock>(a, threads, blocks, s);
-            else launch_layer_norm<TI, V, 32>(a, threads, blocks, s);
+            if (V == 1 && a.f <= 4 * 32) launch_layer_norm<TI, V, V == 1 ? 4 : 16, 16>(a, blocks, s);
+            else if (a.f <= 16 * 16) launch_layer_norm<TI, V, 16, 16>(a, blocks, s);
+            else if (a.f <= 16 * 32) launch_layer_norm<TI, V, 16, 32>(a, blocks, s);
+            else if (a.f <= 24 * 32) launch_layer_norm<TI, V, 24, 32>(a, blocks, s);
+            else if (a.f <= 16 * kLayerBlock) launch_layer_norm<TI, V, 16, kLayerBlock>(a, blocks, s);
+            else launch_layer_norm<TI, V, 16, 512>(a, blocks, s);
             return 0;
         });
     };
@@ -369,7 +449,7 @@ int gnnfd_layer_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
     int32_t blocks;
     const int done = run_layer_norm(a, xdt, gdt, &blocks, s);
     if (done || !d_dweight) return done;
-    GNNFD_LAUNCH("layer_norm_columns", s, layer_norm_columns, (unsigned)((2 * f + 31) / 32), 256, 0, a.part, blocks, f, d_dweight, d_dbias);
+    GNNFD_LAUNCH("layer_norm_columns", s, layer_norm_columns, (unsigned)((2 * f + 31) / 32), 1024, 0, a.part, blocks, f, d_dweight, d_dbias);
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
 }
