@@ -505,7 +505,7 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * behind the last offset are left as they are; graphs may be empty (their last state is the first one).  Offsets outside [0, n] or not ascending are cut to what is
  * inside: nothing outside of the arrays is touched.  d_x, d_gate [n, ld] of type dt, d_out [n, ldo] of type odt, not overlapping them.  d_final (fp32
  * [graphs, f], may be NULL) receives the last state of each graph; it may be d_initial itself where graphs = n and d_graph_ptr is NULL, and does not overlap it otherwise.  d_states
- * (may be NULL): fp32 [(n + 15) / 16, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
+ * (may be NULL): fp32 [(n + 7) / 8, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
  * d_scratch: gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, d_graph_ptr == NULL, 0) bytes, 256-byte aligned (0 and NULL for few rows).
  *
  * gnnfd_linear_recurrence_backward: for d_dout [n, ldd] of type dt and d_dfinal (fp32 [graphs, f]; NULL: 0), the gradients of out and the last states, d_dx and

@@ -22,10 +22,13 @@
 
 namespace gnnfd {
 
-constexpr int kScanBlock = 256;
 constexpr int kScanSms = 148;
-constexpr int kStateRows = 16;
-constexpr int kFusedRows = 2048, kFusedLanes = 8, kFusedWays = 64;        // rows of a call that takes one launch; its blocks
+constexpr int kStateRows = 8;
+constexpr int kFewRows = 2048;                   // rows of a call that takes one launch
+
+// Threads of the kernels, of the gradient's walk; lanes and ways of the one launch for few rows
+constexpr int kRowsBlock = 256, kGradBlock = 64;
+template <bool BACK> struct Few { static constexpr int kLanes = BACK ? 2 : 8, kWays = 32, kThreads = kLanes * kWays; };
 
 struct ScanArgs {
     const void *x, *gate, *dout;
@@ -38,7 +41,8 @@ struct ScanArgs {
     float* carry;                                // [tiles, f] state at the tile's start (null: no state crosses chunks)
     int32_t* chunk_graph;                        // [chunks] graph of the first row (going back: of the last)
     int64_t ldx, ldg, ldd, ldo, lddg;
-    int32_t n, graphs, length, f, nvec, ptr64, out_bf16;
+    int32_t n, graphs, length, f, ptr64, out_bf16;
+    int32_t places;                              // threads that share a row: see Columns
     int32_t chunk_rows, chunks, tiles, tile_chunks, lanes, ways;
 };
 
@@ -54,12 +58,16 @@ __device__ __forceinline__ float one_over(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// e^-|g| with g's sign, from which a and 1 - a come without cancellation
-__device__ __forceinline__ float signed_exp(float g) { return copysignf(power_of_2(-1.4426950408889634f * fabsf(g)), g); }
-__device__ __forceinline__ void sigmoid_parts(float e, float& a, float& rest)
+// The smaller one of a = 1 / (1 + e^-g) and 1 - a, with g's sign: both come from it without cancellation.
+__device__ __forceinline__ float smaller_part(float g)
 {
-    const float size = fabsf(e), large = one_over(1.f + size), small = size * large;
-    const bool negative = __float_as_uint(e) >> 31;
+    const float e = power_of_2(-1.4426950408889634f * fabsf(g));
+    return copysignf(e * one_over(1.f + e), g);
+}
+__device__ __forceinline__ void sigmoid_parts(float smaller, float& a, float& rest)
+{
+    const float small = fabsf(smaller), large = 1.f - small;
+    const bool negative = __float_as_uint(smaller) >> 31;
     a = negative ? small : large;
     rest = negative ? large : small;
 }
@@ -69,7 +77,7 @@ __device__ __forceinline__ void step_of(float g, float x, float& a, float& b)
 {
     if constexpr (SIGMOID) {
         float rest;
-        sigmoid_parts(signed_exp(g), a, rest);
+        sigmoid_parts(smaller_part(g), a, rest);
         b = rest * x;
     } else {
         a = g;
@@ -138,179 +146,336 @@ struct Graph {
     }
 };
 
-template <int V>
-__device__ __forceinline__ void load_state(const float* p, const ScanArgs& a, int64_t row, int c, float (&s)[V])
+// The columns of a thread: P pieces of W neighbouring ones, `step` columns apart (so that the threads of a row read neighbouring pieces), of which
+// the first `pieces` exist.
+template <int W, int P>
+struct Columns {
+    int first, step, pieces;
+    __device__ __forceinline__ void at(const ScanArgs& a, int place)
+    {
+        first = place * W;
+        step = a.places * W;
+        pieces = P;
+        if constexpr (P > 1)
+            while (pieces > 0 && first + (pieces - 1) * step >= a.f) --pieces;
+    }
+    __device__ __forceinline__ bool has(int p) const { return P == 1 || p < pieces; }
+    __device__ __forceinline__ int column(int p, int i) const { return first + p * step + i; }
+};
+
+// Rows on their way into shared memory.  Every thread copies the pieces of its own columns into places of its own and reads them from there, so nobody waits
+// for others, and how many rows are on their way does not cost registers.
+template <typename TI, int W>
+__device__ __forceinline__ void copy_piece(char* to, const TI* from)
 {
-#pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = p ? load4(p + row * a.f + c + i) : 0.f;
+    constexpr int kBytes = W * (int)sizeof(TI);
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else if constexpr (kBytes >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes < 4 ? 4 : kBytes) : "memory");
+    else *reinterpret_cast<TI*>(to) = *from;                    // (these copies take 4 bytes at least: the threads wait for one row after the other)
 }
-template <int V>
-__device__ __forceinline__ void store_state(float* p, const ScanArgs& a, int64_t row, int c, const float (&s)[V])
+__device__ __forceinline__ void end_of_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void all_but_last() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <typename TI, int W>
+__device__ __forceinline__ void read_piece(const char* from, float* x)
 {
+    constexpr int kBytes = W * (int)sizeof(TI);
+    Raw<TI, W> raw;
+    if constexpr (kBytes == 16) {
+        const uint4 v = *reinterpret_cast<const uint4*>(from);
+        raw.w[0] = v.x; raw.w[1] = v.y; raw.w[2] = v.z; raw.w[3] = v.w;
+    } else if constexpr (kBytes == 8) {
+        const uint2 v = *reinterpret_cast<const uint2*>(from);
+        raw.w[0] = v.x; raw.w[1] = v.y;
+    } else if constexpr (kBytes == 4) {
+        raw.w[0] = *reinterpret_cast<const uint32_t*>(from);
+    } else {
+        raw.w[0] = *reinterpret_cast<const unsigned short*>(from);
+    }
+    float v[W];
+    raw.get(v);
 #pragma unroll
-    for (int i = 0; i < V; ++i) p[row * a.f + c + i] = s[i];
+    for (int i = 0; i < W; ++i) x[i] = v[i];
 }
 
-// The map over rows r0 .. r1 - 1 of V columns from c on; `g` is the graph of r0 (going back, of r1 - 1).
-template <typename TI, int V, bool SIGMOID, bool BACK, int U>
-__device__ __forceinline__ void chunk_map(const ScanArgs& a, int32_t r0, int32_t r1, int c, Graph g, float2 (&map)[V])
-{
+// A row of two matrices in the places of a thread among THREADS.
+template <typename TI, int W, int P, int THREADS>
+struct Pair {
+    static constexpr int kPiece = THREADS * W * (int)sizeof(TI), kRow = 2 * P * kPiece;
+    static constexpr int kAhead = W * P * (int)sizeof(TI) >= 16 ? 4 : 8;       // rows on their way
+    static constexpr int kBytes = kAhead * kRow;                                // (a power of two)
+    // `slot` is the thread's first place of the row
+    __device__ __forceinline__ static void copy(char* slot, const TI* first, const TI* second, const Columns<W, P>& c)
+    {
 #pragma unroll
-    for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
-    const TI *const gates = static_cast<const TI*>(a.gate) + c, *const in = static_cast<const TI*>(BACK ? a.dout : a.x) + c;
-    const int64_t ld = BACK ? a.ldd : a.ldx;
-    for (int32_t r = 0; r < r1 - r0; r += U) {
-        Raw<TI, V> gate[U], value[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r + u < r1 - r0) {
-                const int64_t row = BACK ? r1 - 1 - r - u : r0 + r + u;
-                gate[u].load(gates + row * a.ldg);
-                value[u].load(in + row * ld);
+        for (int k = 0; k < P; ++k)
+            if (c.has(k)) {
+                copy_piece<TI, W>(slot + k * kPiece, first + k * c.step);
+                copy_piece<TI, W>(slot + (P + k) * kPiece, second + k * c.step);
             }
+    }
+    // (pieces that do not exist: whatever lies there, for columns that are not written)
+    __device__ __forceinline__ static void read(const char* slot, float (&x)[W * P], float (&y)[W * P])
+    {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (r + u >= r1 - r0) break;
-            const int32_t row = BACK ? r1 - 1 - r - u : r0 + r + u;
-            float gv[V], v[V];
-            gate[u].get(gv);
-            value[u].get(v);
-            if (row == (BACK ? g.end - 1 : g.start)) {
-                float s[V];
-                load_state(BACK ? a.last_grad : a.first, a, g.b, c, s);
-#pragma unroll
-                for (int i = 0; i < V; ++i) map[i] = make_float2(__uint_as_float(0x7fffffffu), s[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float w, b;
-                step_of<SIGMOID>(gv[i], v[i], w, b);
-                map[i].x *= w;
-                map[i].y = BACK ? w * (map[i].y + v[i]) : fmaf(w, map[i].y, b);
-            }
-            if (BACK && row == g.start) g.previous(a);
-            if (!BACK && row + 1 == g.end) g.next(a);
+        for (int k = 0; k < P; ++k) {
+            read_piece<TI, W>(slot + k * kPiece, x + k * W);
+            read_piece<TI, W>(slot + (P + k) * kPiece, y + k * W);
         }
     }
+};
+
+// work(row, a row of the first matrix, of the second) for `rows` rows from r on (BACK: towards the first).
+template <typename TI, int W, int P, int THREADS, bool BACK, typename F>
+__device__ __forceinline__ void stream_rows(char* ring, const TI* first, int64_t ld_first, const TI* second, int64_t ld_second, int32_t r, int32_t rows,
+                                            const Columns<W, P>& c, F work)
+{
+    using Rows = Pair<TI, W, P, THREADS>;
+    char* const place = ring + threadIdx.x * (W * (int)sizeof(TI));
+    first += r * ld_first + c.first;
+    second += r * ld_second + c.first;
+    if (BACK) {
+        ld_first = -ld_first;
+        ld_second = -ld_second;
+    }
+#pragma unroll
+    for (int k = 0; k < Rows::kAhead; ++k) {
+        if (k < rows) Rows::copy(place + k * Rows::kRow, first, second, c);
+        end_of_row();
+        first += ld_first;
+        second += ld_second;
+    }
+    int at = 0;
+#pragma unroll 1
+    for (int32_t k = 0; k < rows; ++k, r += BACK ? -1 : 1) {
+        float x[W * P], y[W * P];
+        all_but_last<Rows::kAhead - 1>();
+        Rows::read(place + at, x, y);
+        work(r, x, y);
+        if (k + Rows::kAhead < rows) Rows::copy(place + at, first, second, c);
+        end_of_row();
+        first += ld_first;
+        second += ld_second;
+        at = (at + Rows::kRow) & (Rows::kBytes - 1);
+    }
+}
+
+template <int W, int P>
+__device__ __forceinline__ void store_pieces(void* out, int bf16, int64_t at, const Columns<W, P>& c, const float (&x)[W * P])
+{
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        float v[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = x[k * W + i];
+        if (c.has(k)) store_row<W>(out, bf16, at + k * c.step, v);
+    }
+}
+// one row of fp32 [.., f], at any alignment; zeros where there is no array
+template <int W, int P>
+__device__ __forceinline__ void load_state(const float* p, const ScanArgs& a, int64_t row, const Columns<W, P>& c, float (&s)[W * P])
+{
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+#pragma unroll
+        for (int i = 0; i < W; ++i) s[k * W + i] = p && c.has(k) ? load4(p + row * a.f + c.column(k, i)) : 0.f;
+}
+template <int W, int P>
+__device__ __forceinline__ void store_state(float* p, const ScanArgs& a, int64_t row, const Columns<W, P>& c, const float (&s)[W * P])
+{
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+        if (c.has(k))
+#pragma unroll
+            for (int i = 0; i < W; ++i) p[row * a.f + c.column(k, i)] = s[k * W + i];
+}
+
+// The map over rows r0 .. r1 - 1; `g` is the graph of r0 (going back, of r1 - 1).
+template <typename TI, int W, int P, int THREADS, bool SIGMOID, bool BACK>
+__device__ __forceinline__ void chunk_map(const ScanArgs& a, char* ring, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float2 (&map)[W * P])
+{
+    constexpr int V = W * P;
+    auto cut = [&] {                                             // (from its graph's own state)
+        float s[V];
+        load_state(BACK ? a.last_grad : a.first, a, g.b, c, s);
+#pragma unroll
+        for (int i = 0; i < V; ++i) map[i] = make_float2(__uint_as_float(0x7fffffffu), s[i]);
+    };
+#pragma unroll
+    for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
+    if (BACK ? r1 == g.end : r0 == g.start) cut();
+    stream_rows<TI, W, P, THREADS, BACK>(ring, static_cast<const TI*>(a.gate), a.ldg, static_cast<const TI*>(BACK ? a.dout : a.x), BACK ? a.ldd : a.ldx,
+                                         BACK ? r1 - 1 : r0, r1 - r0, c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
+        if (BACK ? row + 1 == g.start : row == g.end) {
+            if (BACK) g.previous(a);
+            else g.next(a);
+            cut();
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float w, b;
+            step_of<SIGMOID>(gate[i], value[i], w, b);
+            map[i].x *= w;
+            map[i].y = BACK ? w * (map[i].y + value[i]) : fmaf(w, map[i].y, b);
+        }
+    });
 }
 
 // The rows themselves, from the state h on.
-template <typename TI, int V, bool SIGMOID, int U>
-__device__ __forceinline__ void forward_rows(const ScanArgs& a, int32_t r0, int32_t r1, int c, Graph g, float (&h)[V])
+template <typename TI, int W, int P, int THREADS, bool SIGMOID>
+__device__ __forceinline__ void forward_rows(const ScanArgs& a, char* ring, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float (&h)[W * P])
 {
-    const TI *const gates = static_cast<const TI*>(a.gate) + c, *const in = static_cast<const TI*>(a.x) + c;
-    for (int32_t r = r0; r < r1; r += U) {
-        Raw<TI, V> gate[U], value[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (r + u < r1) {
-                gate[u].load(gates + (int64_t)(r + u) * a.ldg);
-                value[u].load(in + (int64_t)(r + u) * a.ldx);
-            }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t row = r + u;
-            if (row >= r1) break;
-            float gv[V], v[V];
-            gate[u].get(gv);
-            value[u].get(v);
-            if (row == g.start) load_state(a.first, a, g.b, c, h);
-            if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float w, b;
-                step_of<SIGMOID>(gv[i], v[i], w, b);
-                h[i] = fmaf(w, h[i], b);
-            }
-            store_row<V>(a.out, a.out_bf16, row * a.ldo + c, h);
-            if (row + 1 == g.end) {
-                if (a.last) store_state(a.last, a, g.b, c, h);
-                g.next(a);
-            }
+    constexpr int V = W * P;
+    if (r0 == g.start) load_state(a.first, a, g.b, c, h);
+    int64_t at = r0 * a.ldo + c.first;
+    stream_rows<TI, W, P, THREADS, false>(ring, static_cast<const TI*>(a.gate), a.ldg, static_cast<const TI*>(a.x), a.ldx, r0, r1 - r0, c,
+                                          [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
+        if (row == g.end) {
+            if (a.last) store_state(a.last, a, g.b, c, h);
+            g.next(a);
+            load_state(a.first, a, g.b, c, h);
         }
-    }
+        if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float w, b;
+            step_of<SIGMOID>(gate[i], value[i], w, b);
+            h[i] = fmaf(w, h[i], b);
+        }
+        store_pieces<W, P>(a.out, a.out_bf16, at, c, h);
+        at += a.ldo;
+    });
+    if (a.last && r1 == g.end) store_state(a.last, a, g.b, c, h);
 }
 
-// The gradients of the rows, from what arrives behind the last one on; r0 is a multiple of kStateRows.  Rows are taken kStateRows at a time: forward from the
-// state that the forward call left, to what each row multiplies G with, and back.
-template <typename TI, int V, bool SIGMOID>
-__device__ __forceinline__ void backward_rows(const ScanArgs& a, int32_t r0, int32_t r1, int c, Graph g, float (&carry)[V])
+template <int W>
+__device__ __forceinline__ void write_piece(char* to, const float* x)
 {
-    constexpr int N = kStateRows, U = 8;
-    const TI *const gates = static_cast<const TI*>(a.gate) + c, *const in = static_cast<const TI*>(a.x) + c, *const grads = static_cast<const TI*>(a.dout) + c;
-    for (int32_t q0 = (r1 - 1) / N * N; q0 >= r0; q0 -= N) {
-        const int rows = min(N, r1 - q0);
-        float weight[N][V], slope[N][V], h[V];       // a (as signed_exp's result), and G's factor in dgate
+    if constexpr (W == 4) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    else if constexpr (W == 2) *reinterpret_cast<float2*>(to) = make_float2(x[0], x[1]);
+    else *reinterpret_cast<float*>(to) = x[0];
+}
+
+// What the threads of the gradient's walk have in shared memory: places of W fp32 values for each thread and piece of kStateRows rows of gates, x and dout.  Gates
+// and x are replaced there by what the way back needs: the weight of the row's step and the factor of G in dgate.
+template <int W, int P, int THREADS>
+struct GradPlaces {
+    static constexpr int kPiece = THREADS * W * 4, kRow = 3 * P * kPiece, kBytes = kStateRows * kRow;
+    enum { kGate = 0, kX = P, kDout = 2 * P };
+};
+
+// The gradients of the rows, from what arrives behind the last one on; r0 is a multiple of kStateRows.  Rows are taken kStateRows at a time: forward from the
+// state that the forward call left, then back.  On the way forward the rows of dout are sent for, on the way back the gates and x of the rows ahead: whenever
+// a row is waited for, kStateRows - 1 others have been sent for after it.
+template <typename TI, int W, int P, int THREADS, bool SIGMOID>
+__device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float (&carry)[W * P])
+{
+    constexpr int V = W * P, N = kStateRows;
+    using Pl = GradPlaces<W, P, THREADS>;
+    places += threadIdx.x * (W * 4);
+    const TI *const gates = static_cast<const TI*>(a.gate) + c.first, *const in = static_cast<const TI*>(a.x) + c.first,
+             *const douts = static_cast<const TI*>(a.dout) + c.first;
+    auto copy_row = [&](char* to, const TI* from) {
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            if (c.has(j)) copy_piece<TI, W>(to + j * Pl::kPiece, from + j * c.step);
+    };
+    auto copy_inputs = [&](int slot, int32_t row) {
+        copy_row(places + slot * Pl::kRow + Pl::kGate * Pl::kPiece, gates + row * a.ldg);
+        copy_row(places + slot * Pl::kRow + Pl::kX * Pl::kPiece, in + row * a.ldx);
+    };
+    int32_t q0 = (r1 - 1) / N * N;
+    float h[V], next[V];
+#pragma unroll 1
+    for (int k = 0; k < N; ++k) {
+        if (q0 + k < r1) copy_inputs(k, q0 + k);
+        end_of_row();
+    }
+    load_state(a.states, a, q0 / N, c, next);
+    if (r1 == g.end) load_state(a.last_grad, a, g.b, c, carry);
+    // Row k of a stretch lies in slot k ^ flip: places become free on the way back, the last row's first, for the next stretch's first.
+    int flip = 0;
+#pragma unroll 1
+    for (int rows = r1 - q0; q0 >= r0; q0 -= N, rows = N, flip ^= N - 1) {
         Graph from = g;
         while (from.start > q0 && from.b > 0) from.previous(a);
-        load_state(a.states, a, q0 / N, c, h);
 #pragma unroll
-        for (int k = 0; k < N; k += U) {
-            Raw<TI, V> gate[U], value[U];
+        for (int i = 0; i < V; ++i) h[i] = next[i];
+        if (q0 - N >= r0) load_state(a.states, a, q0 / N - 1, c, next);
+#pragma unroll 1
+        for (int k = 0; k < N; ++k) {
+            all_but_last<N - 1>();
+            if (N - 1 - k < rows) copy_row(places + (N - 1 - k) * Pl::kRow + Pl::kDout * Pl::kPiece, douts + (q0 + N - 1 - k) * a.ldd);
+            end_of_row();
+            if (k >= rows) continue;
+            char* const slot = places + (k ^ flip) * Pl::kRow;
+            float gate[V], value[V];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (k + u < rows) {
-                    gate[u].load(gates + (int64_t)(q0 + k + u) * a.ldg);
-                    value[u].load(in + (int64_t)(q0 + k + u) * a.ldx);
-                }
+            for (int j = 0; j < P; ++j) {
+                read_piece<TI, W>(slot + (Pl::kGate + j) * Pl::kPiece, gate + j * W);
+                read_piece<TI, W>(slot + (Pl::kX + j) * Pl::kPiece, value + j * W);
+            }
+            if (q0 + k == from.end) {
+                from.next(a);
+                load_state(a.first, a, from.b, c, h);
+            }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (k + u >= rows) continue;
-                float gv[V], v[V];
-                gate[u].get(gv);
-                value[u].get(v);
-                if (q0 + k + u == from.end) {
-                    from.next(a);
-                    load_state(a.first, a, from.b, c, h);
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if constexpr (SIGMOID) {
-                        const float e = signed_exp(gv[i]);
-                        float w, rest;
-                        sigmoid_parts(e, w, rest);
-                        weight[k + u][i] = e;
-                        slope[k + u][i] = (h[i] - v[i]) * (w * rest);
-                        h[i] = fmaf(w, h[i], rest * v[i]);
-                    } else {
-                        weight[k + u][i] = gv[i];
-                        slope[k + u][i] = h[i];
-                        h[i] = fmaf(gv[i], h[i], v[i]);
-                    }
+            for (int i = 0; i < V; ++i) {
+                const float x = value[i];
+                if constexpr (SIGMOID) {
+                    float w, rest;
+                    gate[i] = smaller_part(gate[i]);
+                    sigmoid_parts(gate[i], w, rest);
+                    value[i] = (h[i] - x) * (w * rest);
+                    h[i] = fmaf(w, h[i], rest * x);
+                } else {
+                    value[i] = h[i];
+                    h[i] = fmaf(gate[i], h[i], x);
                 }
             }
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                write_piece<W>(slot + (Pl::kGate + j) * Pl::kPiece, gate + j * W);
+                write_piece<W>(slot + (Pl::kX + j) * Pl::kPiece, value + j * W);
+            }
         }
+#pragma unroll 1
+        for (int k = N - 1; k >= 0; --k) {
+            all_but_last<N - 1>();
+            if (k < rows) {
+                const int32_t row = q0 + k;
+                const char* const slot = places + (k ^ flip) * Pl::kRow;
+                float d[V], keep[V], dg[V];
 #pragma unroll
-        for (int k = N - U; k >= 0; k -= U) {
-            Raw<TI, V> grad[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (k + u < rows) grad[u].load(grads + (int64_t)(q0 + k + u) * a.ldd);
-#pragma unroll
-            for (int u = U - 1; u >= 0; --u) {
-                if (k + u >= rows) continue;
-                const int32_t row = q0 + k + u;
-                float d[V], dx[V], dg[V];
-                grad[u].get(d);
-                if (row + 1 == g.end) load_state(a.last_grad, a, g.b, c, carry);
+                for (int j = 0; j < P; ++j) {
+                    read_piece<TI, W>(places + k * Pl::kRow + (Pl::kDout + j) * Pl::kPiece, d + j * W);
+                    read_piece<float, W>(slot + (Pl::kGate + j) * Pl::kPiece, keep + j * W);
+                    read_piece<float, W>(slot + (Pl::kX + j) * Pl::kPiece, dg + j * W);
+                }
+                if (row + 1 == g.start) {
+                    if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
+                    g.previous(a);
+                    load_state(a.last_grad, a, g.b, c, carry);
+                }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float total = d[i] + carry[i];
-                    float w = weight[k + u][i], rest = 1.f;
-                    if constexpr (SIGMOID) sigmoid_parts(weight[k + u][i], w, rest);
-                    dx[i] = SIGMOID ? rest * total : total;
-                    dg[i] = slope[k + u][i] * total;
+                    float w = keep[i], rest = 1.f;
+                    if constexpr (SIGMOID) sigmoid_parts(keep[i], w, rest);
+                    d[i] = SIGMOID ? rest * total : total;
+                    dg[i] *= total;
                     carry[i] = w * total;
                 }
-                store_row<V>(a.out, a.out_bf16, row * a.ldo + c, dx);
-                store_row<V>(a.dgate, a.out_bf16, row * a.lddg + c, dg);
-                if (row == g.start) {
-                    if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
-                    g.previous(a);
-                }
+                store_pieces<W, P>(a.out, a.out_bf16, row * a.ldo + c.first, c, d);
+                store_pieces<W, P>(a.dgate, a.out_bf16, row * a.lddg + c.first, c, dg);
             }
+            if (q0 - N >= r0) copy_inputs(k ^ flip, q0 - 1 - k);           // row N - 1 - k of the stretch ahead
+            end_of_row();
         }
     }
+    if (a.first_grad && r0 == g.start) store_state(a.first_grad, a, g.b, c, carry);
 }
 
 // Graphs without rows: their last state is the first one (going back, the same for the gradients).  Columns c0 .. c1 - 1, warp `warp` of `warps`.
@@ -362,13 +527,14 @@ __device__ __forceinline__ void find_graphs(const ScanArgs& a, int32_t chunk0, i
     __syncthreads();
 }
 
-template <typename TI, int V, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(kScanBlock) recurrence_sums(const __grid_constant__ ScanArgs a)
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
+__global__ void __launch_bounds__(kRowsBlock) recurrence_sums(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
-    __shared__ float2 shared[kScanBlock * V];
-    __shared__ int32_t graph[kScanBlock];
-    const int lane = threadIdx.x % a.lanes, way = threadIdx.x / a.lanes, vec = blockIdx.y * a.lanes + lane, c = vec * V;
+    constexpr int V = W * P, kRing = Pair<TI, W, P, kRowsBlock>::kBytes, kMaps = kRowsBlock * V * (int)sizeof(float2);
+    __shared__ __align__(16) char ring[kRing > kMaps ? kRing : kMaps];       // rows on their way, then the chunks' maps
+    __shared__ int32_t graph[kRowsBlock];
+    const int lane = threadIdx.x % a.lanes, way = threadIdx.x / a.lanes, place = blockIdx.y * a.lanes + lane;
     const int32_t used = rows_used(a), chunk0 = blockIdx.x * a.ways, chunk = chunk0 + way;
     find_graphs<BACK>(a, chunk0, a.ways, used, graph);
     const int64_t r0 = (int64_t)chunk * a.chunk_rows;
@@ -376,62 +542,67 @@ __global__ void __launch_bounds__(kScanBlock) recurrence_sums(const __grid_const
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
-    if (r0 < r1 && vec < a.nvec) {
+    Columns<W, P> c;
+    c.at(a, place);
+    if (r0 < r1 && place < a.places) {
         Graph g;
         g.at(a, graph[way]);
-        chunk_map<TI, V, SIGMOID, BACK, sizeof(TI) == 4 && V == 4 ? 4 : 8>(a, (int32_t)r0, r1, c, g, map);
-        if (vec == 0) a.chunk_graph[chunk] = g.b;
+        chunk_map<TI, W, P, kRowsBlock, SIGMOID, BACK>(a, ring, (int32_t)r0, r1, c, g, map);
+        if (place == 0) a.chunk_graph[chunk] = g.b;
     }
-    join_chunks<V, BACK>(shared, lane, way, a.lanes, a.ways, map, ahead, whole);
-    if (vec < a.nvec) {
-        if (chunk < a.chunks)
+    __syncthreads();
+    join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, a.lanes, a.ways, map, ahead, whole);
+    if (place < a.places)
 #pragma unroll
-            for (int i = 0; i < V; ++i) a.chunk_map[(int64_t)chunk * a.f + c + i] = ahead[i];
-        if (way == (BACK ? 0 : a.ways - 1))
+        for (int k = 0; k < P; ++k)
+            if (c.has(k))
 #pragma unroll
-            for (int i = 0; i < V; ++i) a.tile_map[(int64_t)blockIdx.x * a.f + c + i] = whole[i];
-    }
-    empty_graphs<BACK>(a, blockIdx.y * a.lanes * V, min((int)(blockIdx.y + 1) * a.lanes * V, a.f), (int64_t)blockIdx.x * (kScanBlock / 32) + (threadIdx.x >> 5),
-                       (int64_t)gridDim.x * (kScanBlock / 32));
+                for (int i = 0; i < W; ++i) {
+                    if (chunk < a.chunks) a.chunk_map[(int64_t)chunk * a.f + c.column(k, i)] = ahead[k * W + i];
+                    if (way == (BACK ? 0 : a.ways - 1)) a.tile_map[(int64_t)blockIdx.x * a.f + c.column(k, i)] = whole[k * W + i];
+                }
+    const int share = (a.f + gridDim.y - 1) / gridDim.y, c0 = blockIdx.y * share;
+    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), (int64_t)blockIdx.x * (kRowsBlock / 32) + (threadIdx.x >> 5), (int64_t)gridDim.x * (kRowsBlock / 32));
 }
 
-// From tile to tile: 32 ways a column take a share of the tiles each, first to its map, then from the state that it starts with.
+// From tile to tile: 32 ways a column take a share of the tiles each, first to its map, then, from the state that it starts with, to the tiles' states.
 template <bool BACK>
 __global__ void __launch_bounds__(1024) recurrence_carry(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
+    constexpr int U = 8;
     __shared__ float2 shared[32][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), way = threadIdx.x >> 5;
-    const int share = (a.tiles + 31) / 32, t0 = min(way * share, a.tiles), t1 = min(t0 + share, a.tiles);
-    float2 map = make_float2(1.f, 0.f);
+    const int lane = threadIdx.x & 31, way = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    const int share = (a.tiles + 31) / 32, t0 = min(way * share, a.tiles), t1 = c < a.f ? min(t0 + share, a.tiles) : t0;
     auto tile = [&](int k) { return (int64_t)(BACK ? a.tiles - 1 - k : k) * a.f + c; };
-    auto load_map = [&](int k) {
-        float2 m;
-        asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(m.x), "=f"(m.y) : "l"(a.tile_map + tile(k)));
-        return m;
+    float2 m[U], map = make_float2(1.f, 0.f);
+    auto load = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (k + u < t1) asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(m[u].x), "=f"(m[u].y) : "l"(a.tile_map + tile(k + u)));
     };
-    if (c < a.f)
-        for (int k = t0; k < t1; k += 8) {
-            float2 m[8];
+    for (int k = t0; k < t1; k += U) {
+        load(k);
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + u < t1) m[u] = load_map(k + u);
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + u < t1) map = joined(map, m[u]);
-        }
-    shared[way][threadIdx.x & 31] = map;
+        for (int u = 0; u < U; ++u)
+            if (k + u < t1) map = joined(map, m[u]);
+    }
+    shared[way][lane] = map;
     __syncthreads();
-    if (c >= a.f) return;
-    float s = 0.f;
-    for (int q = 0; q < way; ++q) s = applied(shared[q][threadIdx.x & 31], s);
-    for (int k = t0; k < t1; k += 8) {
-        float2 m[8];
+    map = shared[lane][way];                                   // a warp joins the ways of a column
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (k + u < t1) m[u] = load_map(k + u);
+    for (int o = 1; o < 32; o *= 2) {
+        const float2 before = make_float2(__shfl_up_sync(0xffffffffu, map.x, o), __shfl_up_sync(0xffffffffu, map.y, o));
+        if (lane >= o) map = joined(before, map);
+    }
+    const float start = __shfl_up_sync(0xffffffffu, map.y, 1);
+    shared[lane][way].y = lane == 0 ? 0.f : start;
+    __syncthreads();
+    float s = shared[way][lane].y;
+    for (int k = t0; k < t1; k += U) {
+        if (share > U) load(k);                                 // (a single batch is still there)
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < U; ++u)
             if (k + u < t1) {
                 a.carry[tile(k + u)] = s;
                 s = applied(m[u], s);
@@ -439,57 +610,80 @@ __global__ void __launch_bounds__(1024) recurrence_carry(const __grid_constant__
     }
 }
 
-template <typename TI, int V, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(kScanBlock) recurrence_rows(const __grid_constant__ ScanArgs a)
+// The state (gradient) that a thread's chunk starts with, and its graph.
+template <int W, int P, bool BACK>
+__device__ __forceinline__ void chunk_start(const ScanArgs& a, int64_t chunk, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph& g, float (&s)[W * P])
+{
+    if (!a.carry) {
+        g.at(a, (BACK ? r1 - 1 : r0) / a.length);
+        return;                                                 // (chunks are whole graphs)
+    }
+    g.at(a, a.chunk_graph[chunk]);
+    const int64_t tile = chunk / a.tile_chunks;
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            s[k * W + i] = c.has(k) ? applied(a.chunk_map[chunk * a.f + c.column(k, i)], a.carry[tile * a.f + c.column(k, i)]) : 0.f;
+}
+
+// The blocks go from the last rows to the first: what `recurrence_sums` has read last is still in L2.
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
+__global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_rows(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
-    const int64_t at = (int64_t)blockIdx.x * kScanBlock + threadIdx.x, chunk = at / a.nvec;
-    const int c = (int)(at - chunk * a.nvec) * V;
-    const int32_t used = rows_used(a);
+    constexpr int V = W * P, THREADS = BACK ? kGradBlock : kRowsBlock;
+    __shared__ __align__(16) char ring[BACK ? GradPlaces<W, P, THREADS>::kBytes : Pair<TI, W, P, THREADS>::kBytes];
+    const int64_t at = (int64_t)(gridDim.x - 1 - blockIdx.x) * THREADS + threadIdx.x, chunk = at / a.places;
+    Columns<W, P> c;
+    c.at(a, (int)(at - chunk * a.places));
     const int64_t r0 = chunk * a.chunk_rows;
-    const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)used);
+    const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)rows_used(a));
     if (r0 >= r1) return;
-    float s[V];
+    float s[V] = {};
     Graph g;
-    if (a.carry) {
-        g.at(a, a.chunk_graph[chunk]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = applied(a.chunk_map[chunk * a.f + c + i], a.carry[chunk / a.tile_chunks * a.f + c + i]);
-    } else {
-        g.at(a, (int32_t)(BACK ? r1 - 1 : r0) / a.length);
-    }
-    if constexpr (BACK) backward_rows<TI, V, SIGMOID>(a, (int32_t)r0, r1, c, g, s);
-    else forward_rows<TI, V, SIGMOID, sizeof(TI) == 4 && V == 4 ? 4 : 8>(a, (int32_t)r0, r1, c, g, s);
+    chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
+    if constexpr (BACK) backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
+    else forward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
 }
 
 // All rows of some columns in one block.
-template <typename TI, int V, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(kFusedLanes * kFusedWays) recurrence_few(const __grid_constant__ ScanArgs a)
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
+__global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
-    __shared__ float2 shared[kFusedLanes * kFusedWays * V];
-    __shared__ int32_t graph[kFusedWays];
-    const int lane = threadIdx.x % kFusedLanes, way = threadIdx.x / kFusedLanes, vec = blockIdx.x * kFusedLanes + lane, c = vec * V;
+    constexpr int V = W * P, LANES = Few<BACK>::kLanes, WAYS = Few<BACK>::kWays, THREADS = Few<BACK>::kThreads;
+    constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? GradPlaces<W, P, THREADS>::kBytes : kRing;
+    constexpr int kMost = kRing > kMaps ? kRing : kMaps;
+    __shared__ __align__(16) char ring[kMost > kWalk ? kMost : kWalk];        // rows on their way, the chunks' maps, rows again
+    __shared__ int32_t graph[WAYS];
+    const int lane = threadIdx.x % LANES, way = threadIdx.x / LANES, place = blockIdx.x * LANES + lane;
     const int32_t used = rows_used(a), r0 = way * a.chunk_rows, r1 = min(r0 + a.chunk_rows, used);
-    find_graphs<BACK>(a, 0, kFusedWays, used, graph);
-    const bool some = r0 < r1 && vec < a.nvec;
+    find_graphs<BACK>(a, 0, WAYS, used, graph);
+    const bool some = r0 < r1 && place < a.places;
+    Columns<W, P> c;
+    c.at(a, place);
     Graph g;
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
     if (some) {
         g.at(a, graph[way]);
-        chunk_map<TI, V, SIGMOID, BACK, 4>(a, r0, r1, c, g, map);
+        chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, ring, r0, r1, c, g, map);
     }
-    join_chunks<V, BACK>(shared, lane, way, kFusedLanes, kFusedWays, map, ahead, whole);
+    __syncthreads();
+    join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, LANES, WAYS, map, ahead, whole);
+    __syncthreads();
     if (some) {
         float s[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = ahead[i].y;         // (nothing is ahead of the first row but its graph's own state)
-        if constexpr (BACK) backward_rows<TI, V, SIGMOID>(a, r0, r1, c, g, s);
-        else forward_rows<TI, V, SIGMOID, 4>(a, r0, r1, c, g, s);
+        g.at(a, graph[way]);
+        if constexpr (BACK) backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
+        else forward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
     }
-    empty_graphs<BACK>(a, blockIdx.x * kFusedLanes * V, min((int)(blockIdx.x + 1) * kFusedLanes * V, a.f), threadIdx.x >> 5, kFusedLanes * kFusedWays / 32);
+    const int share = (a.f + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * share;
+    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), threadIdx.x >> 5, THREADS / 32);
 }
 
 // ------------------------------------------------------------------ host side
@@ -512,11 +706,11 @@ static ScanPlan plan_scan(int64_t n, int32_t f, int64_t graphs, bool equal, bool
         p.chunks = graphs;
         return p;
     }
-    if (n <= kFusedRows) {
+    if (n <= kFewRows) {
         p.few = true;
-        const int64_t rows = (n + kFusedWays - 1) / kFusedWays, unit = back ? kStateRows : 4;
+        const int64_t ways = back ? Few<true>::kWays : Few<false>::kWays, rows = (n + ways - 1) / ways, unit = back ? kStateRows : 4;
         p.chunk_rows = (int32_t)((rows < 1 ? 1 : rows) + unit - 1) / unit * unit;
-        p.chunks = kFusedWays;
+        p.chunks = ways;
         return p;
     }
     // Long chunks cost fewer maps (24 bytes for a column of each), short ones give the chip more threads.
@@ -545,29 +739,36 @@ static int check_scan(int64_t n, int32_t f, int form, int64_t graphs, const void
     return GNNFD_OK;
 }
 
-template <typename TI, int V, bool SIGMOID, bool BACK>
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
 static void launch_sums(ScanArgs& a, cudaStream_t s)
 {
-    const dim3 grid((unsigned)a.tiles, (unsigned)((a.nvec + a.lanes - 1) / a.lanes));
-    GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, V, SIGMOID, BACK>), grid, kScanBlock, 0, a);
+    a.places = (a.f / W + P - 1) / P;
+    // 32 lanes of a row, or as many as waste no more than an eighth of them, down to 8
+    a.lanes = 32;
+    while (a.lanes > 8 && (a.places + a.lanes - 1) / a.lanes * a.lanes * 7 > a.places * 8) a.lanes /= 2;
+    a.ways = a.tile_chunks = kRowsBlock / a.lanes;
+    a.tiles = (a.chunks + a.ways - 1) / a.ways;
+    const dim3 grid((unsigned)a.tiles, (unsigned)((a.places + a.lanes - 1) / a.lanes));
+    GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, W, P, SIGMOID, BACK>), grid, kRowsBlock, 0, a);
     GNNFD_LAUNCH("recurrence_carry", s, recurrence_carry<BACK>, (unsigned)((a.f + 31) / 32), 1024, 0, a);
 }
-template <typename TI, int V, bool SIGMOID, bool BACK>
-static void launch_rows(const ScanArgs& a, cudaStream_t s)
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
+static void launch_rows(ScanArgs& a, bool few, cudaStream_t s)
 {
-    const int64_t threads = (int64_t)a.chunks * a.nvec;
-    GNNFD_LAUNCH("recurrence_rows", s, (recurrence_rows<TI, V, SIGMOID, BACK>), (unsigned)((threads + kScanBlock - 1) / kScanBlock), kScanBlock, 0, a);
-}
-template <typename TI, int V, bool SIGMOID, bool BACK>
-static void launch_few(const ScanArgs& a, cudaStream_t s)
-{
-    GNNFD_LAUNCH("recurrence_few", s, (recurrence_few<TI, V, SIGMOID, BACK>), (unsigned)((a.nvec + kFusedLanes - 1) / kFusedLanes), kFusedLanes * kFusedWays, 0, a);
+    a.places = (a.f / W + P - 1) / P;
+    if (few) {
+        GNNFD_LAUNCH("recurrence_few", s, (recurrence_few<TI, W, P, SIGMOID, BACK>), (unsigned)((a.places + Few<BACK>::kLanes - 1) / Few<BACK>::kLanes),
+                     Few<BACK>::kThreads, 0, a);
+        return;
+    }
+    const int64_t threads = (int64_t)a.chunks * a.places, block = BACK ? kGradBlock : kRowsBlock;
+    GNNFD_LAUNCH("recurrence_rows", s, (recurrence_rows<TI, W, P, SIGMOID, BACK>), (unsigned)((threads + block - 1) / block), (unsigned)block, 0, a);
 }
 
 template <typename TI, bool SIGMOID, bool BACK>
 static int run_scan(ScanArgs& a, const ScanPlan& p, cudaStream_t s)
 {
-    // Vectors of 4 elements where all rows allow it; the gradient's walk keeps two values per element of 16 rows, so its vectors are of 2 at most.
+    // Pieces as wide as all rows allow, up to 16 bytes; threads have 4 elements of a row at least.
     const int xs = sizeof(TI), os = a.out_bf16 ? 2 : 4;
     auto widest = [&](int v, bool rows) {
         while (v > 1 && !(a.f % v == 0 && rows_fit(a.gate, a.ldg, xs, v) && (!(rows || !BACK) || rows_fit(a.x, a.ldx, xs, v)) &&
@@ -578,30 +779,19 @@ static int run_scan(ScanArgs& a, const ScanPlan& p, cudaStream_t s)
     };
     a.chunk_rows = p.chunk_rows;
     a.chunks = (int32_t)p.chunks;
-    const int rows = widest(BACK ? 2 : 4, true);
-    auto for_rows = [&](auto f) {
-        a.nvec = a.f / rows;
-        if (rows == 4) { if constexpr (!BACK) f(std::integral_constant<int, 4>()); }
-        else if (rows == 2) f(std::integral_constant<int, 2>());
-        else f(std::integral_constant<int, 1>());
-    };
-    if (p.few) {
-        for_rows([&](auto v) { launch_few<TI, decltype(v)::value, SIGMOID, BACK>(a, s); });
-    } else {
-        if (!p.direct) {
-            const int sums = widest(4, false);
-            a.nvec = a.f / sums;
-            // 32 lanes of a row, or as many as waste no more than an eighth of them, down to 8
-            a.lanes = 32;
-            while (a.lanes > 8 && (a.nvec + a.lanes - 1) / a.lanes * a.lanes * 7 > a.nvec * 8) a.lanes /= 2;
-            a.ways = a.tile_chunks = kScanBlock / a.lanes;
-            a.tiles = (int32_t)((p.chunks + a.ways - 1) / a.ways);
-            if (sums == 4) launch_sums<TI, 4, SIGMOID, BACK>(a, s);
-            else if (sums == 2) launch_sums<TI, 2, SIGMOID, BACK>(a, s);
-            else launch_sums<TI, 1, SIGMOID, BACK>(a, s);
-        }
-        for_rows([&](auto v) { launch_rows<TI, decltype(v)::value, SIGMOID, BACK>(a, s); });
+    if (!p.few && !p.direct) {
+        with_vector<TI>(widest(16 / xs, false), [&](auto w) {
+            constexpr int W = decltype(w)::value;
+            launch_sums<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, s);
+            return 0;
+        });
     }
+    // (the gradient's walk has no wider threads than of 4 elements: its shared memory)
+    with_vector<TI>(widest(BACK ? 4 : 16 / xs, true), [&](auto w) {
+        constexpr int W = decltype(w)::value < 4 || !BACK ? decltype(w)::value : 4;
+        launch_rows<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, p.few, s);
+        return 0;
+    });
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
 }
