@@ -43,7 +43,7 @@ struct ScanArgs {
     int64_t ldx, ldg, ldd, ldo, lddg;
     int32_t n, graphs, length, f, ptr64, out_bf16;
     int32_t places;                              // threads that share a row: see Columns
-    int32_t chunk_rows, chunks, tiles, tile_chunks, lanes, ways;
+    int32_t chunk_rows, chunks, tiles, tile_chunks, lanes, ways, column_tiles;
 };
 
 __device__ __forceinline__ float power_of_2(float x)
@@ -58,31 +58,57 @@ __device__ __forceinline__ float one_over(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// The smaller one of a = 1 / (1 + e^-g) and 1 - a, with g's sign: both come from it without cancellation.
-__device__ __forceinline__ float smaller_part(float g)
+// a and 1 - a of a = 1 / (1 + e^-g), neither by subtraction, and `small`, the smaller one with g's sign, from which `sigmoid_parts` has both again
+template <int V>
+__device__ __forceinline__ void sigmoid_of(const float (&g)[V], float (&a)[V], float (&rest)[V], float (&small)[V])
 {
-    const float e = power_of_2(-1.4426950408889634f * fabsf(g));
-    return copysignf(e * one_over(1.f + e), g);
+    float t[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = g[i];
+    scale(t, 1.4426950408889634f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) a[i] = small[i] = power_of_2(-fabsf(t[i]));
+    const float one[1] = {-1.f};
+    add_minus(a, one);
+#pragma unroll
+    for (int i = 0; i < V; ++i) a[i] = one_over(a[i]);
+    multiply(small, a);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const bool negative = g[i] < 0.f;
+        rest[i] = negative ? a[i] : small[i];
+        a[i] = negative ? small[i] : a[i];
+    }
 }
-__device__ __forceinline__ void sigmoid_parts(float smaller, float& a, float& rest)
+__device__ __forceinline__ void sigmoid_parts(float signed_small, float& a, float& rest)
 {
-    const float small = fabsf(smaller), large = 1.f - small;
-    const bool negative = __float_as_uint(smaller) >> 31;
+    const float small = fabsf(signed_small), large = 1.f - small;
+    const bool negative = __float_as_uint(signed_small) >> 31;
     a = negative ? small : large;
     rest = negative ? large : small;
 }
 // a and b of a row
-template <bool SIGMOID>
-__device__ __forceinline__ void step_of(float g, float x, float& a, float& b)
+template <bool SIGMOID, int V>
+__device__ __forceinline__ void steps_of(const float (&g)[V], const float (&x)[V], float (&a)[V], float (&b)[V])
 {
     if constexpr (SIGMOID) {
-        float rest;
-        sigmoid_parts(smaller_part(g), a, rest);
-        b = rest * x;
+        float small[V];
+        sigmoid_of(g, a, b, small);
+        multiply(b, x);
     } else {
-        a = g;
-        b = x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            a[i] = g[i];
+            b[i] = x[i];
+        }
     }
+}
+// x = a * x + b
+template <int V>
+__device__ __forceinline__ void step(float (&x)[V], const float (&a)[V], const float (&b)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; i += 2) scale_shift_pair(x[i], x[i + 1], a[i], a[i + 1], b[i], b[i + 1]);
 }
 // the state behind a map (products beyond the type's range do not matter to a state of 0)
 __device__ __forceinline__ float applied(float2 map, float s) { return map.x != map.x || s == 0.f ? map.y : fmaf(map.x, s, map.y); }
@@ -146,21 +172,18 @@ struct Graph {
     }
 };
 
-// The columns of a thread: P pieces of W neighbouring ones, `step` columns apart (so that the threads of a row read neighbouring pieces), of which
-// the first `pieces` exist.
+// The columns of a thread: P pieces of W neighbouring ones, `step` columns apart (so that the threads of a row read neighbouring pieces).  Where the row
+// ends ahead of a piece the thread has its first one again: the same values from and to the same places.
 template <int W, int P>
 struct Columns {
-    int first, step, pieces;
-    __device__ __forceinline__ void at(const ScanArgs& a, int place)
+    int first, off[P];
+    __device__ __forceinline__ void at(const ScanArgs& a, int first_column, int step)
     {
-        first = place * W;
-        step = a.places * W;
-        pieces = P;
-        if constexpr (P > 1)
-            while (pieces > 0 && first + (pieces - 1) * step >= a.f) --pieces;
+        first = first_column;
+#pragma unroll
+        for (int k = 0; k < P; ++k) off[k] = P > 1 && first + k * step < a.f ? k * step : 0;
     }
-    __device__ __forceinline__ bool has(int p) const { return P == 1 || p < pieces; }
-    __device__ __forceinline__ int column(int p, int i) const { return first + p * step + i; }
+    __device__ __forceinline__ int column(int p, int i) const { return first + off[p] + i; }
 };
 
 // Rows on their way into shared memory.  Every thread copies the pieces of its own columns into places of its own and reads them from there, so nobody waits
@@ -210,13 +233,11 @@ struct Pair {
     __device__ __forceinline__ static void copy(char* slot, const TI* first, const TI* second, const Columns<W, P>& c)
     {
 #pragma unroll
-        for (int k = 0; k < P; ++k)
-            if (c.has(k)) {
-                copy_piece<TI, W>(slot + k * kPiece, first + k * c.step);
-                copy_piece<TI, W>(slot + (P + k) * kPiece, second + k * c.step);
-            }
+        for (int k = 0; k < P; ++k) {
+            copy_piece<TI, W>(slot + k * kPiece, first + c.off[k]);
+            copy_piece<TI, W>(slot + (P + k) * kPiece, second + c.off[k]);
+        }
     }
-    // (pieces that do not exist: whatever lies there, for columns that are not written)
     __device__ __forceinline__ static void read(const char* slot, float (&x)[W * P], float (&y)[W * P])
     {
 #pragma unroll
@@ -227,51 +248,68 @@ struct Pair {
     }
 };
 
-// work(row, a row of the first matrix, of the second) for `rows` rows from r on (BACK: towards the first).
-template <typename TI, int W, int P, int THREADS, bool BACK, typename F>
-__device__ __forceinline__ void stream_rows(char* ring, const TI* first, int64_t ld_first, const TI* second, int64_t ld_second, int32_t r, int32_t rows,
-                                            const Columns<W, P>& c, F work)
-{
+// Rows r, r + 1, .. (BACK: r, r - 1, ..) of two matrices, one after the other: `start` sends for the first ones, `run` does work(row, a row of the first
+// matrix, of the second).
+template <typename TI, int W, int P, int THREADS, bool BACK>
+struct Stream {
     using Rows = Pair<TI, W, P, THREADS>;
-    char* const place = ring + threadIdx.x * (W * (int)sizeof(TI));
-    first += r * ld_first + c.first;
-    second += r * ld_second + c.first;
-    if (BACK) {
-        ld_first = -ld_first;
-        ld_second = -ld_second;
-    }
+    char* place;
+    const TI *first, *second;
+    int64_t ld_first, ld_second;
+    int32_t r, rows;
+    __device__ __forceinline__ void start(char* ring, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r_,
+                                          int32_t rows_, const Columns<W, P>& c)
+    {
+        place = ring + threadIdx.x * (W * (int)sizeof(TI));
+        r = r_;
+        rows = rows_;
+        first = static_cast<const TI*>(first_) + r * ld_first_ + c.first;
+        second = static_cast<const TI*>(second_) + r * ld_second_ + c.first;
+        ld_first = BACK ? -ld_first_ : ld_first_;
+        ld_second = BACK ? -ld_second_ : ld_second_;
 #pragma unroll
-    for (int k = 0; k < Rows::kAhead; ++k) {
-        if (k < rows) Rows::copy(place + k * Rows::kRow, first, second, c);
-        end_of_row();
-        first += ld_first;
-        second += ld_second;
+        for (int k = 0; k < Rows::kAhead; ++k) {
+            if (k < rows) Rows::copy(place + k * Rows::kRow, first, second, c);
+            end_of_row();
+            first += ld_first;
+            second += ld_second;
+        }
     }
-    int at = 0;
+    template <typename F>
+    __device__ __forceinline__ void run(const Columns<W, P>& c, F work)
+    {
+        int at = 0;
 #pragma unroll 1
-    for (int32_t k = 0; k < rows; ++k, r += BACK ? -1 : 1) {
-        float x[W * P], y[W * P];
-        all_but_last<Rows::kAhead - 1>();
-        Rows::read(place + at, x, y);
-        work(r, x, y);
-        if (k + Rows::kAhead < rows) Rows::copy(place + at, first, second, c);
-        end_of_row();
-        first += ld_first;
-        second += ld_second;
-        at = (at + Rows::kRow) & (Rows::kBytes - 1);
+        for (int32_t k = 0; k < rows; ++k, r += BACK ? -1 : 1) {
+            float x[W * P], y[W * P];
+            all_but_last<Rows::kAhead - 1>();
+            Rows::read(place + at, x, y);
+            work(r, x, y);
+            if (k + Rows::kAhead < rows) Rows::copy(place + at, first, second, c);
+            end_of_row();
+            first += ld_first;
+            second += ld_second;
+            at = (at + Rows::kRow) & (Rows::kBytes - 1);
+        }
     }
-}
+};
 
+// `at`: of the row's first piece
 template <int W, int P>
 __device__ __forceinline__ void store_pieces(void* out, int bf16, int64_t at, const Columns<W, P>& c, const float (&x)[W * P])
 {
+    auto put = [&](auto* p) {
+        using TO = typename std::remove_pointer<decltype(p)>::type;
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        float v[W];
+        for (int k = 0; k < P; ++k) {
+            float v[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = x[k * W + i];
-        if (c.has(k)) store_row<W>(out, bf16, at + k * c.step, v);
-    }
+            for (int i = 0; i < W; ++i) v[i] = x[k * W + i];
+            store_packed<TO, W>(p + c.off[k], v);
+        }
+    };
+    if (bf16) put(static_cast<__nv_bfloat16*>(out) + at);
+    else put(static_cast<float*>(out) + at);
 }
 // one row of fp32 [.., f], at any alignment; zeros where there is no array
 template <int W, int P>
@@ -280,70 +318,73 @@ __device__ __forceinline__ void load_state(const float* p, const ScanArgs& a, in
 #pragma unroll
     for (int k = 0; k < P; ++k)
 #pragma unroll
-        for (int i = 0; i < W; ++i) s[k * W + i] = p && c.has(k) ? load4(p + row * a.f + c.column(k, i)) : 0.f;
+        for (int i = 0; i < W; ++i) s[k * W + i] = p ? load4(p + row * a.f + c.column(k, i)) : 0.f;
 }
 template <int W, int P>
 __device__ __forceinline__ void store_state(float* p, const ScanArgs& a, int64_t row, const Columns<W, P>& c, const float (&s)[W * P])
 {
 #pragma unroll
     for (int k = 0; k < P; ++k)
-        if (c.has(k))
 #pragma unroll
-            for (int i = 0; i < W; ++i) p[row * a.f + c.column(k, i)] = s[k * W + i];
+        for (int i = 0; i < W; ++i) p[row * a.f + c.column(k, i)] = s[k * W + i];
 }
 
-// The map over rows r0 .. r1 - 1; `g` is the graph of r0 (going back, of r1 - 1).
+// The map over rows r0 .. r1 - 1, for which `stream` has been started; `g` is the graph of r0 (going back, of r1 - 1).
 template <typename TI, int W, int P, int THREADS, bool SIGMOID, bool BACK>
-__device__ __forceinline__ void chunk_map(const ScanArgs& a, char* ring, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float2 (&map)[W * P])
+__device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, THREADS, BACK>& stream, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g,
+                                          float2 (&map)[W * P])
 {
     constexpr int V = W * P;
+    float product[V], state[V];
     auto cut = [&] {                                             // (from its graph's own state)
-        float s[V];
-        load_state(BACK ? a.last_grad : a.first, a, g.b, c, s);
+        load_state(BACK ? a.last_grad : a.first, a, g.b, c, state);
 #pragma unroll
-        for (int i = 0; i < V; ++i) map[i] = make_float2(__uint_as_float(0x7fffffffu), s[i]);
+        for (int i = 0; i < V; ++i) product[i] = __uint_as_float(0x7fffffffu);
     };
 #pragma unroll
-    for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
+    for (int i = 0; i < V; ++i) {
+        product[i] = 1.f;
+        state[i] = 0.f;
+    }
     if (BACK ? r1 == g.end : r0 == g.start) cut();
-    stream_rows<TI, W, P, THREADS, BACK>(ring, static_cast<const TI*>(a.gate), a.ldg, static_cast<const TI*>(BACK ? a.dout : a.x), BACK ? a.ldd : a.ldx,
-                                         BACK ? r1 - 1 : r0, r1 - r0, c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
+    stream.run(c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
         if (BACK ? row + 1 == g.start : row == g.end) {
             if (BACK) g.previous(a);
             else g.next(a);
             cut();
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float w, b;
-            step_of<SIGMOID>(gate[i], value[i], w, b);
-            map[i].x *= w;
-            map[i].y = BACK ? w * (map[i].y + value[i]) : fmaf(w, map[i].y, b);
+        float w[V], b[V];
+        steps_of<SIGMOID>(gate, value, w, b);
+        multiply(product, w);
+        if constexpr (BACK) {
+            add_all(state, value);
+            multiply(state, w);
+        } else {
+            step(state, w, b);
         }
     });
+#pragma unroll
+    for (int i = 0; i < V; ++i) map[i] = make_float2(product[i], state[i]);
 }
 
 // The rows themselves, from the state h on.
 template <typename TI, int W, int P, int THREADS, bool SIGMOID>
-__device__ __forceinline__ void forward_rows(const ScanArgs& a, char* ring, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float (&h)[W * P])
+__device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P, THREADS, false>& stream, int32_t r0, int32_t r1, const Columns<W, P>& c,
+                                             Graph g, float (&h)[W * P])
 {
     constexpr int V = W * P;
     if (r0 == g.start) load_state(a.first, a, g.b, c, h);
     int64_t at = r0 * a.ldo + c.first;
-    stream_rows<TI, W, P, THREADS, false>(ring, static_cast<const TI*>(a.gate), a.ldg, static_cast<const TI*>(a.x), a.ldx, r0, r1 - r0, c,
-                                          [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
+    stream.run(c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
         if (row == g.end) {
             if (a.last) store_state(a.last, a, g.b, c, h);
             g.next(a);
             load_state(a.first, a, g.b, c, h);
         }
         if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float w, b;
-            step_of<SIGMOID>(gate[i], value[i], w, b);
-            h[i] = fmaf(w, h[i], b);
-        }
+        float w[V], b[V];
+        steps_of<SIGMOID>(gate, value, w, b);
+        step(h, w, b);
         store_pieces<W, P>(a.out, a.out_bf16, at, c, h);
         at += a.ldo;
     });
@@ -358,12 +399,13 @@ __device__ __forceinline__ void write_piece(char* to, const float* x)
     else *reinterpret_cast<float*>(to) = x[0];
 }
 
-// What the threads of the gradient's walk have in shared memory: places of W fp32 values for each thread and piece of kStateRows rows of gates, x and dout.  Gates
-// and x are replaced there by what the way back needs: the weight of the row's step and the factor of G in dgate.
-template <int W, int P, int THREADS>
+// What the threads of the gradient's walk have in shared memory: places of W fp32 values for each thread and piece of kStateRows rows of gates and x, and
+// kStateRows rows of dout as they are.  Gates and x are replaced there by what the way back needs: the weight of the row's step and the factor of G in dgate.
+template <typename TI, int W, int P, int THREADS>
 struct GradPlaces {
-    static constexpr int kPiece = THREADS * W * 4, kRow = 3 * P * kPiece, kBytes = kStateRows * kRow;
-    enum { kGate = 0, kX = P, kDout = 2 * P };
+    static constexpr int kPiece = THREADS * W * 4, kX = P * kPiece, kRow = 2 * P * kPiece;                  // of gates and x
+    static constexpr int kDoutPiece = THREADS * W * (int)sizeof(TI), kDoutRow = P * kDoutPiece, kDout = kStateRows * kRow;
+    static constexpr int kBytes = kDout + kStateRows * kDoutRow;
 };
 
 // The gradients of the rows, from what arrives behind the last one on; r0 is a multiple of kStateRows.  Rows are taken kStateRows at a time: forward from the
@@ -373,26 +415,29 @@ template <typename TI, int W, int P, int THREADS, bool SIGMOID>
 __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float (&carry)[W * P])
 {
     constexpr int V = W * P, N = kStateRows;
-    using Pl = GradPlaces<W, P, THREADS>;
+    using Pl = GradPlaces<TI, W, P, THREADS>;
+    char* const grads = places + Pl::kDout + threadIdx.x * (W * (int)sizeof(TI));
     places += threadIdx.x * (W * 4);
-    const TI *const gates = static_cast<const TI*>(a.gate) + c.first, *const in = static_cast<const TI*>(a.x) + c.first,
-             *const douts = static_cast<const TI*>(a.dout) + c.first;
-    auto copy_row = [&](char* to, const TI* from) {
+    auto copy_row = [&](char* to, int piece, const TI* from) {
 #pragma unroll
-        for (int j = 0; j < P; ++j)
-            if (c.has(j)) copy_piece<TI, W>(to + j * Pl::kPiece, from + j * c.step);
-    };
-    auto copy_inputs = [&](int slot, int32_t row) {
-        copy_row(places + slot * Pl::kRow + Pl::kGate * Pl::kPiece, gates + row * a.ldg);
-        copy_row(places + slot * Pl::kRow + Pl::kX * Pl::kPiece, in + row * a.ldx);
+        for (int j = 0; j < P; ++j) copy_piece<TI, W>(to + j * piece, from + c.off[j]);
     };
     int32_t q0 = (r1 - 1) / N * N;
+    const TI *gates = static_cast<const TI*>(a.gate) + q0 * a.ldg + c.first, *in = static_cast<const TI*>(a.x) + q0 * a.ldx + c.first,
+             *douts = static_cast<const TI*>(a.dout) + (q0 + N - 1) * a.ldd + c.first;        // of the next row that is sent for
+    int64_t at = (q0 + N - 1) * a.ldo + c.first, at_gate = (q0 + N - 1) * a.lddg + c.first;
+    auto copy_inputs = [&](char* slot, bool inside) {
+        if (inside) {
+            copy_row(slot, Pl::kPiece, gates);
+            copy_row(slot + Pl::kX, Pl::kPiece, in);
+        }
+        end_of_row();
+        gates += a.ldg;
+        in += a.ldx;
+    };
     float h[V], next[V];
 #pragma unroll 1
-    for (int k = 0; k < N; ++k) {
-        if (q0 + k < r1) copy_inputs(k, q0 + k);
-        end_of_row();
-    }
+    for (int k = 0; k < N; ++k) copy_inputs(places + k * Pl::kRow, q0 + k < r1);
     load_state(a.states, a, q0 / N, c, next);
     if (r1 == g.end) load_state(a.last_grad, a, g.b, c, carry);
     // Row k of a stretch lies in slot k ^ flip: places become free on the way back, the last row's first, for the next stretch's first.
@@ -403,76 +448,90 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
         while (from.start > q0 && from.b > 0) from.previous(a);
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = next[i];
-        if (q0 - N >= r0) load_state(a.states, a, q0 / N - 1, c, next);
+        const bool more = q0 - N >= r0;
+        if (more) load_state(a.states, a, q0 / N - 1, c, next);
 #pragma unroll 1
         for (int k = 0; k < N; ++k) {
             all_but_last<N - 1>();
-            if (N - 1 - k < rows) copy_row(places + (N - 1 - k) * Pl::kRow + Pl::kDout * Pl::kPiece, douts + (q0 + N - 1 - k) * a.ldd);
+            if (N - 1 - k < rows) copy_row(grads + (N - 1 - k) * Pl::kDoutRow, Pl::kDoutPiece, douts);
             end_of_row();
+            douts -= a.ldd;
             if (k >= rows) continue;
             char* const slot = places + (k ^ flip) * Pl::kRow;
             float gate[V], value[V];
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                read_piece<TI, W>(slot + (Pl::kGate + j) * Pl::kPiece, gate + j * W);
-                read_piece<TI, W>(slot + (Pl::kX + j) * Pl::kPiece, value + j * W);
+                read_piece<TI, W>(slot + j * Pl::kPiece, gate + j * W);
+                read_piece<TI, W>(slot + Pl::kX + j * Pl::kPiece, value + j * W);
             }
             if (q0 + k == from.end) {
                 from.next(a);
                 load_state(a.first, a, from.b, c, h);
             }
+            if constexpr (SIGMOID) {
+                float w[V], rest[V], small[V], slope[V];
+                sigmoid_of(gate, w, rest, small);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float x = value[i];
-                if constexpr (SIGMOID) {
-                    float w, rest;
-                    gate[i] = smaller_part(gate[i]);
-                    sigmoid_parts(gate[i], w, rest);
-                    value[i] = (h[i] - x) * (w * rest);
-                    h[i] = fmaf(w, h[i], rest * x);
-                } else {
-                    value[i] = h[i];
-                    h[i] = fmaf(gate[i], h[i], x);
+                for (int i = 0; i < V; ++i) {
+                    gate[i] = copysignf(small[i], gate[i]);
+                    slope[i] = h[i];
                 }
+                add_minus(slope, value);
+                multiply(value, rest);
+                multiply(rest, w);
+                multiply(slope, rest);
+                step(h, w, value);
+#pragma unroll
+                for (int i = 0; i < V; ++i) value[i] = slope[i];
+            } else {
+                float was[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) was[i] = h[i];
+                step(h, gate, value);
+#pragma unroll
+                for (int i = 0; i < V; ++i) value[i] = was[i];
             }
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                write_piece<W>(slot + (Pl::kGate + j) * Pl::kPiece, gate + j * W);
-                write_piece<W>(slot + (Pl::kX + j) * Pl::kPiece, value + j * W);
+                write_piece<W>(slot + j * Pl::kPiece, gate + j * W);
+                write_piece<W>(slot + Pl::kX + j * Pl::kPiece, value + j * W);
             }
         }
+        gates -= 2 * N * a.ldg;                                  // (to the stretch ahead)
+        in -= 2 * N * a.ldx;
 #pragma unroll 1
         for (int k = N - 1; k >= 0; --k) {
             all_but_last<N - 1>();
+            char* const slot = places + (k ^ flip) * Pl::kRow;
             if (k < rows) {
-                const int32_t row = q0 + k;
-                const char* const slot = places + (k ^ flip) * Pl::kRow;
-                float d[V], keep[V], dg[V];
+                float d[V], keep[V], dg[V], w[V];
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
-                    read_piece<TI, W>(places + k * Pl::kRow + (Pl::kDout + j) * Pl::kPiece, d + j * W);
-                    read_piece<float, W>(slot + (Pl::kGate + j) * Pl::kPiece, keep + j * W);
-                    read_piece<float, W>(slot + (Pl::kX + j) * Pl::kPiece, dg + j * W);
+                    read_piece<TI, W>(grads + k * Pl::kDoutRow + j * Pl::kDoutPiece, d + j * W);
+                    read_piece<float, W>(slot + j * Pl::kPiece, keep + j * W);
+                    read_piece<float, W>(slot + Pl::kX + j * Pl::kPiece, dg + j * W);
                 }
-                if (row + 1 == g.start) {
+                if (q0 + k + 1 == g.start) {
                     if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
                     g.previous(a);
                     load_state(a.last_grad, a, g.b, c, carry);
                 }
+                add_all(d, carry);
+                multiply(dg, d);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float total = d[i] + carry[i];
-                    float w = keep[i], rest = 1.f;
-                    if constexpr (SIGMOID) sigmoid_parts(keep[i], w, rest);
-                    d[i] = SIGMOID ? rest * total : total;
-                    dg[i] *= total;
-                    carry[i] = w * total;
+                    w[i] = keep[i];
+                    if constexpr (SIGMOID) sigmoid_parts(keep[i], w[i], keep[i]);
+                    carry[i] = d[i];
                 }
-                store_pieces<W, P>(a.out, a.out_bf16, row * a.ldo + c.first, c, d);
-                store_pieces<W, P>(a.dgate, a.out_bf16, row * a.lddg + c.first, c, dg);
+                multiply(carry, w);
+                if constexpr (SIGMOID) multiply(d, keep);
+                store_pieces<W, P>(a.out, a.out_bf16, at, c, d);
+                store_pieces<W, P>(a.dgate, a.out_bf16, at_gate, c, dg);
             }
-            if (q0 - N >= r0) copy_inputs(k ^ flip, q0 - 1 - k);           // row N - 1 - k of the stretch ahead
-            end_of_row();
+            at -= a.ldo;
+            at_gate -= a.lddg;
+            copy_inputs(slot, more);                             // row N - 1 - k of the stretch ahead
         }
     }
     if (a.first_grad && r0 == g.start) store_state(a.first_grad, a, g.b, c, carry);
@@ -514,15 +573,24 @@ __device__ __forceinline__ void join_chunks(float2* shared, int lane, int way, i
     for (int i = 0; i < V; ++i) whole[i] = joined(ahead[i], map[i]);
 }
 
-// the ways' graphs: of the first row (BACK: the last one) of each chunk of a block, by whole warps
+// The ways' graphs: of the first row (BACK: the last one) of each chunk of a block.  Warps look for that of the block's first row all together, each has a look at the
+// 32 offsets that follow, and only rows behind these are looked for again.
 template <bool BACK>
 __device__ __forceinline__ void find_graphs(const ScanArgs& a, int32_t chunk0, int ways, int32_t used, int32_t* graph)
 {
-    for (int w = threadIdx.x >> 5; w < ways; w += blockDim.x >> 5) {
-        const int64_t r0 = ((int64_t)chunk0 + w) * a.chunk_rows;
-        if (r0 >= used) continue;
-        const int32_t b = graph_of_row(a, BACK ? (int32_t)min(r0 + a.chunk_rows, (int64_t)used) - 1 : (int32_t)r0);
-        if ((threadIdx.x & 31) == 0) graph[w] = b;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t row0 = (int64_t)chunk0 * a.chunk_rows;
+    if (row0 < used && warp < ways) {
+        const int32_t b0 = graph_of_row(a, (int32_t)row0);
+        const int32_t end = b0 + lane < a.graphs ? offset_of(a, b0 + lane + 1) : 0x7fffffff;
+        for (int w = warp; w < ways; w += warps) {
+            const int64_t r0 = row0 + (int64_t)w * a.chunk_rows;
+            if (r0 >= used) break;
+            const int32_t row = BACK ? (int32_t)min(r0 + a.chunk_rows, (int64_t)used) - 1 : (int32_t)r0;
+            const unsigned behind = __ballot_sync(0xffffffffu, end > row);        // the first graph that ends behind the row
+            const int32_t b = behind ? b0 + __ffs(behind) - 1 : graph_of_row(a, row);
+            if (lane == 0) graph[w] = min(b, a.graphs - 1);
+        }
     }
     __syncthreads();
 }
@@ -534,46 +602,52 @@ __global__ void __launch_bounds__(kRowsBlock) recurrence_sums(const __grid_const
     constexpr int V = W * P, kRing = Pair<TI, W, P, kRowsBlock>::kBytes, kMaps = kRowsBlock * V * (int)sizeof(float2);
     __shared__ __align__(16) char ring[kRing > kMaps ? kRing : kMaps];       // rows on their way, then the chunks' maps
     __shared__ int32_t graph[kRowsBlock];
-    const int lane = threadIdx.x % a.lanes, way = threadIdx.x / a.lanes, place = blockIdx.y * a.lanes + lane;
-    const int32_t used = rows_used(a), chunk0 = blockIdx.x * a.ways, chunk = chunk0 + way;
-    find_graphs<BACK>(a, chunk0, a.ways, used, graph);
+    // (the column tiles of the same rows side by side: rows start and end inside of the pieces of memory that are read)
+    const int lane = threadIdx.x % a.lanes, way = threadIdx.x / a.lanes, tile = blockIdx.x / a.column_tiles, across = blockIdx.x - tile * a.column_tiles;
+    const int first = (across * a.lanes * P + lane) * W;
+    const int32_t used = rows_used(a), chunk0 = tile * a.ways, chunk = chunk0 + way;
     const int64_t r0 = (int64_t)chunk * a.chunk_rows;
     const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)used);
+    const bool some = r0 < r1 && first < a.f;
+    Columns<W, P> c;
+    c.at(a, first, a.lanes * W);
+    Stream<TI, W, P, kRowsBlock, BACK> stream;
+    if (some) stream.start(ring, a.gate, a.ldg, BACK ? a.dout : a.x, BACK ? a.ldd : a.ldx, BACK ? r1 - 1 : (int32_t)r0, r1 - (int32_t)r0, c);
+    find_graphs<BACK>(a, chunk0, a.ways, used, graph);
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
-    Columns<W, P> c;
-    c.at(a, place);
-    if (r0 < r1 && place < a.places) {
+    if (some) {
         Graph g;
         g.at(a, graph[way]);
-        chunk_map<TI, W, P, kRowsBlock, SIGMOID, BACK>(a, ring, (int32_t)r0, r1, c, g, map);
-        if (place == 0) a.chunk_graph[chunk] = g.b;
+        chunk_map<TI, W, P, kRowsBlock, SIGMOID, BACK>(a, stream, (int32_t)r0, r1, c, g, map);
+        if (first == 0) a.chunk_graph[chunk] = g.b;
     }
     __syncthreads();
     join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, a.lanes, a.ways, map, ahead, whole);
-    if (place < a.places)
+    if (first < a.f)
 #pragma unroll
         for (int k = 0; k < P; ++k)
-            if (c.has(k))
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    if (chunk < a.chunks) a.chunk_map[(int64_t)chunk * a.f + c.column(k, i)] = ahead[k * W + i];
-                    if (way == (BACK ? 0 : a.ways - 1)) a.tile_map[(int64_t)blockIdx.x * a.f + c.column(k, i)] = whole[k * W + i];
-                }
-    const int share = (a.f + gridDim.y - 1) / gridDim.y, c0 = blockIdx.y * share;
-    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), (int64_t)blockIdx.x * (kRowsBlock / 32) + (threadIdx.x >> 5), (int64_t)gridDim.x * (kRowsBlock / 32));
+            for (int i = 0; i < W; ++i) {
+                if (chunk < a.chunks) a.chunk_map[(int64_t)chunk * a.f + c.column(k, i)] = ahead[k * W + i];
+                if (way == (BACK ? 0 : a.ways - 1)) a.tile_map[(int64_t)tile * a.f + c.column(k, i)] = whole[k * W + i];
+            }
+    const int share = (a.f + a.column_tiles - 1) / a.column_tiles, c0 = across * share;
+    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), (int64_t)tile * (kRowsBlock / 32) + (threadIdx.x >> 5), (int64_t)a.tiles * (kRowsBlock / 32));
 }
 
-// From tile to tile: 32 ways a column take a share of the tiles each, first to its map, then, from the state that it starts with, to the tiles' states.
+// From tile to tile: 128 ways a column take a share of the tiles each, first to its map, then, from the state that it starts with, to the tiles' states.
+// (With 32 ways 518 tiles took 10 us, waiting for three batches of loads twice.)
+constexpr int kCarryColumns = 8, kCarryWays = 128;
 template <bool BACK>
-__global__ void __launch_bounds__(1024) recurrence_carry(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(kCarryColumns * kCarryWays) recurrence_carry(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
-    constexpr int U = 8;
-    __shared__ float2 shared[32][33];
-    const int lane = threadIdx.x & 31, way = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    const int share = (a.tiles + 31) / 32, t0 = min(way * share, a.tiles), t1 = c < a.f ? min(t0 + share, a.tiles) : t0;
+    constexpr int U = 8, PER_LANE = kCarryWays / 32;
+    __shared__ float2 shared[kCarryWays][kCarryColumns + 1];
+    const int across = threadIdx.x % kCarryColumns, way = threadIdx.x / kCarryColumns, c = blockIdx.x * kCarryColumns + across;
+    const int share = (a.tiles + kCarryWays - 1) / kCarryWays, t0 = min(way * share, a.tiles), t1 = c < a.f ? min(t0 + share, a.tiles) : t0;
     auto tile = [&](int k) { return (int64_t)(BACK ? a.tiles - 1 - k : k) * a.f + c; };
     float2 m[U], map = make_float2(1.f, 0.f);
     auto load = [&](int k) {
@@ -587,18 +661,31 @@ __global__ void __launch_bounds__(1024) recurrence_carry(const __grid_constant__
         for (int u = 0; u < U; ++u)
             if (k + u < t1) map = joined(map, m[u]);
     }
-    shared[way][lane] = map;
+    shared[way][across] = map;
     __syncthreads();
-    map = shared[lane][way];                                   // a warp joins the ways of a column
+    if (threadIdx.x < 32 * kCarryColumns) {                    // a warp joins the ways of a column, each lane some neighbouring ones
+        const int lane = threadIdx.x & 31, column = threadIdx.x >> 5;
+        float2 own[PER_LANE], all = make_float2(1.f, 0.f);
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const float2 before = make_float2(__shfl_up_sync(0xffffffffu, map.x, o), __shfl_up_sync(0xffffffffu, map.y, o));
-        if (lane >= o) map = joined(before, map);
+        for (int k = 0; k < PER_LANE; ++k) {
+            own[k] = shared[lane * PER_LANE + k][column];
+            all = joined(all, own[k]);
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const float2 before = make_float2(__shfl_up_sync(0xffffffffu, all.x, o), __shfl_up_sync(0xffffffffu, all.y, o));
+            if (lane >= o) all = joined(before, all);
+        }
+        float s = __shfl_up_sync(0xffffffffu, all.y, 1);
+        if (lane == 0) s = 0.f;
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) {
+            shared[lane * PER_LANE + k][column].y = s;
+            s = applied(own[k], s);
+        }
     }
-    const float start = __shfl_up_sync(0xffffffffu, map.y, 1);
-    shared[lane][way].y = lane == 0 ? 0.f : start;
     __syncthreads();
-    float s = shared[way][lane].y;
+    float s = shared[way][across].y;
     for (int k = t0; k < t1; k += U) {
         if (share > U) load(k);                                 // (a single batch is still there)
 #pragma unroll
@@ -624,7 +711,7 @@ __device__ __forceinline__ void chunk_start(const ScanArgs& a, int64_t chunk, in
     for (int k = 0; k < P; ++k)
 #pragma unroll
         for (int i = 0; i < W; ++i)
-            s[k * W + i] = c.has(k) ? applied(a.chunk_map[chunk * a.f + c.column(k, i)], a.carry[tile * a.f + c.column(k, i)]) : 0.f;
+            s[k * W + i] = applied(a.chunk_map[chunk * a.f + c.column(k, i)], a.carry[tile * a.f + c.column(k, i)]);
 }
 
 // The blocks go from the last rows to the first: what `recurrence_sums` has read last is still in L2.
@@ -633,18 +720,24 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
 {
     grid_dependency<true>();
     constexpr int V = W * P, THREADS = BACK ? kGradBlock : kRowsBlock;
-    __shared__ __align__(16) char ring[BACK ? GradPlaces<W, P, THREADS>::kBytes : Pair<TI, W, P, THREADS>::kBytes];
+    __shared__ __align__(16) char ring[BACK ? GradPlaces<TI, W, P, THREADS>::kBytes : Pair<TI, W, P, THREADS>::kBytes];
     const int64_t at = (int64_t)(gridDim.x - 1 - blockIdx.x) * THREADS + threadIdx.x, chunk = at / a.places;
     Columns<W, P> c;
-    c.at(a, (int)(at - chunk * a.places));
+    c.at(a, (int)(at - chunk * a.places) * W, a.places * W);
     const int64_t r0 = chunk * a.chunk_rows;
     const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)rows_used(a));
     if (r0 >= r1) return;
     float s[V] = {};
     Graph g;
-    chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
-    if constexpr (BACK) backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
-    else forward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
+    if constexpr (BACK) {
+        chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
+        backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
+    } else {
+        Stream<TI, W, P, THREADS, false> stream;
+        stream.start(ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, r1 - (int32_t)r0, c);
+        chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
+        forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, (int32_t)r0, r1, c, g, s);
+    }
 }
 
 // All rows of some columns in one block.
@@ -653,23 +746,25 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
 {
     grid_dependency<true>();
     constexpr int V = W * P, LANES = Few<BACK>::kLanes, WAYS = Few<BACK>::kWays, THREADS = Few<BACK>::kThreads;
-    constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? GradPlaces<W, P, THREADS>::kBytes : kRing;
+    constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? GradPlaces<TI, W, P, THREADS>::kBytes : kRing;
     constexpr int kMost = kRing > kMaps ? kRing : kMaps;
     __shared__ __align__(16) char ring[kMost > kWalk ? kMost : kWalk];        // rows on their way, the chunks' maps, rows again
     __shared__ int32_t graph[WAYS];
     const int lane = threadIdx.x % LANES, way = threadIdx.x / LANES, place = blockIdx.x * LANES + lane;
     const int32_t used = rows_used(a), r0 = way * a.chunk_rows, r1 = min(r0 + a.chunk_rows, used);
-    find_graphs<BACK>(a, 0, WAYS, used, graph);
     const bool some = r0 < r1 && place < a.places;
     Columns<W, P> c;
-    c.at(a, place);
+    c.at(a, place * W, a.places * W);
+    Stream<TI, W, P, THREADS, BACK> stream;
+    if (some) stream.start(ring, a.gate, a.ldg, BACK ? a.dout : a.x, BACK ? a.ldd : a.ldx, BACK ? r1 - 1 : r0, r1 - r0, c);
+    find_graphs<BACK>(a, 0, WAYS, used, graph);
     Graph g;
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
     if (some) {
         g.at(a, graph[way]);
-        chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, ring, r0, r1, c, g, map);
+        chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, stream, r0, r1, c, g, map);
     }
     __syncthreads();
     join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, LANES, WAYS, map, ahead, whole);
@@ -679,8 +774,12 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = ahead[i].y;         // (nothing is ahead of the first row but its graph's own state)
         g.at(a, graph[way]);
-        if constexpr (BACK) backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
-        else forward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
+        if constexpr (BACK) {
+            backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
+        } else {
+            stream.start(ring, a.gate, a.ldg, a.x, a.ldx, r0, r1 - r0, c);
+            forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, r0, r1, c, g, s);
+        }
     }
     const int share = (a.f + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * share;
     empty_graphs<BACK>(a, c0, min(c0 + share, a.f), threadIdx.x >> 5, THREADS / 32);
@@ -748,9 +847,10 @@ static void launch_sums(ScanArgs& a, cudaStream_t s)
     while (a.lanes > 8 && (a.places + a.lanes - 1) / a.lanes * a.lanes * 7 > a.places * 8) a.lanes /= 2;
     a.ways = a.tile_chunks = kRowsBlock / a.lanes;
     a.tiles = (a.chunks + a.ways - 1) / a.ways;
-    const dim3 grid((unsigned)a.tiles, (unsigned)((a.places + a.lanes - 1) / a.lanes));
-    GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, W, P, SIGMOID, BACK>), grid, kRowsBlock, 0, a);
-    GNNFD_LAUNCH("recurrence_carry", s, recurrence_carry<BACK>, (unsigned)((a.f + 31) / 32), 1024, 0, a);
+    a.column_tiles = (a.places + a.lanes - 1) / a.lanes;
+    GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, W, P, SIGMOID, BACK>), (unsigned)(a.tiles * a.column_tiles), kRowsBlock, 0, a);
+    GNNFD_LAUNCH("recurrence_carry", s, recurrence_carry<BACK>, (unsigned)((a.f + kCarryColumns - 1) / kCarryColumns),
+                 kCarryColumns * kCarryWays, 0, a);
 }
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
 static void launch_rows(ScanArgs& a, bool few, cudaStream_t s)
@@ -779,15 +879,17 @@ static int run_scan(ScanArgs& a, const ScanPlan& p, cudaStream_t s)
     };
     a.chunk_rows = p.chunk_rows;
     a.chunks = (int32_t)p.chunks;
+    // (8 bf16 elements a thread where there are enough threads all the same)
+    const int most = xs == 2 && (int64_t)a.n * a.f >= (int64_t)kScanSms * 512 * 8 * p.chunk_rows ? 8 : 4;
     if (!p.few && !p.direct) {
-        with_vector<TI>(widest(16 / xs, false), [&](auto w) {
+        with_vector<TI>(widest(most, false), [&](auto w) {
             constexpr int W = decltype(w)::value;
             launch_sums<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, s);
             return 0;
         });
     }
     // (the gradient's walk has no wider threads than of 4 elements: its shared memory)
-    with_vector<TI>(widest(BACK ? 4 : 16 / xs, true), [&](auto w) {
+    with_vector<TI>(widest(BACK ? 4 : most, true), [&](auto w) {
         constexpr int W = decltype(w)::value < 4 || !BACK ? decltype(w)::value : 4;
         launch_rows<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, p.few, s);
         return 0;
