@@ -197,7 +197,7 @@ __device__ __forceinline__ void copy_piece(char* to, const TI* from)
     else if constexpr (kBytes >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes < 4 ? 4 : kBytes) : "memory");
     else *reinterpret_cast<TI*>(to) = *from;                    // (these copies take 4 bytes at least: the threads wait for one row after the other)
 }
-__device__ __forceinline__ void end_of_row() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void end_of_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void all_but_last() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -268,29 +268,33 @@ struct Stream {
         ld_first = BACK ? -ld_first_ : ld_first_;
         ld_second = BACK ? -ld_second_ : ld_second_;
 #pragma unroll
-        for (int k = 0; k < Rows::kAhead; ++k) {
-            if (k < rows) Rows::copy(place + k * Rows::kRow, first, second, c);
-            end_of_row();
-            first += ld_first;
-            second += ld_second;
-        }
+        for (int k = 0; k < Rows::kAhead; k += 2) send_two(k, k * Rows::kRow, c);
     }
     template <typename F>
     __device__ __forceinline__ void run(const Columns<W, P>& c, F work)
     {
+        // Two rows at a time: what does not depend on the row before is done for both before either goes on
         int at = 0;
 #pragma unroll 1
-        for (int32_t k = 0; k < rows; ++k, r += BACK ? -1 : 1) {
-            float x[W * P], y[W * P];
-            all_but_last<Rows::kAhead - 1>();
-            Rows::read(place + at, x, y);
-            work(r, x, y);
-            if (k + Rows::kAhead < rows) Rows::copy(place + at, first, second, c);
-            end_of_row();
+        for (int32_t k = 0; k < rows; k += 2, r += BACK ? -2 : 2) {
+            float x[2][W * P], y[2][W * P];
+            all_but_last<Rows::kAhead / 2 - 1>();
+            Rows::read(place + at, x[0], y[0]);
+            Rows::read(place + at + Rows::kRow, x[1], y[1]);
+            work(r, k + 1 < rows, x, y);
+            send_two(k + Rows::kAhead, at, c);
+            at = (at + 2 * Rows::kRow) & (Rows::kBytes - 1);
+        }
+    }
+    __device__ __forceinline__ void send_two(int32_t k, int at, const Columns<W, P>& c)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (k + u < rows) Rows::copy(place + at + u * Rows::kRow, first, second, c);
             first += ld_first;
             second += ld_second;
-            at = (at + Rows::kRow) & (Rows::kBytes - 1);
         }
+        end_of_group();
     }
 };
 
@@ -347,20 +351,26 @@ __device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, TH
         state[i] = 0.f;
     }
     if (BACK ? r1 == g.end : r0 == g.start) cut();
-    stream.run(c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
-        if (BACK ? row + 1 == g.start : row == g.end) {
-            if (BACK) g.previous(a);
-            else g.next(a);
-            cut();
-        }
-        float w[V], b[V];
-        steps_of<SIGMOID>(gate, value, w, b);
-        multiply(product, w);
-        if constexpr (BACK) {
-            add_all(state, value);
-            multiply(state, w);
-        } else {
-            step(state, w, b);
+    stream.run(c, [&](int32_t first_row, bool second, const float (&gate)[2][V], const float (&value)[2][V]) {
+        float w[2][V], b[2][V];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) steps_of<SIGMOID>(gate[u], value[u], w[u], b[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int32_t row = BACK ? first_row - u : first_row + u;
+            if (u == 1 && !second) break;
+            if (BACK ? row + 1 == g.start : row == g.end) {
+                if (BACK) g.previous(a);
+                else g.next(a);
+                cut();
+            }
+            multiply(product, w[u]);
+            if constexpr (BACK) {
+                add_all(state, value[u]);
+                multiply(state, w[u]);
+            } else {
+                step(state, w[u], b[u]);
+            }
         }
     });
 #pragma unroll
@@ -375,18 +385,24 @@ __device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P,
     constexpr int V = W * P;
     if (r0 == g.start) load_state(a.first, a, g.b, c, h);
     int64_t at = r0 * a.ldo + c.first;
-    stream.run(c, [&](int32_t row, const float (&gate)[V], const float (&value)[V]) {
-        if (row == g.end) {
-            if (a.last) store_state(a.last, a, g.b, c, h);
-            g.next(a);
-            load_state(a.first, a, g.b, c, h);
+    stream.run(c, [&](int32_t first_row, bool second, const float (&gate)[2][V], const float (&value)[2][V]) {
+        float w[2][V], b[2][V];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) steps_of<SIGMOID>(gate[u], value[u], w[u], b[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int32_t row = first_row + u;
+            if (u == 1 && !second) break;
+            if (row == g.end) {
+                if (a.last) store_state(a.last, a, g.b, c, h);
+                g.next(a);
+                load_state(a.first, a, g.b, c, h);
+            }
+            if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
+            step(h, w[u], b[u]);
+            store_pieces<W, P>(a.out, a.out_bf16, at, c, h);
+            at += a.ldo;
         }
-        if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
-        float w[V], b[V];
-        steps_of<SIGMOID>(gate, value, w, b);
-        step(h, w, b);
-        store_pieces<W, P>(a.out, a.out_bf16, at, c, h);
-        at += a.ldo;
     });
     if (a.last && r1 == g.end) store_state(a.last, a, g.b, c, h);
 }
@@ -431,16 +447,20 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
             copy_row(slot, Pl::kPiece, gates);
             copy_row(slot + Pl::kX, Pl::kPiece, in);
         }
-        end_of_row();
         gates += a.ldg;
         in += a.ldx;
     };
     float h[V], next[V];
 #pragma unroll 1
-    for (int k = 0; k < N; ++k) copy_inputs(places + k * Pl::kRow, q0 + k < r1);
+    for (int k = 0; k < N; k += 2) {
+        copy_inputs(places + k * Pl::kRow, q0 + k < r1);
+        copy_inputs(places + (k + 1) * Pl::kRow, q0 + k + 1 < r1);
+        end_of_group();
+    }
     load_state(a.states, a, q0 / N, c, next);
     if (r1 == g.end) load_state(a.last_grad, a, g.b, c, carry);
-    // Row k of a stretch lies in slot k ^ flip: places become free on the way back, the last row's first, for the next stretch's first.
+    // Row k of a stretch lies in slot k ^ flip: places become free on the way back, the last row's first, for the next stretch's first.  Two rows are a
+    // group and are worked on together, as in Stream.
     int flip = 0;
 #pragma unroll 1
     for (int rows = r1 - q0; q0 >= r0; q0 -= N, rows = N, flip ^= N - 1) {
@@ -451,87 +471,105 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
         const bool more = q0 - N >= r0;
         if (more) load_state(a.states, a, q0 / N - 1, c, next);
 #pragma unroll 1
-        for (int k = 0; k < N; ++k) {
-            all_but_last<N - 1>();
-            if (N - 1 - k < rows) copy_row(grads + (N - 1 - k) * Pl::kDoutRow, Pl::kDoutPiece, douts);
-            end_of_row();
-            douts -= a.ldd;
+        for (int k = 0; k < N; k += 2) {
+            all_but_last<N / 2 - 1>();
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int row = N - 1 - k - u;
+                if (row < rows) copy_row(grads + row * Pl::kDoutRow, Pl::kDoutPiece, douts);
+                douts -= a.ldd;
+            }
+            end_of_group();
             if (k >= rows) continue;
-            char* const slot = places + (k ^ flip) * Pl::kRow;
-            float gate[V], value[V];
+            float gate[2][V], value[2][V], w[2][V], rest[2][V];
 #pragma unroll
-            for (int j = 0; j < P; ++j) {
-                read_piece<TI, W>(slot + j * Pl::kPiece, gate + j * W);
-                read_piece<TI, W>(slot + Pl::kX + j * Pl::kPiece, value + j * W);
-            }
-            if (q0 + k == from.end) {
-                from.next(a);
-                load_state(a.first, a, from.b, c, h);
-            }
-            if constexpr (SIGMOID) {
-                float w[V], rest[V], small[V], slope[V];
-                sigmoid_of(gate, w, rest, small);
+            for (int u = 0; u < 2; ++u) {
+                const char* const slot = places + ((k + u) ^ flip) * Pl::kRow;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    gate[i] = copysignf(small[i], gate[i]);
-                    slope[i] = h[i];
+                for (int j = 0; j < P; ++j) {
+                    read_piece<TI, W>(slot + j * Pl::kPiece, gate[u] + j * W);
+                    read_piece<TI, W>(slot + Pl::kX + j * Pl::kPiece, value[u] + j * W);
                 }
-                add_minus(slope, value);
-                multiply(value, rest);
-                multiply(rest, w);
-                multiply(slope, rest);
-                step(h, w, value);
+                if constexpr (SIGMOID) {
+                    float small[V];
+                    sigmoid_of(gate[u], w[u], rest[u], small);
 #pragma unroll
-                for (int i = 0; i < V; ++i) value[i] = slope[i];
-            } else {
-                float was[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) was[i] = h[i];
-                step(h, gate, value);
-#pragma unroll
-                for (int i = 0; i < V; ++i) value[i] = was[i];
+                    for (int i = 0; i < V; ++i) gate[u][i] = copysignf(small[i], gate[u][i]);
+                }
             }
 #pragma unroll
-            for (int j = 0; j < P; ++j) {
-                write_piece<W>(slot + j * Pl::kPiece, gate + j * W);
-                write_piece<W>(slot + Pl::kX + j * Pl::kPiece, value + j * W);
+            for (int u = 0; u < 2; ++u) {
+                if (u == 1 && k + 1 >= rows) break;
+                char* const slot = places + ((k + u) ^ flip) * Pl::kRow;
+                if (q0 + k + u == from.end) {
+                    from.next(a);
+                    load_state(a.first, a, from.b, c, h);
+                }
+                float slope[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) slope[i] = h[i];
+                if constexpr (SIGMOID) {
+                    add_minus(slope, value[u]);
+                    multiply(value[u], rest[u]);
+                    multiply(rest[u], w[u]);
+                    multiply(slope, rest[u]);
+                    step(h, w[u], value[u]);
+                } else {
+                    step(h, gate[u], value[u]);
+                }
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    write_piece<W>(slot + j * Pl::kPiece, gate[u] + j * W);
+                    write_piece<W>(slot + Pl::kX + j * Pl::kPiece, slope + j * W);
+                }
             }
         }
         gates -= 2 * N * a.ldg;                                  // (to the stretch ahead)
         in -= 2 * N * a.ldx;
 #pragma unroll 1
-        for (int k = N - 1; k >= 0; --k) {
-            all_but_last<N - 1>();
-            char* const slot = places + (k ^ flip) * Pl::kRow;
-            if (k < rows) {
-                float d[V], keep[V], dg[V], w[V];
+        for (int k = N - 1; k >= 0; k -= 2) {
+            all_but_last<N / 2 - 1>();
+            if (k - 1 < rows) {
+                float d[2][V], keep[2][V], dg[2][V], w[2][V];
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    read_piece<TI, W>(grads + k * Pl::kDoutRow + j * Pl::kDoutPiece, d + j * W);
-                    read_piece<float, W>(slot + j * Pl::kPiece, keep + j * W);
-                    read_piece<float, W>(slot + Pl::kX + j * Pl::kPiece, dg + j * W);
-                }
-                if (q0 + k + 1 == g.start) {
-                    if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
-                    g.previous(a);
-                    load_state(a.last_grad, a, g.b, c, carry);
-                }
-                add_all(d, carry);
-                multiply(dg, d);
+                for (int u = 0; u < 2; ++u) {
+                    const char* const slot = places + ((k - u) ^ flip) * Pl::kRow;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    w[i] = keep[i];
-                    if constexpr (SIGMOID) sigmoid_parts(keep[i], w[i], keep[i]);
-                    carry[i] = d[i];
+                    for (int j = 0; j < P; ++j) {
+                        read_piece<TI, W>(grads + (k - u) * Pl::kDoutRow + j * Pl::kDoutPiece, d[u] + j * W);
+                        read_piece<float, W>(slot + j * Pl::kPiece, keep[u] + j * W);
+                        read_piece<float, W>(slot + Pl::kX + j * Pl::kPiece, dg[u] + j * W);
+                    }
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        w[u][i] = keep[u][i];
+                        if constexpr (SIGMOID) sigmoid_parts(keep[u][i], w[u][i], keep[u][i]);
+                    }
                 }
-                multiply(carry, w);
-                if constexpr (SIGMOID) multiply(d, keep);
-                store_pieces<W, P>(a.out, a.out_bf16, at, c, d);
-                store_pieces<W, P>(a.dgate, a.out_bf16, at_gate, c, dg);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int32_t row = q0 + k - u;
+                    if (u == 0 && k >= rows) continue;
+                    if (row + 1 == g.start) {
+                        if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
+                        g.previous(a);
+                        load_state(a.last_grad, a, g.b, c, carry);
+                    }
+                    add_all(d[u], carry);
+                    multiply(dg[u], d[u]);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) carry[i] = d[u][i];
+                    multiply(carry, w[u]);
+                    if constexpr (SIGMOID) multiply(d[u], keep[u]);
+                    store_pieces<W, P>(a.out, a.out_bf16, at - u * a.ldo, c, d[u]);
+                    store_pieces<W, P>(a.dgate, a.out_bf16, at_gate - u * a.lddg, c, dg[u]);
+                }
             }
-            at -= a.ldo;
-            at_gate -= a.lddg;
-            copy_inputs(slot, more);                             // row N - 1 - k of the stretch ahead
+            at -= 2 * a.ldo;
+            at_gate -= 2 * a.lddg;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) copy_inputs(places + ((k - u) ^ flip) * Pl::kRow, more);      // rows N - 1 - k + u of the stretch ahead
+            end_of_group();
         }
     }
     if (a.first_grad && r0 == g.start) store_state(a.first_grad, a, g.b, c, carry);
