@@ -333,15 +333,60 @@ __device__ __forceinline__ void store_state(float* p, const ScanArgs& a, int64_t
         for (int i = 0; i < W; ++i) p[row * a.f + c.column(k, i)] = s[k * W + i];
 }
 
+// A walk from graph to graph (BACK: towards the first) that has asked for the next one's offset and state when it gets there.
+template <int W, int P, bool BACK>
+struct Walk {
+    static constexpr bool kAsks = W * P <= 4;    // (threads of 8 columns are for long calls, and have no registers to spare)
+    Graph g;
+    int32_t bound, further;                      // rows end there; the next graph's far end
+    float state[kAsks ? W * P : 1];              // of the next graph
+    __device__ __forceinline__ void at(const ScanArgs& a, const Graph& graph, int32_t bound_, const Columns<W, P>& c)
+    {
+        g = graph;
+        bound = bound_;
+        look(a, c);
+    }
+    __device__ __forceinline__ const float* states(const ScanArgs& a) const { return BACK ? a.last_grad : a.first; }
+    __device__ __forceinline__ void look(const ScanArgs& a, const Columns<W, P>& c)
+    {
+        further = BACK ? g.start : g.end;        // (an empty one, as far as one can see)
+        if constexpr (kAsks) if (BACK ? g.start > bound && g.b > 0 : g.end < bound && g.b + 1 < a.graphs) {
+            further = offset_of(a, BACK ? g.b - 1 : g.b + 2);
+            load_state(states(a), a, BACK ? g.b - 1 : g.b + 1, c, state);
+        }
+    }
+    // on to the next graph; s: its state
+    __device__ __forceinline__ void go(const ScanArgs& a, const Columns<W, P>& c, float (&s)[W * P])
+    {
+        if (kAsks && (BACK ? further < g.start : further > g.end)) {
+            if (BACK) {
+                g.end = g.start;
+                g.start = further;
+                --g.b;
+            } else {
+                g.start = g.end;
+                g.end = further;
+                ++g.b;
+            }
+#pragma unroll
+            for (int i = 0; i < W * P; ++i) s[i] = state[kAsks ? i : 0];
+        } else {
+            if (BACK) g.previous(a);
+            else g.next(a);
+            load_state(states(a), a, g.b, c, s);
+        }
+        look(a, c);
+    }
+};
+
 // The map over rows r0 .. r1 - 1, for which `stream` has been started; `g` is the graph of r0 (going back, of r1 - 1).
 template <typename TI, int W, int P, int THREADS, bool SIGMOID, bool BACK>
-__device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, THREADS, BACK>& stream, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g,
+__device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, THREADS, BACK>& stream, int32_t r0, int32_t r1, const Columns<W, P>& c, const Graph& graph,
                                           float2 (&map)[W * P])
 {
     constexpr int V = W * P;
     float product[V], state[V];
     auto cut = [&] {                                             // (from its graph's own state)
-        load_state(BACK ? a.last_grad : a.first, a, g.b, c, state);
 #pragma unroll
         for (int i = 0; i < V; ++i) product[i] = __uint_as_float(0x7fffffffu);
     };
@@ -350,7 +395,12 @@ __device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, TH
         product[i] = 1.f;
         state[i] = 0.f;
     }
-    if (BACK ? r1 == g.end : r0 == g.start) cut();
+    if (BACK ? r1 == graph.end : r0 == graph.start) {
+        load_state(BACK ? a.last_grad : a.first, a, graph.b, c, state);
+        cut();
+    }
+    Walk<W, P, BACK> walk;
+    walk.at(a, graph, BACK ? r0 : r1, c);
     stream.run(c, [&](int32_t first_row, bool second, const float (&gate)[2][V], const float (&value)[2][V]) {
         float w[2][V], b[2][V];
 #pragma unroll
@@ -359,9 +409,8 @@ __device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, TH
         for (int u = 0; u < 2; ++u) {
             const int32_t row = BACK ? first_row - u : first_row + u;
             if (u == 1 && !second) break;
-            if (BACK ? row + 1 == g.start : row == g.end) {
-                if (BACK) g.previous(a);
-                else g.next(a);
+            if (BACK ? row + 1 == walk.g.start : row == walk.g.end) {
+                walk.go(a, c, state);
                 cut();
             }
             multiply(product, w[u]);
@@ -380,10 +429,12 @@ __device__ __forceinline__ void chunk_map(const ScanArgs& a, Stream<TI, W, P, TH
 // The rows themselves, from the state h on.
 template <typename TI, int W, int P, int THREADS, bool SIGMOID>
 __device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P, THREADS, false>& stream, int32_t r0, int32_t r1, const Columns<W, P>& c,
-                                             Graph g, float (&h)[W * P])
+                                             const Graph& graph, float (&h)[W * P])
 {
     constexpr int V = W * P;
-    if (r0 == g.start) load_state(a.first, a, g.b, c, h);
+    if (r0 == graph.start) load_state(a.first, a, graph.b, c, h);
+    Walk<W, P, false> walk;
+    walk.at(a, graph, r1, c);
     int64_t at = r0 * a.ldo + c.first;
     stream.run(c, [&](int32_t first_row, bool second, const float (&gate)[2][V], const float (&value)[2][V]) {
         float w[2][V], b[2][V];
@@ -393,10 +444,9 @@ __device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P,
         for (int u = 0; u < 2; ++u) {
             const int32_t row = first_row + u;
             if (u == 1 && !second) break;
-            if (row == g.end) {
-                if (a.last) store_state(a.last, a, g.b, c, h);
-                g.next(a);
-                load_state(a.first, a, g.b, c, h);
+            if (row == walk.g.end) {
+                if (a.last) store_state(a.last, a, walk.g.b, c, h);
+                walk.go(a, c, h);
             }
             if (a.states && row % kStateRows == 0) store_state(a.states, a, row / kStateRows, c, h);
             step(h, w[u], b[u]);
@@ -404,7 +454,7 @@ __device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P,
             at += a.ldo;
         }
     });
-    if (a.last && r1 == g.end) store_state(a.last, a, g.b, c, h);
+    if (a.last && r1 == walk.g.end) store_state(a.last, a, walk.g.b, c, h);
 }
 
 template <int W>
@@ -428,7 +478,8 @@ struct GradPlaces {
 // state that the forward call left, then back.  On the way forward the rows of dout are sent for, on the way back the gates and x of the rows ahead: whenever
 // a row is waited for, kStateRows - 1 others have been sent for after it.
 template <typename TI, int W, int P, int THREADS, bool SIGMOID>
-__device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, Graph g, float (&carry)[W * P])
+__device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, const Graph& graph,
+                                              float (&carry)[W * P])
 {
     constexpr int V = W * P, N = kStateRows;
     using Pl = GradPlaces<TI, W, P, THREADS>;
@@ -458,14 +509,18 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
         end_of_group();
     }
     load_state(a.states, a, q0 / N, c, next);
-    if (r1 == g.end) load_state(a.last_grad, a, g.b, c, carry);
+    if (r1 == graph.end) load_state(a.last_grad, a, graph.b, c, carry);
+    Walk<W, P, true> walk;
+    walk.at(a, graph, r0, c);
     // Row k of a stretch lies in slot k ^ flip: places become free on the way back, the last row's first, for the next stretch's first.  Two rows are a
     // group and are worked on together, as in Stream.
     int flip = 0;
 #pragma unroll 1
     for (int rows = r1 - q0; q0 >= r0; q0 -= N, rows = N, flip ^= N - 1) {
-        Graph from = g;
-        while (from.start > q0 && from.b > 0) from.previous(a);
+        Graph start = walk.g;
+        while (start.start > q0 && start.b > 0) start.previous(a);
+        Walk<W, P, false> from;
+        from.at(a, start, q0 + rows, c);
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = next[i];
         const bool more = q0 - N >= r0;
@@ -501,10 +556,7 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
             for (int u = 0; u < 2; ++u) {
                 if (u == 1 && k + 1 >= rows) break;
                 char* const slot = places + ((k + u) ^ flip) * Pl::kRow;
-                if (q0 + k + u == from.end) {
-                    from.next(a);
-                    load_state(a.first, a, from.b, c, h);
-                }
+                if (q0 + k + u == from.g.end) from.go(a, c, h);
                 float slope[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) slope[i] = h[i];
@@ -550,10 +602,9 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
                 for (int u = 0; u < 2; ++u) {
                     const int32_t row = q0 + k - u;
                     if (u == 0 && k >= rows) continue;
-                    if (row + 1 == g.start) {
-                        if (a.first_grad) store_state(a.first_grad, a, g.b, c, carry);
-                        g.previous(a);
-                        load_state(a.last_grad, a, g.b, c, carry);
+                    if (row + 1 == walk.g.start) {
+                        if (a.first_grad) store_state(a.first_grad, a, walk.g.b, c, carry);
+                        walk.go(a, c, carry);
                     }
                     add_all(d[u], carry);
                     multiply(dg[u], d[u]);
@@ -572,7 +623,7 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
             end_of_group();
         }
     }
-    if (a.first_grad && r0 == g.start) store_state(a.first_grad, a, g.b, c, carry);
+    if (a.first_grad && r0 == walk.g.start) store_state(a.first_grad, a, walk.g.b, c, carry);
 }
 
 // Graphs without rows: their last state is the first one (going back, the same for the gradients).  Columns c0 .. c1 - 1, warp `warp` of `warps`.
