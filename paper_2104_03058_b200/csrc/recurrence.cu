@@ -250,7 +250,12 @@ struct Pair {
 
 // Rows r, r + 1, .. (BACK: r, r - 1, ..) of two matrices, one after the other: `start` sends for the first ones, `run` does work(row, a row of the first
 // matrix, of the second).
-template <typename TI, int W, int P, int THREADS, bool BACK>
+// Narrow pieces (below 8 bytes) stay in registers on their way, four rows of them: an instruction to send for a piece and one to read it are then one.
+// (Gradients of 301 fp32 columns, 233 k rows, factors: 400 us through shared memory, 315 in registers; the sums the same, 136.)
+template <typename TI, int W>
+constexpr bool kNarrow = W * (int)sizeof(TI) < 8;
+
+template <typename TI, int W, int P, int THREADS, bool BACK, bool NARROW = kNarrow<TI, W>>
 struct Stream {
     using Rows = Pair<TI, W, P, THREADS>;
     char* place;
@@ -295,6 +300,71 @@ struct Stream {
             second += ld_second;
         }
         end_of_group();
+    }
+};
+
+template <typename TI, int W, int P, int THREADS, bool BACK>
+struct Stream<TI, W, P, THREADS, BACK, true> {
+    const TI *first, *second;
+    int64_t ld_first, ld_second;
+    int32_t r, rows;
+    Raw<TI, W> one[2][2][P], two[2][2][P];       // [pair of rows][row][piece]
+    __device__ __forceinline__ void start(char*, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r_, int32_t rows_,
+                                          const Columns<W, P>& c)
+    {
+        r = r_;
+        rows = rows_;
+        first = static_cast<const TI*>(first_) + r * ld_first_ + c.first;
+        second = static_cast<const TI*>(second_) + r * ld_second_ + c.first;
+        ld_first = BACK ? -ld_first_ : ld_first_;
+        ld_second = BACK ? -ld_second_ : ld_second_;
+        send<0>(0, c);
+        send<1>(2, c);
+    }
+    template <int Q>
+    __device__ __forceinline__ void send(int32_t k, const Columns<W, P>& c)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (k + u < rows)
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    one[Q][u][j].load(first + c.off[j]);
+                    two[Q][u][j].load(second + c.off[j]);
+                }
+            first += ld_first;
+            second += ld_second;
+        }
+    }
+    template <int Q, typename F>
+    __device__ __forceinline__ void take(int32_t k, const Columns<W, P>& c, F& work)
+    {
+        float x[2][W * P], y[2][W * P];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                float v[W], w[W];
+                one[Q][u][j].get(v);
+                two[Q][u][j].get(w);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    x[u][j * W + i] = v[i];
+                    y[u][j * W + i] = w[i];
+                }
+            }
+        send<Q>(k + 4, c);
+        work(r, k + 1 < rows, x, y);
+        r += BACK ? -2 : 2;
+    }
+    template <typename F>
+    __device__ __forceinline__ void run(const Columns<W, P>& c, F work)
+    {
+#pragma unroll 1
+        for (int32_t k = 0; k < rows; k += 4) {
+            take<0>(k, c, work);
+            if (k + 2 < rows) take<1>(k + 2, c, work);
+        }
     }
 };
 
@@ -457,6 +527,35 @@ __device__ __forceinline__ void forward_rows(const ScanArgs& a, Stream<TI, W, P,
     if (a.last && r1 == walk.g.end) store_state(a.last, a, walk.g.b, c, h);
 }
 
+// A row on the way forward: h to the next state; keep and slope: what the way back needs, the weight of the step (of a sigmoid `signed_small`) and the factor of G
+// in dgate.  w and rest: of `sigmoid_of`.
+template <bool SIGMOID, int V>
+__device__ __forceinline__ void forward_step(float (&h)[V], const float (&gate)[V], float (&value)[V], const float (&w)[V], float (&rest)[V], float (&slope)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) slope[i] = h[i];
+    if constexpr (SIGMOID) {
+        add_minus(slope, value);
+        multiply(value, rest);
+        multiply(rest, w);
+        multiply(slope, rest);
+        step(h, w, value);
+    } else {
+        step(h, gate, value);
+    }
+}
+// A row on the way back: d, the gradient of the result, to that of x, dg, the slope, to that of the gate, carry to what reaches the row before.
+template <bool SIGMOID, int V>
+__device__ __forceinline__ void backward_step(float (&carry)[V], float (&d)[V], float (&dg)[V], const float (&w)[V], const float (&rest)[V])
+{
+    add_all(d, carry);
+    multiply(dg, d);
+#pragma unroll
+    for (int i = 0; i < V; ++i) carry[i] = d[i];
+    multiply(carry, w);
+    if constexpr (SIGMOID) multiply(d, rest);
+}
+
 template <int W>
 __device__ __forceinline__ void write_piece(char* to, const float* x)
 {
@@ -558,17 +657,7 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
                 char* const slot = places + ((k + u) ^ flip) * Pl::kRow;
                 if (q0 + k + u == from.g.end) from.go(a, c, h);
                 float slope[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) slope[i] = h[i];
-                if constexpr (SIGMOID) {
-                    add_minus(slope, value[u]);
-                    multiply(value[u], rest[u]);
-                    multiply(rest[u], w[u]);
-                    multiply(slope, rest[u]);
-                    step(h, w[u], value[u]);
-                } else {
-                    step(h, gate[u], value[u]);
-                }
+                forward_step<SIGMOID>(h, gate[u], value[u], w[u], rest[u], slope);
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     write_piece<W>(slot + j * Pl::kPiece, gate[u] + j * W);
@@ -606,12 +695,7 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
                         if (a.first_grad) store_state(a.first_grad, a, walk.g.b, c, carry);
                         walk.go(a, c, carry);
                     }
-                    add_all(d[u], carry);
-                    multiply(dg[u], d[u]);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) carry[i] = d[u][i];
-                    multiply(carry, w[u]);
-                    if constexpr (SIGMOID) multiply(d[u], keep[u]);
+                    backward_step<SIGMOID>(carry, d[u], dg[u], w[u], keep[u]);
                     store_pieces<W, P>(a.out, a.out_bf16, at - u * a.ldo, c, d[u]);
                     store_pieces<W, P>(a.dgate, a.out_bf16, at_gate - u * a.lddg, c, dg[u]);
                 }
@@ -624,6 +708,138 @@ __device__ __forceinline__ void backward_rows(const ScanArgs& a, char* places, i
         }
     }
     if (a.first_grad && r0 == walk.g.start) store_state(a.first_grad, a, walk.g.b, c, carry);
+}
+
+// The same for narrow pieces: rows come through registers, two at a time ahead, and only what the way back needs is in shared memory, four values at once.
+template <int P, int THREADS>
+struct NarrowPlaces {
+    static constexpr int kBytes = kStateRows * 2 * THREADS * 16;                 // [row][keep, slope][thread]
+};
+template <typename TI, int W, int P, int THREADS, bool SIGMOID>
+__device__ __forceinline__ void backward_rows_narrow(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, const Graph& graph,
+                                                     float (&carry)[W * P])
+{
+    constexpr int V = W * P, N = kStateRows;
+    static_assert(V == 4, "four values of a thread are one access");
+    float4* const kept = reinterpret_cast<float4*>(places) + threadIdx.x;
+    const TI *const gates = static_cast<const TI*>(a.gate) + c.first, *const in = static_cast<const TI*>(a.x) + c.first,
+             *const douts = static_cast<const TI*>(a.dout) + c.first;
+    Raw<TI, W> gate_raw[2][P], in_raw[2][P], dout_raw[2][P];
+    auto load = [&](Raw<TI, W> (&raw)[P], const TI* row) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) raw[j].load(row + c.off[j]);
+    };
+    auto unpack = [&](const Raw<TI, W> (&raw)[P], float (&x)[V]) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            float v[W];
+            raw[j].get(v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) x[j * W + i] = v[i];
+        }
+    };
+    // rows first, first + 1 of gates and x; rows last, last - 1 of dout
+    auto ask_inputs = [&](int32_t first, int32_t end) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (first + u < end) {
+                load(gate_raw[u], gates + (first + u) * a.ldg);
+                load(in_raw[u], in + (first + u) * a.ldx);
+            }
+    };
+    auto ask_douts = [&](int32_t last, int32_t begin) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (last - u >= begin) load(dout_raw[u], douts + (last - u) * a.ldd);
+    };
+    int32_t q0 = (r1 - 1) / N * N;
+    float h[V], next[V];
+    ask_inputs(q0, r1);
+    load_state(a.states, a, q0 / N, c, next);
+    if (r1 == graph.end) load_state(a.last_grad, a, graph.b, c, carry);
+    Walk<W, P, true> walk;
+    walk.at(a, graph, r0, c);
+#pragma unroll 1
+    for (int rows = r1 - q0; q0 >= r0; q0 -= N, rows = N) {
+        Graph start = walk.g;
+        while (start.start > q0 && start.b > 0) start.previous(a);
+        Walk<W, P, false> from;
+        from.at(a, start, q0 + rows, c);
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = next[i];
+        if (q0 - N >= r0) load_state(a.states, a, q0 / N - 1, c, next);
+        ask_douts(q0 + rows - 1, q0);
+#pragma unroll 1
+        for (int k = 0; k < rows; k += 2) {
+            float gate[2][V], value[2][V], w[2][V], rest[2][V];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                unpack(gate_raw[u], gate[u]);
+                unpack(in_raw[u], value[u]);
+            }
+            ask_inputs(q0 + k + 2, q0 + rows);
+            if constexpr (SIGMOID) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float small[V];
+                    sigmoid_of(gate[u], w[u], rest[u], small);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) gate[u][i] = copysignf(small[i], gate[u][i]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u == 1 && k + 1 >= rows) break;
+                if (q0 + k + u == from.g.end) from.go(a, c, h);
+                float slope[V];
+                forward_step<SIGMOID>(h, gate[u], value[u], w[u], rest[u], slope);
+                kept[(k + u) * 2 * THREADS] = make_float4(gate[u][0], gate[u][1], gate[u][2], gate[u][3]);
+                kept[((k + u) * 2 + 1) * THREADS] = make_float4(slope[0], slope[1], slope[2], slope[3]);
+            }
+        }
+        if (q0 - N >= r0) ask_inputs(q0 - N, q0);
+        int64_t at = (q0 + rows - 1) * a.ldo + c.first, at_gate = (q0 + rows - 1) * a.lddg + c.first;
+#pragma unroll 1
+        for (int k = rows - 1; k >= 0; k -= 2, at -= 2 * a.ldo, at_gate -= 2 * a.lddg) {
+            float d[2][V], keep[2][V], dg[2][V], w[2][V];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) unpack(dout_raw[u], d[u]);
+            ask_douts(q0 + k - 2, q0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u == 1 && k == 0) break;
+                const float4 p = kept[(k - u) * 2 * THREADS], q = kept[((k - u) * 2 + 1) * THREADS];
+                keep[u][0] = p.x; keep[u][1] = p.y; keep[u][2] = p.z; keep[u][3] = p.w;
+                dg[u][0] = q.x; dg[u][1] = q.y; dg[u][2] = q.z; dg[u][3] = q.w;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    w[u][i] = keep[u][i];
+                    if constexpr (SIGMOID) sigmoid_parts(keep[u][i], w[u][i], keep[u][i]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u == 1 && k == 0) break;
+                if (q0 + k - u + 1 == walk.g.start) {
+                    if (a.first_grad) store_state(a.first_grad, a, walk.g.b, c, carry);
+                    walk.go(a, c, carry);
+                }
+                backward_step<SIGMOID>(carry, d[u], dg[u], w[u], keep[u]);
+                store_pieces<W, P>(a.out, a.out_bf16, at - u * a.ldo, c, d[u]);
+                store_pieces<W, P>(a.dgate, a.out_bf16, at_gate - u * a.lddg, c, dg[u]);
+            }
+        }
+    }
+    if (a.first_grad && r0 == walk.g.start) store_state(a.first_grad, a, walk.g.b, c, carry);
+}
+
+template <typename TI, int W, int P, int THREADS>
+constexpr int kGradBytes = kNarrow<TI, W> ? NarrowPlaces<P, THREADS>::kBytes : GradPlaces<TI, W, P, THREADS>::kBytes;
+template <typename TI, int W, int P, int THREADS, bool SIGMOID>
+__device__ __forceinline__ void walk_back(const ScanArgs& a, char* places, int32_t r0, int32_t r1, const Columns<W, P>& c, const Graph& graph, float (&carry)[W * P])
+{
+    if constexpr (kNarrow<TI, W>) backward_rows_narrow<TI, W, P, THREADS, SIGMOID>(a, places, r0, r1, c, graph, carry);
+    else backward_rows<TI, W, P, THREADS, SIGMOID>(a, places, r0, r1, c, graph, carry);
 }
 
 // Graphs without rows: their last state is the first one (going back, the same for the gradients).  Columns c0 .. c1 - 1, warp `warp` of `warps`.
@@ -809,7 +1025,7 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
 {
     grid_dependency<true>();
     constexpr int V = W * P, THREADS = BACK ? kGradBlock : kRowsBlock;
-    __shared__ __align__(16) char ring[BACK ? GradPlaces<TI, W, P, THREADS>::kBytes : Pair<TI, W, P, THREADS>::kBytes];
+    __shared__ __align__(16) char ring[BACK ? kGradBytes<TI, W, P, THREADS> : Pair<TI, W, P, THREADS>::kBytes];
     const int64_t at = (int64_t)(gridDim.x - 1 - blockIdx.x) * THREADS + threadIdx.x, chunk = at / a.places;
     Columns<W, P> c;
     c.at(a, (int)(at - chunk * a.places) * W, a.places * W);
@@ -820,7 +1036,7 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
     Graph g;
     if constexpr (BACK) {
         chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
-        backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
+        walk_back<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
     } else {
         Stream<TI, W, P, THREADS, false> stream;
         stream.start(ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, r1 - (int32_t)r0, c);
@@ -835,7 +1051,7 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
 {
     grid_dependency<true>();
     constexpr int V = W * P, LANES = Few<BACK>::kLanes, WAYS = Few<BACK>::kWays, THREADS = Few<BACK>::kThreads;
-    constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? GradPlaces<TI, W, P, THREADS>::kBytes : kRing;
+    constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? kGradBytes<TI, W, P, THREADS> : kRing;
     constexpr int kMost = kRing > kMaps ? kRing : kMaps;
     __shared__ __align__(16) char ring[kMost > kWalk ? kMost : kWalk];        // rows on their way, the chunks' maps, rows again
     __shared__ int32_t graph[WAYS];
@@ -864,7 +1080,7 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
         for (int i = 0; i < V; ++i) s[i] = ahead[i].y;         // (nothing is ahead of the first row but its graph's own state)
         g.at(a, graph[way]);
         if constexpr (BACK) {
-            backward_rows<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
+            walk_back<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
         } else {
             stream.start(ring, a.gate, a.ldg, a.x, a.ldx, r0, r1 - r0, c);
             forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, r0, r1, c, g, s);
