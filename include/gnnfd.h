@@ -475,9 +475,9 @@ int gnnfd_layer_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * with (u, v) the columns (i, i + rotary_dim / 2) of the head or, with interleaved != 0, (2 i, 2 i + 1).  The other columns are copied.  inverse != 0 turns by the
  * opposite angle (the scale stays): this is the gradient, out's for x's.  A matrix that holds queries, keys and values side by side is turned in one call: `heads` counts
  * those of the queries and keys, and ldx goes on to the values.
- * d_positions [n] of type itype, any value (fractions of a turn are exact to 2^-52 of the angle); NULL: the row's number.  d_freq [rotary_dim / 2] fp64, radians per position:
+ * d_positions [n] of type itype, any value (an angle is exact to 2^-51 of itself; beyond 2^50 radians it has no meaning, results stay finite); NULL: the row's number.  d_freq [rotary_dim / 2] fp64, radians per position:
  * gnnfd_rotary_frequencies or any other.  d_x [n, ldx] of type xdt, d_out [n, ldo] of type odt (d_x itself with ldo = ldx and odt = xdt; columns of
- * heads that are not turned and columns past heads * dim then stay as they are).  fp32 arithmetic on cosines and sines within 2 * 2^-24; one rounding at the end.
+ * heads that are not turned and columns past heads * dim then stay as they are).  fp32 arithmetic on cosines and sines within 3 * 2^-24; one rounding at the end.
  * GNNFD_TOO_LARGE: more than 2^20 columns.  The call only enqueues work.
  *
  * gnnfd_rotary_frequencies (host memory, no device): freq[i] = base^(-2 i / rotary_dim), for contexts beyond the length that a model was trained on

@@ -92,6 +92,22 @@ def test_far_and_negative_positions(itype):
     run(p.numel(), 2, 64, 64, positions=p, freq=g.rotary_frequencies(64, scaling="ramp", factor=32.0, length=4096))
 
 
+def test_angles_without_meaning_stay_finite():
+    """Positions up to the type's ends: x comes back no longer than it was (cosine and sine within 3 u of a point of the circle)."""
+    p = torch.tensor([2**63 - 1, -2**63, 2**55 + 1, -2**52 - 1, 2**51], device="cuda")
+    x = rand(5, 64)
+    for interleaved in (False, True):
+        y = g.rotary(x, g.rotary_frequencies(64), 1, 64, p, interleaved)
+        assert torch.isfinite(y).all() and (y.norm(dim=1) <= 1.01 * x.norm(dim=1)).all()
+
+
+@pytest.mark.parametrize("heads,dim,part", [(1, 100_000, 2), (3, 300_000, 4), (1, 1 << 20, 4096), (1 << 18, 4, 2)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rows_of_many_columns(heads, dim, part, interleaved):
+    run(3, heads, dim, part, interleaved=interleaved)
+    run(700 if heads == 1 and dim == 100_000 else 2, heads, dim, part, BF16, BF16, interleaved=interleaved)
+
+
 def test_quarter_turns_land_on_the_axes():
     """A frequency of pi / 2: positions are quarter turns (64 bits of pi are off by 1e-16 a turn)."""
     freq = torch.full((1,), math.pi / 2, dtype=torch.float64, device="cuda")
