@@ -22,7 +22,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 ROTARY_SCALINGS = {"none": 0, "position": 1, "base": 2, "ramp": 3}
 GATES = {"factor": 0, "sigmoid": 1}
-STATE_ROWS = 8
+STATE_ROWS, RECURRENCE_FEW_ROWS = 8, 2048
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056
@@ -195,10 +195,13 @@ def _need_rows(t, rows: int, name: str):
 
 def _extent(t):
     """[first byte, one past the last byte) of the storage a strided 2-D / 1-D tensor touches."""
-    if t.numel() == 0:
-        return (t.data_ptr(), t.data_ptr())
+    begin, count = t.data_ptr(), t.numel()
+    if count == 0:
+        return (begin, begin)
+    if t.is_contiguous():
+        return (begin, begin + count * t.element_size())
     last = sum((n - 1) * st for n, st in zip(t.shape, t.stride()))
-    return (t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size())
+    return (begin, begin + (last + 1) * t.element_size())
 
 
 def _no_overlap(a, b, name_a: str, name_b: str):
@@ -1168,9 +1171,12 @@ def _recurrence_operands(x, gate, form: str, graph_ptr, graphs: int, f: int, **s
             raise ValueError("%d rows do not make %d graphs of one length" % (n, graphs))
     pointers = []
     for name, t in states.items():
-        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (graphs, f) or not t.is_contiguous() or t.device != x.device):
+        if t is None:
+            pointers.append(None)
+            continue
+        if t.dtype != torch.float32 or t.shape != (graphs, f) or not t.is_contiguous() or t.device != x.device:
             raise ValueError("%s must be a contiguous float32 [graphs = %d, %d] tensor on %s" % (name, graphs, f, x.device))
-        pointers.append(None if t is None else t.data_ptr())
+        pointers.append(t.data_ptr())
     return xp, ldx, gp, ldg, GATES[form], graphs, pp, itype, pointers
 
 
@@ -1189,24 +1195,29 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
     n, width = x.shape
     f = width if f is None else f
     xp, ldx, gp, ldg, code, graphs, pp, itype, (ip, fp) = _recurrence_operands(x, gate, form, graph_ptr, graphs, f, initial=initial, final=final)
-    if out is None:
+    fresh = out is None
+    if fresh:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
-    else:
+    op, ldo = _matrix(out, f, "out")
+    if not fresh:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
         _no_overlap(x, out, "x", "out")
         _no_overlap(gate, out, "gate", "out")
-    op, ldo = _matrix(out, f, "out")
     if final is not None:
         if initial is not None and not (ip == fp and graph_ptr is None and graphs == n):
             _no_overlap(initial, final, "initial", "final")
-        for name, t in (("x", x), ("gate", gate), ("out", out)):
-            _no_overlap(t, final, name, "final")
+        _no_overlap(x, final, "x", "final")
+        _no_overlap(gate, final, "gate", "final")
+        if not fresh:
+            _no_overlap(final, out, "final", "out")
+            if initial is not None and ip != fp:
+                _no_overlap(initial, out, "initial", "out")
     elif with_final:
         final = _new(x, (graphs, f), torch.float32, stream)
         fp = final.data_ptr()
     states = _new(x, (-(-n // STATE_ROWS), f), torch.float32, stream) if with_states else None
-    if scratch is None:
+    if scratch is None and n > RECURRENCE_FEW_ROWS:
         need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None)
         scratch = _new(x, need, torch.uint8, stream) if need else None
     scr, scr_n = _scratch_args(scratch, x.device)
@@ -1238,7 +1249,7 @@ def linear_recurrence_backward(dout: torch.Tensor, x: torch.Tensor, gate: torch.
         raise ValueError("states must be the contiguous float32 [%d, %d] tensor of the forward call, on %s" % (-(-n // STATE_ROWS), f, x.device))
     dx, dgate = (_new(x, (n, f), out_dtype or torch.float32, stream) for _ in range(2))
     dinitial = _new(x, (graphs, f), torch.float32, stream) if initial is not None else None
-    if scratch is None:
+    if scratch is None and n > RECURRENCE_FEW_ROWS:
         need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None, True)
         scratch = _new(x, need, torch.uint8, stream) if need else None
     scr, scr_n = _scratch_args(scratch, x.device)

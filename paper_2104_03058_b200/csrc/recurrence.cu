@@ -24,7 +24,7 @@ namespace gnnfd {
 
 constexpr int kScanSms = 148;
 constexpr int kStateRows = 8;
-constexpr int kFewRows = 2048;                   // rows of a call that takes one launch
+constexpr int kFewRows = GNNFD_RECURRENCE_FEW_ROWS;          // rows of a call that takes one launch
 
 // Threads of the kernels, of the gradient's walk; lanes and ways of the one launch for few rows
 constexpr int kRowsBlock = 256, kGradBlock = 64;

@@ -114,4 +114,5 @@ def test_constants_of_the_header():
     for prefix, table in (("ROTARY", g.ROTARY_SCALINGS), ("GATE", g.GATES)):
         for name, code in table.items():
             assert int(re.search(r"GNNFD_%s_%s = (\d+)" % (prefix, name.upper()), text).group(1)) == code
+    assert int(re.search(r"#define GNNFD_RECURRENCE_FEW_ROWS (\d+)", text).group(1)) == g.RECURRENCE_FEW_ROWS
     assert "fp32 [(n + %d) / %d, f]" % (b.STATE_ROWS - 1, b.STATE_ROWS) in text
