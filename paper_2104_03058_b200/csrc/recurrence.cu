@@ -58,6 +58,12 @@ __device__ __forceinline__ float one_over(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float smaller_or_nan(float x, float y)
+{
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
 // a and 1 - a of a = 1 / (1 + e^-g), neither by subtraction, and `small`, the smaller one with g's sign, from which `sigmoid_parts` has both again
 template <int V>
 __device__ __forceinline__ void sigmoid_of(const float (&g)[V], float (&a)[V], float (&rest)[V], float (&small)[V])
@@ -92,9 +98,21 @@ template <bool SIGMOID, int V>
 __device__ __forceinline__ void steps_of(const float (&g)[V], const float (&x)[V], float (&a)[V], float (&b)[V])
 {
     if constexpr (SIGMOID) {
-        float small[V];
-        sigmoid_of(g, a, b, small);
+        // e = e^-g up to 2^126, a = 1 / (1 + e), 1 - a = e a, without a choice by sign.  Gates below -87, where e is cut, have a = 2^-126: taken off, so that a gate
+        // of -infinity keeps nothing (for others it is below a rounding down to 2^-102).
+        float e[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = g[i];
+        scale(e, -1.4426950408889634f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = e[i] = power_of_2(smaller_or_nan(e[i], 126.f));
+        const float one[1] = {-1.f}, least[1] = {1.17549435e-38f};
+        add_minus(a, one);
+#pragma unroll
+        for (int i = 0; i < V; ++i) b[i] = a[i] = one_over(a[i]);
+        multiply(b, e);
         multiply(b, x);
+        add_minus(a, least);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
