@@ -919,7 +919,7 @@ __device__ __forceinline__ void find_graphs(const ScanArgs& a, int32_t chunk0, i
 }
 
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(kRowsBlock) recurrence_sums(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(kRowsBlock, kNarrow<TI, W> ? 1 : 4) recurrence_sums(const __grid_constant__ ScanArgs a)
 {
     grid_dependency<true>();
     constexpr int V = W * P, kRing = Pair<TI, W, P, kRowsBlock>::kBytes, kMaps = kRowsBlock * V * (int)sizeof(float2);
@@ -1135,10 +1135,10 @@ static ScanPlan plan_scan(int64_t n, int32_t f, int64_t graphs, bool equal, bool
         p.chunks = ways;
         return p;
     }
-    // Long chunks cost fewer maps (24 bytes for a column of each), short ones give the chip more threads.
+    // Long chunks cost fewer maps (24 bytes for a column of each), short ones give the chip more threads.  These are the longest; `balance` may halve them.
     p.chunk_rows = 128;
     while (p.chunk_rows > 16 && n / p.chunk_rows * vectors < kScanSms * 1024) p.chunk_rows /= 2;
-    p.chunks = (n + p.chunk_rows - 1) / p.chunk_rows;
+    p.chunks = (n + p.chunk_rows / 2 - 1) / (p.chunk_rows / 2);
     return p;
 }
 
@@ -1169,8 +1169,20 @@ static void launch_sums(ScanArgs& a, cudaStream_t s)
     a.lanes = 32;
     while (a.lanes > 8 && (a.places + a.lanes - 1) / a.lanes * a.lanes * 7 > a.places * 8) a.lanes /= 2;
     a.ways = a.tile_chunks = kRowsBlock / a.lanes;
-    a.tiles = (a.chunks + a.ways - 1) / a.ways;
     a.column_tiles = (a.places + a.lanes - 1) / a.lanes;
+    // Where there are few blocks, chunks as long as make them fill the chip's places evenly: 133 k x 256 bf16, 518 blocks of 32 rows a chunk for 592 places
+    // 37 us, 592 of 28 34; 1 M x 128 fp32 163 and 153.
+    constexpr int kUnit = BACK ? kStateRows : 4, kPlaces = 4 * kScanSms;
+    const int64_t longest = a.chunk_rows, blocks = (a.n + longest * a.ways - 1) / (longest * a.ways) * a.column_tiles, waves = (blocks + kPlaces - 1) / kPlaces;
+    if (waves <= 4) {
+        int64_t tiles = kPlaces * waves / a.column_tiles, rows;
+        tiles = tiles < 1 ? 1 : tiles;
+        rows = (a.n + tiles * a.ways - 1) / (tiles * a.ways);
+        rows = (rows + kUnit - 1) / kUnit * kUnit;
+        a.chunk_rows = (int32_t)(rows < longest / 2 ? longest / 2 : rows > longest ? longest : rows);
+    }
+    a.chunks = (int32_t)(((int64_t)a.n + a.chunk_rows - 1) / a.chunk_rows);
+    a.tiles = (a.chunks + a.ways - 1) / a.ways;
     GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, W, P, SIGMOID, BACK>), (unsigned)(a.tiles * a.column_tiles), kRowsBlock, 0, a);
     GNNFD_LAUNCH("recurrence_carry", s, recurrence_carry<BACK>, (unsigned)((a.f + kCarryColumns - 1) / kCarryColumns),
                  kCarryColumns * kCarryWays, 0, a);
