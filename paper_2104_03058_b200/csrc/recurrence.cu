@@ -1041,7 +1041,7 @@ __device__ __forceinline__ void chunk_start(const ScanArgs& a, int64_t chunk, in
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_rows(const __grid_constant__ ScanArgs a)
 {
-    grid_dependency<true>();
+    grid_dependency<false>();
     constexpr int V = W * P, THREADS = BACK ? kGradBlock : kRowsBlock;
     __shared__ __align__(16) char ring[BACK ? kGradBytes<TI, W, P, THREADS> : Pair<TI, W, P, THREADS>::kBytes];
     const int64_t at = (int64_t)(gridDim.x - 1 - blockIdx.x) * THREADS + threadIdx.x, chunk = at / a.places;
@@ -1067,7 +1067,7 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __grid_constant__ ScanArgs a)
 {
-    grid_dependency<true>();
+    grid_dependency<false>();
     constexpr int V = W * P, LANES = Few<BACK>::kLanes, WAYS = Few<BACK>::kWays, THREADS = Few<BACK>::kThreads;
     constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? kGradBytes<TI, W, P, THREADS> : kRing;
     constexpr int kMost = kRing > kMaps ? kRing : kMaps;

@@ -164,7 +164,7 @@ struct Unit<TI, 0, true> {
 template <typename TI, int P, bool INTERLEAVED, int R>
 __global__ void __launch_bounds__(kRotaryBlock, INTERLEAVED ? 4 : 3) rotary_rows(const __grid_constant__ RotaryArgs a)
 {
-    grid_dependency<true>();
+    grid_dependency<false>();
     constexpr int STEP = P == 0 ? 1 : P, U = kRotaryUnits;
     __shared__ __align__(16) float cosine[kRotaryTable], sine[kRotaryTable];
     __shared__ double position[kRotaryBlock * kRotaryUnits];

@@ -68,9 +68,9 @@ def test_workspaces():
     for backward in (False, True):
         assert g.linear_recurrence_workspace_bytes(2048, 512, 1, False, backward) == 0
         assert g.linear_recurrence_workspace_bytes(1_000_000, 512, 1_000_000, True) == 0                # single tokens
-        for f in (1, 8, 64, 301, 4096):                     # 24 bytes a column for every 16 rows at most, and 12 for an eighth of that
+        for f in (1, 8, 64, 301, 4096):                     # for a column: 8 bytes for every 8 rows at most, and 12 for an eighth of that
             for n in (2049, 10_000, 100_000, 1_000_000, 30_000_000):
-                assert 0 < g.linear_recurrence_workspace_bytes(n, f, 1, False, backward) <= (n / 16 + 2) * (8 + 12 / 8) * f + (n / 16 + 12 * f) * 4 + 2048
+                assert 0 < g.linear_recurrence_workspace_bytes(n, f, 1, False, backward) <= (n / 8 + 2) * (8 + 12 / 8) * f + (n / 8 + 12 * f) * 4 + 2048
 
 
 def test_frequencies():
