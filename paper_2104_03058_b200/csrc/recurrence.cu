@@ -39,7 +39,7 @@ struct ScanArgs {
     float* states;                               // [rows / kStateRows, f] states ahead of every kStateRows-th row
     float2 *chunk_map, *tile_map;                // [chunks, f] map from the tile's start to the chunk's, [tiles, f] over the whole tile
     float* carry;                                // [tiles, f] state at the tile's start (null: no state crosses chunks)
-    int32_t* chunk_graph;                        // [chunks] graph of the first row (going back: of the last)
+    int4* chunk_graph;                           // [chunks] graph of the first row (going back: of the last), its first row and one past its last
     int64_t ldx, ldg, ldd, ldo, lddg;
     int32_t n, graphs, length, f, ptr64, out_bf16;
     int32_t places;                              // threads that share a row: see Columns
@@ -266,8 +266,8 @@ struct Pair {
     }
 };
 
-// Rows r, r + 1, .. (BACK: r, r - 1, ..) of two matrices, one after the other: `start` sends for the first ones, `run` does work(row, a row of the first
-// matrix, of the second).
+// Rows r0, r0 + 1, .. (BACK: r1 - 1, r1 - 2, ..) of two matrices, one after the other: `start` sends for the first ones, `run` does work(row, whether there is
+// another, two rows of the first matrix, of the second).
 // Narrow pieces (below 8 bytes) stay in registers on their way, four rows of them: an instruction to send for a piece and one to read it are then one.
 // (Gradients of 301 fp32 columns, 233 k rows, factors: 400 us through shared memory, 315 in registers; the sums the same, 136.)
 template <typename TI, int W>
@@ -280,18 +280,25 @@ struct Stream {
     const TI *first, *second;
     int64_t ld_first, ld_second;
     int32_t r, rows;
-    __device__ __forceinline__ void start(char* ring, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r_,
-                                          int32_t rows_, const Columns<W, P>& c)
+    __device__ __forceinline__ void start(char* ring, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r0, int32_t r1,
+                                          const Columns<W, P>& c)
     {
         place = ring + threadIdx.x * (W * (int)sizeof(TI));
-        r = r_;
-        rows = rows_;
+        r = BACK ? r1 - 1 : r0;
+        rows = r1 - r0;
         first = static_cast<const TI*>(first_) + r * ld_first_ + c.first;
         second = static_cast<const TI*>(second_) + r * ld_second_ + c.first;
         ld_first = BACK ? -ld_first_ : ld_first_;
         ld_second = BACK ? -ld_second_ : ld_second_;
 #pragma unroll
         for (int k = 0; k < Rows::kAhead; k += 2) send_two(k, k * Rows::kRow, c);
+    }
+    // fewer rows than have been sent for: r0 .. r1 - 1, or none
+    __device__ __forceinline__ void only(bool some, char* ring, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r0,
+                                         int32_t r1, const Columns<W, P>& c)
+    {
+        all_but_last<0>();                       // (nothing may come into places that others get)
+        if (some) start(ring, first_, ld_first_, second_, ld_second_, r0, r1, c);
     }
     template <typename F>
     __device__ __forceinline__ void run(const Columns<W, P>& c, F work)
@@ -327,11 +334,11 @@ struct Stream<TI, W, P, THREADS, BACK, true> {
     int64_t ld_first, ld_second;
     int32_t r, rows;
     Raw<TI, W> one[2][2][P], two[2][2][P];       // [pair of rows][row][piece]
-    __device__ __forceinline__ void start(char*, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r_, int32_t rows_,
+    __device__ __forceinline__ void start(char*, const void* first_, int64_t ld_first_, const void* second_, int64_t ld_second_, int32_t r0, int32_t r1,
                                           const Columns<W, P>& c)
     {
-        r = r_;
-        rows = rows_;
+        r = BACK ? r1 - 1 : r0;
+        rows = r1 - r0;
         first = static_cast<const TI*>(first_) + r * ld_first_ + c.first;
         second = static_cast<const TI*>(second_) + r * ld_second_ + c.first;
         ld_first = BACK ? -ld_first_ : ld_first_;
@@ -339,6 +346,7 @@ struct Stream<TI, W, P, THREADS, BACK, true> {
         send<0>(0, c);
         send<1>(2, c);
     }
+    __device__ __forceinline__ void only(bool, char*, const void*, int64_t, const void*, int64_t, int32_t, int32_t, const Columns<W, P>&) {}
     template <int Q>
     __device__ __forceinline__ void send(int32_t k, const Columns<W, P>& c)
     {
@@ -899,23 +907,41 @@ __device__ __forceinline__ void join_chunks(float2* shared, int lane, int way, i
 // The ways' graphs: of the first row (BACK: the last one) of each chunk of a block.  Warps look for that of the block's first row all together, each has a look at the
 // 32 offsets that follow, and only rows behind these are looked for again.
 template <bool BACK>
-__device__ __forceinline__ void find_graphs(const ScanArgs& a, int32_t chunk0, int ways, int32_t used, int32_t* graph)
+__device__ __forceinline__ void find_graphs(const ScanArgs& a, int32_t chunk0, int ways, int32_t used, Graph* graph)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int64_t row0 = (int64_t)chunk0 * a.chunk_rows;
     if (row0 < used && warp < ways) {
         const int32_t b0 = graph_of_row(a, (int32_t)row0);
         const int32_t end = b0 + lane < a.graphs ? offset_of(a, b0 + lane + 1) : 0x7fffffff;
+        int32_t start = __shfl_up_sync(0xffffffffu, end, 1);
+        if (lane == 0) start = offset_of(a, b0);
         for (int w = warp; w < ways; w += warps) {
             const int64_t r0 = row0 + (int64_t)w * a.chunk_rows;
             if (r0 >= used) break;
             const int32_t row = BACK ? (int32_t)min(r0 + a.chunk_rows, (int64_t)used) - 1 : (int32_t)r0;
             const unsigned behind = __ballot_sync(0xffffffffu, end > row);        // the first graph that ends behind the row
-            const int32_t b = behind ? b0 + __ffs(behind) - 1 : graph_of_row(a, row);
-            if (lane == 0) graph[w] = min(b, a.graphs - 1);
+            const int at = __ffs(behind) - 1;
+            Graph g;
+            if (at >= 0 && b0 + at < a.graphs) {
+                g.b = b0 + at;
+                g.start = __shfl_sync(0xffffffffu, start, at);
+                g.end = __shfl_sync(0xffffffffu, end, at);
+            } else {
+                g.at(a, graph_of_row(a, row));
+            }
+            if (lane == 0) graph[w] = g;
         }
     }
     __syncthreads();
+}
+
+// One past the last row of a chunk that is sent for at once.  How many rows belong to graphs has to be read first; copies into shared memory do not wait for
+// that, loads into registers do (sent for twice they are no longer kept ahead: sums of 301 fp32 columns 136 -> 183 us).
+template <bool KNOWN>
+__device__ __forceinline__ int32_t rows_to_send_for(const ScanArgs& a, int64_t r0)
+{
+    return (int32_t)min(r0 + a.chunk_rows, (int64_t)(KNOWN ? rows_used(a) : a.n));
 }
 
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
@@ -924,27 +950,30 @@ __global__ void __launch_bounds__(kRowsBlock, kNarrow<TI, W> ? 1 : 4) recurrence
     grid_dependency<true>();
     constexpr int V = W * P, kRing = Pair<TI, W, P, kRowsBlock>::kBytes, kMaps = kRowsBlock * V * (int)sizeof(float2);
     __shared__ __align__(16) char ring[kRing > kMaps ? kRing : kMaps];       // rows on their way, then the chunks' maps
-    __shared__ int32_t graph[kRowsBlock];
+    __shared__ Graph graph[kRowsBlock / 8];                                  // (8 lanes a row at least)
     // (the column tiles of the same rows side by side: rows start and end inside of the pieces of memory that are read)
     const int lane = threadIdx.x % a.lanes, way = threadIdx.x / a.lanes, tile = blockIdx.x / a.column_tiles, across = blockIdx.x - tile * a.column_tiles;
     const int first = (across * a.lanes * P + lane) * W;
-    const int32_t used = rows_used(a), chunk0 = tile * a.ways, chunk = chunk0 + way;
+    const int32_t chunk0 = tile * a.ways, chunk = chunk0 + way;
     const int64_t r0 = (int64_t)chunk * a.chunk_rows;
-    const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)used);
-    const bool some = r0 < r1 && first < a.f;
     Columns<W, P> c;
     c.at(a, first, a.lanes * W);
     Stream<TI, W, P, kRowsBlock, BACK> stream;
-    if (some) stream.start(ring, a.gate, a.ldg, BACK ? a.dout : a.x, BACK ? a.ldd : a.ldx, BACK ? r1 - 1 : (int32_t)r0, r1 - (int32_t)r0, c);
+    const void* const in = BACK ? a.dout : a.x;
+    const int64_t ld = BACK ? a.ldd : a.ldx;
+    const int32_t most = rows_to_send_for<kNarrow<TI, W>>(a, r0);
+    if (r0 < most && first < a.f) stream.start(ring, a.gate, a.ldg, in, ld, (int32_t)r0, most, c);
+    const int32_t used = rows_used(a), r1 = min(most, used);
+    const bool some = r0 < r1 && first < a.f;
     find_graphs<BACK>(a, chunk0, a.ways, used, graph);
+    if (!kNarrow<TI, W> && r1 < most) stream.only(some, ring, a.gate, a.ldg, in, ld, (int32_t)r0, r1, c);
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
     if (some) {
-        Graph g;
-        g.at(a, graph[way]);
+        const Graph g = graph[way];
         chunk_map<TI, W, P, kRowsBlock, SIGMOID, BACK>(a, stream, (int32_t)r0, r1, c, g, map);
-        if (first == 0) a.chunk_graph[chunk] = g.b;
+        if (first == 0) a.chunk_graph[chunk] = make_int4(g.b, g.start, g.end, 0);
     }
     __syncthreads();
     join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, a.lanes, a.ways, map, ahead, whole);
@@ -1028,7 +1057,10 @@ __device__ __forceinline__ void chunk_start(const ScanArgs& a, int64_t chunk, in
         g.at(a, (BACK ? r1 - 1 : r0) / a.length);
         return;                                                 // (chunks are whole graphs)
     }
-    g.at(a, a.chunk_graph[chunk]);
+    const int4 found = a.chunk_graph[chunk];
+    g.b = found.x;
+    g.start = found.y;
+    g.end = found.z;
     const int64_t tile = chunk / a.tile_chunks;
 #pragma unroll
     for (int k = 0; k < P; ++k)
@@ -1048,7 +1080,11 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
     Columns<W, P> c;
     c.at(a, (int)(at - chunk * a.places) * W, a.places * W);
     const int64_t r0 = chunk * a.chunk_rows;
-    const int32_t r1 = (int32_t)min(r0 + a.chunk_rows, (int64_t)rows_used(a));
+    const int32_t most = rows_to_send_for<!BACK && kNarrow<TI, W>>(a, r0);
+    if (r0 >= most) return;
+    Stream<TI, W, P, THREADS, false> stream;
+    if constexpr (!BACK) stream.start(ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, most, c);
+    const int32_t r1 = min(most, rows_used(a));
     if (r0 >= r1) return;
     float s[V] = {};
     Graph g;
@@ -1056,8 +1092,7 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
         chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
         walk_back<TI, W, P, THREADS, SIGMOID>(a, ring, (int32_t)r0, r1, c, g, s);
     } else {
-        Stream<TI, W, P, THREADS, false> stream;
-        stream.start(ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, r1 - (int32_t)r0, c);
+        if (!kNarrow<TI, W> && r1 < most) stream.only(true, ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, r1, c);
         chunk_start<W, P, BACK>(a, chunk, (int32_t)r0, r1, c, g, s);
         forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, (int32_t)r0, r1, c, g, s);
     }
@@ -1072,23 +1107,23 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
     constexpr int kRing = Pair<TI, W, P, THREADS>::kBytes, kMaps = THREADS * V * (int)sizeof(float2), kWalk = BACK ? kGradBytes<TI, W, P, THREADS> : kRing;
     constexpr int kMost = kRing > kMaps ? kRing : kMaps;
     __shared__ __align__(16) char ring[kMost > kWalk ? kMost : kWalk];        // rows on their way, the chunks' maps, rows again
-    __shared__ int32_t graph[WAYS];
+    __shared__ Graph graph[WAYS];
     const int lane = threadIdx.x % LANES, way = threadIdx.x / LANES, place = blockIdx.x * LANES + lane;
-    const int32_t used = rows_used(a), r0 = way * a.chunk_rows, r1 = min(r0 + a.chunk_rows, used);
-    const bool some = r0 < r1 && place < a.places;
+    const int32_t r0 = way * a.chunk_rows, most = rows_to_send_for<kNarrow<TI, W>>(a, r0);
     Columns<W, P> c;
     c.at(a, place * W, a.places * W);
     Stream<TI, W, P, THREADS, BACK> stream;
-    if (some) stream.start(ring, a.gate, a.ldg, BACK ? a.dout : a.x, BACK ? a.ldd : a.ldx, BACK ? r1 - 1 : r0, r1 - r0, c);
+    const void* const in = BACK ? a.dout : a.x;
+    const int64_t ld = BACK ? a.ldd : a.ldx;
+    if (r0 < most && place < a.places) stream.start(ring, a.gate, a.ldg, in, ld, r0, most, c);
+    const int32_t used = rows_used(a), r1 = min(most, used);
+    const bool some = r0 < r1 && place < a.places;
     find_graphs<BACK>(a, 0, WAYS, used, graph);
-    Graph g;
+    if (!kNarrow<TI, W> && r1 < most) stream.only(some, ring, a.gate, a.ldg, in, ld, r0, r1, c);
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) map[i] = make_float2(1.f, 0.f);
-    if (some) {
-        g.at(a, graph[way]);
-        chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, stream, r0, r1, c, g, map);
-    }
+    if (some) chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, stream, r0, r1, c, graph[way], map);
     __syncthreads();
     join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, LANES, WAYS, map, ahead, whole);
     __syncthreads();
@@ -1096,11 +1131,11 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
         float s[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = ahead[i].y;         // (nothing is ahead of the first row but its graph's own state)
-        g.at(a, graph[way]);
+        const Graph g = graph[way];
         if constexpr (BACK) {
             walk_back<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
         } else {
-            stream.start(ring, a.gate, a.ldg, a.x, a.ldx, r0, r1 - r0, c);
+            stream.start(ring, a.gate, a.ldg, a.x, a.ldx, r0, r1, c);
             forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, r0, r1, c, g, s);
         }
     }
@@ -1149,7 +1184,7 @@ static void carve_scan(Carver& c, const ScanPlan& p, int32_t f, ScanArgs* a)
     a->chunk_map = c.take<float2>((size_t)p.chunks * f);
     a->tile_map = c.take<float2>(tiles * f);
     a->carry = c.take<float>(tiles * f);
-    a->chunk_graph = c.take<int32_t>((size_t)p.chunks);
+    a->chunk_graph = c.take<int4>((size_t)p.chunks);
 }
 
 static int check_scan(int64_t n, int32_t f, int form, int64_t graphs, const void* d_ptr, gnnfd_itype_t itype, gnnfd_dtype_t dt, gnnfd_dtype_t odt)
