@@ -311,10 +311,15 @@ __global__ void __launch_bounds__(1024) layer_norm_columns(const float* part, in
     grid_dependency<true>();
     __shared__ double sums[32][33];
     const int lane = threadIdx.x & 31, way = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    constexpr int U = 10;                                 // (296 blocks: one batch of loads)
     double sum = 0.0;
-    if (c < 2 * f)
-#pragma unroll 10
-        for (int r = way; r < rows; r += 32) sum += load4(part + (int64_t)r * 2 * f + c);
+    for (int r = way; r < rows && c < 2 * f; r += 32 * U) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = r + 32 * u < rows ? load4(part + (int64_t)(r + 32 * u) * 2 * f + c) : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += v[u];
+    }
     sums[way][lane] = sum;
     __syncthreads();
     sum = sums[lane][way];                                // a warp adds up the ways of a column
