@@ -515,7 +515,7 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * GNNFD_TOO_LARGE: more than 2^31 - 65536 rows or 2^20 columns.  The calls only enqueue work. */
 typedef enum { GNNFD_GATE_FACTOR = 0, GNNFD_GATE_SIGMOID = 1 } gnnfd_gate_t;
 
-#define GNNFD_RECURRENCE_FEW_ROWS 2048
+#define GNNFD_RECURRENCE_FEW_ROWS 512
 int gnnfd_linear_recurrence_workspace_bytes(int64_t n, int32_t f, int64_t graphs, int equal_lengths, int backward, size_t* scratch_bytes);
 
 int gnnfd_linear_recurrence(int64_t n, const void* d_x, int64_t ldx, const void* d_gate, int64_t ldg, gnnfd_dtype_t dt, int32_t f, int form,

@@ -22,7 +22,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 ROTARY_SCALINGS = {"none": 0, "position": 1, "base": 2, "ramp": 3}
 GATES = {"factor": 0, "sigmoid": 1}
-STATE_ROWS, RECURRENCE_FEW_ROWS = 8, 2048
+STATE_ROWS, RECURRENCE_FEW_ROWS = 8, 512
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056

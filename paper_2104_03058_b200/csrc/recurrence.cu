@@ -24,7 +24,8 @@ namespace gnnfd {
 
 constexpr int kScanSms = 148;
 constexpr int kStateRows = 8;
-constexpr int kFewRows = GNNFD_RECURRENCE_FEW_ROWS;          // rows of a call that takes one launch
+// Rows of a call that takes one launch.  512 columns, one launch / three, us: 256 rows 7 / 11, 512 10 / 11, 1024 16 / 11, 2048 27 / 11; gradients 11, 14, 21, 35 / 14.
+constexpr int kFewRows = GNNFD_RECURRENCE_FEW_ROWS;
 
 // Threads of the kernels, of the gradient's walk; lanes and ways of the one launch for few rows
 constexpr int kRowsBlock = 256, kGradBlock = 64;
