@@ -240,10 +240,6 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
     __shared__ __align__(16) float columns[(TEAM < kLayerBlock ? kLayerBlock : TEAM) * N];      // the weights, at the end the sums of columns
     const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
     const int left = a.nvec - lane;
-    // the weights, for columns that no lane has 0
-    if (a.weight)
-        for (int c = threadIdx.x; c < lanes * N; c += blockDim.x) columns[c] = c < a.f ? load4(a.weight + c) : 0.f;
-    __syncthreads();
     float dw[N], db[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
@@ -262,6 +258,10 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
     };
     int64_t base = (int64_t)blockIdx.x * a.groups;
     fetch(base + group);
+    // the weights, 0 for columns that no lane has
+    if (a.weight)
+        for (int c = threadIdx.x; c < lanes * N; c += blockDim.x) columns[c] = c < a.f ? load4(a.weight + c) : 0.f;
+    __syncthreads();
     for (int turn = 0; base < a.n; base += step, turn ^= 1) {
         const int64_t row = base + group;
         float x[N], d[N], sums[2];

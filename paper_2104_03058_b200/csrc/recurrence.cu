@@ -1157,8 +1157,10 @@ static ScanPlan plan_scan(int64_t n, int32_t f, int64_t graphs, bool equal, bool
 {
     ScanPlan p{};
     const int64_t length = n / graphs, vectors = (f + 3) / 4;
-    // Graphs of one length that are a thread's whole work: single tokens above all.  (The gradient wants graphs that start where states are kept.)
-    if (equal && n > 0 && (back ? length % kStateRows == 0 && length <= 64 : length <= 64) && (length <= 16 || graphs * vectors >= kScanSms * 512)) {
+    // Graphs of one length that are a thread's whole work, single tokens above all: x and gates are read once.  Up to 128 rows where there are enough threads (64 k rows of
+    // 256 bf16 columns in graphs of 64: 39 us with the three launches, 20 so), of few rows only the shortest.  (The gradient wants graphs that start where states are kept.)
+    const int64_t longest = n <= kFewRows ? 4 : graphs * vectors >= kScanSms * 256 ? 128 : 64;
+    if (equal && n > 0 && length <= longest && (!back || length % kStateRows == 0)) {
         p.direct = true;
         p.chunk_rows = (int32_t)length;
         p.chunks = graphs;
