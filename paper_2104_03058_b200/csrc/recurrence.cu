@@ -205,16 +205,20 @@ struct Columns {
     __device__ __forceinline__ int column(int p, int i) const { return first + off[p] + i; }
 };
 
-// Rows on their way into shared memory.  Every thread copies the pieces of its own columns into places of its own and reads them from there, so nobody waits
-// for others, and how many rows are on their way does not cost registers.
+// Narrow pieces (below 8 bytes) stay in registers on their way, wider ones go through shared memory: every thread copies the pieces of its own columns into
+// places of its own and reads them from there, so nobody waits for others, and how many rows are on their way does not cost registers.  (Gradients of 301 fp32
+// columns, 233 k rows, factors: 400 us through shared memory, 315 in registers; the sums the same, 136.)
+template <typename TI, int W>
+constexpr bool kNarrow = W * (int)sizeof(TI) < 8;
+
 template <typename TI, int W>
 __device__ __forceinline__ void copy_piece(char* to, const TI* from)
 {
     constexpr int kBytes = W * (int)sizeof(TI);
+    static_assert(kBytes == 8 || kBytes == 16, "widths of the copies");
     const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
     if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-    else if constexpr (kBytes >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes < 4 ? 4 : kBytes) : "memory");
-    else *reinterpret_cast<TI*>(to) = *from;                    // (these copies take 4 bytes at least: the threads wait for one row after the other)
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(at), "l"(from) : "memory");
 }
 __device__ __forceinline__ void end_of_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -223,18 +227,13 @@ __device__ __forceinline__ void all_but_last() { asm volatile("cp.async.wait_gro
 template <typename TI, int W>
 __device__ __forceinline__ void read_piece(const char* from, float* x)
 {
-    constexpr int kBytes = W * (int)sizeof(TI);
     Raw<TI, W> raw;
-    if constexpr (kBytes == 16) {
+    if constexpr (W * sizeof(TI) == 16) {
         const uint4 v = *reinterpret_cast<const uint4*>(from);
         raw.w[0] = v.x; raw.w[1] = v.y; raw.w[2] = v.z; raw.w[3] = v.w;
-    } else if constexpr (kBytes == 8) {
+    } else {
         const uint2 v = *reinterpret_cast<const uint2*>(from);
         raw.w[0] = v.x; raw.w[1] = v.y;
-    } else if constexpr (kBytes == 4) {
-        raw.w[0] = *reinterpret_cast<const uint32_t*>(from);
-    } else {
-        raw.w[0] = *reinterpret_cast<const unsigned short*>(from);
     }
     float v[W];
     raw.get(v);
@@ -247,7 +246,7 @@ template <typename TI, int W, int P, int THREADS>
 struct Pair {
     static constexpr int kPiece = THREADS * W * (int)sizeof(TI), kRow = 2 * P * kPiece;
     static constexpr int kAhead = W * P * (int)sizeof(TI) >= 16 ? 4 : 8;       // rows on their way
-    static constexpr int kBytes = kAhead * kRow;                                // (a power of two)
+    static constexpr int kBytes = kNarrow<TI, W> ? 16 : kAhead * kRow;          // (a power of two)
     // `slot` is the thread's first place of the row
     __device__ __forceinline__ static void copy(char* slot, const TI* first, const TI* second, const Columns<W, P>& c)
     {
@@ -269,11 +268,6 @@ struct Pair {
 
 // Rows r0, r0 + 1, .. (BACK: r1 - 1, r1 - 2, ..) of two matrices, one after the other: `start` sends for the first ones, `run` does work(row, whether there is
 // another, two rows of the first matrix, of the second).
-// Narrow pieces (below 8 bytes) stay in registers on their way, four rows of them: an instruction to send for a piece and one to read it are then one.
-// (Gradients of 301 fp32 columns, 233 k rows, factors: 400 us through shared memory, 315 in registers; the sums the same, 136.)
-template <typename TI, int W>
-constexpr bool kNarrow = W * (int)sizeof(TI) < 8;
-
 template <typename TI, int W, int P, int THREADS, bool BACK, bool NARROW = kNarrow<TI, W>>
 struct Stream {
     using Rows = Pair<TI, W, P, THREADS>;
@@ -587,8 +581,7 @@ template <int W>
 __device__ __forceinline__ void write_piece(char* to, const float* x)
 {
     if constexpr (W == 4) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
-    else if constexpr (W == 2) *reinterpret_cast<float2*>(to) = make_float2(x[0], x[1]);
-    else *reinterpret_cast<float*>(to) = x[0];
+    else *reinterpret_cast<float2*>(to) = make_float2(x[0], x[1]);
 }
 
 // What the threads of the gradient's walk have in shared memory: places of W fp32 values for each thread and piece of kStateRows rows of gates and x, and
