@@ -22,7 +22,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 ROTARY_SCALINGS = {"none": 0, "position": 1, "base": 2, "ramp": 3}
 GATES = {"factor": 0, "sigmoid": 1}
-STATE_ROWS, RECURRENCE_FEW_ROWS = 8, 512
+STATE_ROWS, RECURRENCE_FEW_ROWS, RECURRENCE_FEW_VALUES = 8, 2048, 524288
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056
@@ -1249,7 +1249,7 @@ def linear_recurrence_backward(dout: torch.Tensor, x: torch.Tensor, gate: torch.
         raise ValueError("states must be the contiguous float32 [%d, %d] tensor of the forward call, on %s" % (-(-n // STATE_ROWS), f, x.device))
     dx, dgate = (_new(x, (n, f), out_dtype or torch.float32, stream) for _ in range(2))
     dinitial = _new(x, (graphs, f), torch.float32, stream) if initial is not None else None
-    if scratch is None and n > RECURRENCE_FEW_ROWS:
+    if scratch is None and (n > RECURRENCE_FEW_ROWS or n * f > RECURRENCE_FEW_VALUES):
         need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None, True)
         scratch = _new(x, need, torch.uint8, stream) if need else None
     scr, scr_n = _scratch_args(scratch, x.device)

@@ -80,19 +80,27 @@ struct LaunchScope {
 // that share for as long as it runs (GCN layer 602 -> 64 on 116 M entries 1.78 -> 2.28 ms, build of 80 M edges 2.85 -> 3.14); nor the edge
 // softmax kernels (20,000 rows of 50 entries 37 -> 41 us).
 template <typename... Params, typename... Args>
-inline void launch_early(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args)
+inline void launch_cluster(void (*kernel)(Params...), dim3 grid, dim3 block, unsigned blocks, size_t smem, cudaStream_t stream, Args&&... args)
 {
-    cudaLaunchAttribute attribute;
-    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attribute.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attribute[2];
+    attribute[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute[0].val.programmaticStreamSerializationAllowed = 1;
+    attribute[1].id = cudaLaunchAttributeClusterDimension;
+    attribute[1].val.clusterDim.x = blocks;
+    attribute[1].val.clusterDim.y = attribute[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t config{};
     config.gridDim = grid;
     config.blockDim = block;
     config.dynamicSmemBytes = smem;
     config.stream = stream;
-    config.attrs = &attribute;
-    config.numAttrs = 1;
+    config.attrs = attribute;
+    config.numAttrs = blocks > 1 ? 2 : 1;
     cudaLaunchKernelEx(&config, kernel, std::forward<Args>(args)...);      // errors are picked up by cudaGetLastError
+}
+template <typename... Params, typename... Args>
+inline void launch_early(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args)
+{
+    launch_cluster(kernel, grid, block, 1u, smem, stream, std::forward<Args>(args)...);
 }
 
 // Blocks of a kernel that an SM has room for: of kernels whose blocks stay and take work in turn as many are launched as the chip holds, once found out.

@@ -10,8 +10,8 @@
 // chunk's map and, in a block, joins those of a tile of chunks; `recurrence_carry` goes from tile to tile; `recurrence_rows` goes through the
 // rows again from the state that its chunk starts with.  The gradient does the same from the last row to the first, and needs the states of the
 // forward pass: that call leaves one for every kStateRows rows in fp32, from which a thread finds those in between.
-// Few rows take one launch, in which a block has all of them for some columns; equal graphs of few rows need no carry and take one launch of
-// `recurrence_rows`.
+// Few rows take one launch, in which a block or a cluster of blocks has all of them for some columns; equal graphs of few rows need no carry and take one launch
+// of `recurrence_rows`.
 //
 // A graph's first row inside of a chunk cuts it off from what is ahead: such a map has A = NaN, and a state that meets one becomes B.  (Gates that are NaN
 // themselves, or an infinite product times 0, make B NaN or cut off rightly: 0 times what came before.)
@@ -24,8 +24,11 @@ namespace gnnfd {
 
 constexpr int kScanSms = 148;
 constexpr int kStateRows = 8;
-// Rows of a call that takes one launch.  512 columns, one launch / three, us: 256 rows 7 / 11, 512 10 / 11, 1024 16 / 11, 2048 27 / 11; gradients 11, 14, 21, 35 / 14.
+// Rows of a call that takes one launch, and values of a gradient that does.  One launch / three, us on the device (the two launches less are 4 us on the host): 64
+// columns fp32 1024 rows 8 / 11, 2048 9 / 11, 4096 12 / 11; 512 columns 8.5 / 10, 11 / 11, 14.5 / 14; gradients of 512 columns 512 rows 11 / 12, 1024 12 / 12,
+// 2048 14 / 13, of 2048 columns 512 rows 14 / 17, 1024 20 / 18, 2048 39 / 25.
 constexpr int kFewRows = GNNFD_RECURRENCE_FEW_ROWS;
+constexpr int64_t kFewValues = GNNFD_RECURRENCE_FEW_VALUES;
 
 // Threads of the kernels, of the gradient's walk; lanes and ways of the one launch for few rows
 constexpr int kRowsBlock = 256, kGradBlock = 64;
@@ -1092,7 +1095,33 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
     }
 }
 
-// All rows of some columns in one block.
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meets()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a map in the shared memory of another block of the cluster, at the same place as `here`
+__device__ __forceinline__ float2 map_of_block(const float2* here, uint32_t rank)
+{
+    float2 m;
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(here)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m.x), "=f"(m.y) : "r"(at) : "memory");
+    return m;
+}
+
+// All rows of some columns in one block, or in the blocks of a cluster, which read one another's maps.
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __grid_constant__ ScanArgs a)
 {
@@ -1102,8 +1131,10 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
     constexpr int kMost = kRing > kMaps ? kRing : kMaps;
     __shared__ __align__(16) char ring[kMost > kWalk ? kMost : kWalk];        // rows on their way, the chunks' maps, rows again
     __shared__ Graph graph[WAYS];
-    const int lane = threadIdx.x % LANES, way = threadIdx.x / LANES, place = blockIdx.x * LANES + lane;
-    const int32_t r0 = way * a.chunk_rows, most = rows_to_send_for<kNarrow<TI, W>>(a, r0);
+    __shared__ __align__(8) float2 wholes[V][LANES];                          // maps over all of the block's rows
+    const int blocks = (int)cluster_size(), rank = (int)cluster_rank(), strip = blockIdx.x / blocks, strips = gridDim.x / blocks;
+    const int lane = threadIdx.x % LANES, way = threadIdx.x / LANES, place = strip * LANES + lane;
+    const int32_t chunk0 = rank * WAYS, r0 = (chunk0 + way) * a.chunk_rows, most = rows_to_send_for<kNarrow<TI, W>>(a, r0);
     Columns<W, P> c;
     c.at(a, place * W, a.places * W);
     Stream<TI, W, P, THREADS, BACK> stream;
@@ -1112,7 +1143,7 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
     if (r0 < most && place < a.places) stream.start(ring, a.gate, a.ldg, in, ld, r0, most, c);
     const int32_t used = rows_used(a), r1 = min(most, used);
     const bool some = r0 < r1 && place < a.places;
-    find_graphs<BACK>(a, 0, WAYS, used, graph);
+    find_graphs<BACK>(a, chunk0, WAYS, used, graph);
     if (!kNarrow<TI, W> && r1 < most) stream.only(some, ring, a.gate, a.ldg, in, ld, r0, r1, c);
     float2 map[V], ahead[V], whole[V];
 #pragma unroll
@@ -1120,11 +1151,24 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
     if (some) chunk_map<TI, W, P, THREADS, SIGMOID, BACK>(a, stream, r0, r1, c, graph[way], map);
     __syncthreads();
     join_chunks<V, BACK>(reinterpret_cast<float2*>(ring), lane, way, LANES, WAYS, map, ahead, whole);
-    __syncthreads();
-    if (some) {
-        float s[V];
+    float s[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = ahead[i].y;         // (nothing is ahead of the first row but its graph's own state)
+    for (int i = 0; i < V; ++i) s[i] = 0.f;                     // (nothing is ahead of the first row but its graph's own state)
+    if (blocks > 1) {
+        if (way == (BACK ? 0 : WAYS - 1))
+#pragma unroll
+            for (int i = 0; i < V; ++i) wholes[i][lane] = whole[i];
+        cluster_meets();
+        for (int q = BACK ? blocks - 1 : 0; q != rank; q += BACK ? -1 : 1)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] = applied(map_of_block(&wholes[i][lane], q), s[i]);
+        cluster_meets();                                        // (a block's memory lives as long as others read it)
+    } else {
+        __syncthreads();
+    }
+    if (some) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = applied(ahead[i], s[i]);
         const Graph g = graph[way];
         if constexpr (BACK) {
             walk_back<TI, W, P, THREADS, SIGMOID>(a, ring, r0, r1, c, g, s);
@@ -1133,15 +1177,16 @@ __global__ void __launch_bounds__(Few<BACK>::kThreads) recurrence_few(const __gr
             forward_rows<TI, W, P, THREADS, SIGMOID>(a, stream, r0, r1, c, g, s);
         }
     }
-    const int share = (a.f + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * share;
-    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), threadIdx.x >> 5, THREADS / 32);
+    const int share = (a.f + strips - 1) / strips, c0 = strip * share;
+    empty_graphs<BACK>(a, c0, min(c0 + share, a.f), (int64_t)rank * (THREADS / 32) + (threadIdx.x >> 5), (int64_t)blocks * (THREADS / 32));
 }
 
 // ------------------------------------------------------------------ host side
 
 // How rows are cut up: by sizes alone, so that the workspace query knows it.
 struct ScanPlan {
-    bool direct, few;
+    bool direct;
+    int32_t few;                                 // blocks of a cluster, of the one launch for few rows (0: three launches)
     int32_t chunk_rows;
     int64_t chunks;
 };
@@ -1159,11 +1204,14 @@ static ScanPlan plan_scan(int64_t n, int32_t f, int64_t graphs, bool equal, bool
         p.chunks = graphs;
         return p;
     }
-    if (n <= kFewRows) {
-        p.few = true;
-        const int64_t ways = back ? Few<true>::kWays : Few<false>::kWays, rows = (n + ways - 1) / ways, unit = back ? kStateRows : 4;
-        p.chunk_rows = (int32_t)((rows < 1 ? 1 : rows) + unit - 1) / unit * unit;
-        p.chunks = ways;
+    if (n <= kFewRows && (!back || n * f <= kFewValues)) {
+        // as many blocks as leave a thread no more than eight rows, up to the eight of a cluster
+        const int64_t ways = back ? Few<true>::kWays : Few<false>::kWays, unit = back ? kStateRows : 2;
+        p.few = 1;
+        while (p.few < 8 && n > 8 * ways * p.few) p.few *= 2;
+        const int64_t rows = (n + ways * p.few - 1) / (ways * p.few);
+        p.chunk_rows = (int32_t)(((rows < 1 ? 1 : rows) + unit - 1) / unit * unit);
+        p.chunks = ways * p.few;
         return p;
     }
     // Long chunks cost fewer maps (24 bytes for a column of each), short ones give the chip more threads.  These are the longest; `balance` may halve them.
@@ -1219,12 +1267,13 @@ static void launch_sums(ScanArgs& a, cudaStream_t s)
                  kCarryColumns * kCarryWays, 0, a);
 }
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
-static void launch_rows(ScanArgs& a, bool few, cudaStream_t s)
+static void launch_rows(ScanArgs& a, unsigned few, cudaStream_t s)
 {
     a.places = (a.f / W + P - 1) / P;
     if (few) {
-        GNNFD_LAUNCH("recurrence_few", s, (recurrence_few<TI, W, P, SIGMOID, BACK>), (unsigned)((a.places + Few<BACK>::kLanes - 1) / Few<BACK>::kLanes),
-                     Few<BACK>::kThreads, 0, a);
+        const unsigned strips = (unsigned)((a.places + Few<BACK>::kLanes - 1) / Few<BACK>::kLanes);
+        LaunchScope scope("recurrence_few", s);
+        launch_cluster(recurrence_few<TI, W, P, SIGMOID, BACK>, strips * few, Few<BACK>::kThreads, few, 0, s, a);
         return;
     }
     const int64_t threads = (int64_t)a.chunks * a.places, block = BACK ? kGradBlock : kRowsBlock;
@@ -1257,7 +1306,7 @@ static int run_scan(ScanArgs& a, const ScanPlan& p, cudaStream_t s)
     // (the gradient's walk has no wider threads than of 4 elements: its shared memory)
     with_vector<TI>(widest(BACK ? 4 : most, true), [&](auto w) {
         constexpr int W = decltype(w)::value < 4 || !BACK ? decltype(w)::value : 4;
-        launch_rows<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, p.few, s);
+        launch_rows<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, (unsigned)p.few, s);
         return 0;
     });
     GNNFD_CUDA_CHECK(cudaGetLastError());

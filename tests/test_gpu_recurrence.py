@@ -141,7 +141,7 @@ def offsets(n, graphs, seed=0, itype=torch.int32, last=None):
 
 @pytest.mark.parametrize("form", ["factor", "sigmoid"])
 @pytest.mark.parametrize("xdt,odt", [(F32, F32), (BF16, BF16), (F32, BF16), (BF16, F32)])
-@pytest.mark.parametrize("n,f,ld,offset", [(1, 1, 1, 0), (5, 3, 3, 1), (15, 8, 8, 0), (16, 8, 8, 0), (17, 41, 41, 0), (300, 64, 64, 0), (333, 20, 22, 0), (511, 9, 9, 0), (512, 24, 24, 0), (513, 12, 12, 0),
+@pytest.mark.parametrize("n,f,ld,offset", [(1, 1, 1, 0), (5, 3, 3, 1), (15, 8, 8, 0), (16, 8, 8, 0), (17, 41, 41, 0), (300, 64, 64, 0), (333, 20, 22, 0), (511, 9, 9, 0), (512, 24, 24, 0), (513, 12, 12, 0), (1030, 16, 16, 0), (600, 900, 900, 0),
                                            (2047, 12, 12, 2), (2048, 4, 4, 0), (2049, 4, 4, 0), (2500, 33, 40, 0), (3001, 70, 72, 4), (4100, 301, 301, 0),
                                            (2600, 128, 128, 0), (3000, 260, 260, 2)])
 def test_one_graph(n, f, ld, offset, xdt, odt, form):

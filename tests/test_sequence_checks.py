@@ -66,7 +66,7 @@ def test_workspaces():
     sizes = [g.layer_norm_backward_workspace_bytes(n, 64) for n in (0, 1, 100, 10_000, 1_000_000)]
     assert sizes == sorted(sizes) and sizes[-1] == sizes[-2]
     for backward in (False, True):
-        assert g.linear_recurrence_workspace_bytes(g.RECURRENCE_FEW_ROWS, 512, 1, False, backward) == 0
+        assert g.linear_recurrence_workspace_bytes(g.RECURRENCE_FEW_ROWS, g.RECURRENCE_FEW_VALUES // g.RECURRENCE_FEW_ROWS, 1, False, backward) == 0
         assert g.linear_recurrence_workspace_bytes(1_000_000, 512, 1_000_000, True) == 0                # single tokens
         # for a chunk of 8 rows or more: 8 bytes a column and 16, for every 8 chunks 12 bytes a column more; four arrays, rounded up to 256 bytes each
         for f in (1, 8, 64, 301, 4096):
@@ -117,4 +117,5 @@ def test_constants_of_the_header():
         for name, code in table.items():
             assert int(re.search(r"GNNFD_%s_%s = (\d+)" % (prefix, name.upper()), text).group(1)) == code
     assert int(re.search(r"#define GNNFD_RECURRENCE_FEW_ROWS (\d+)", text).group(1)) == g.RECURRENCE_FEW_ROWS
+    assert int(re.search(r"#define GNNFD_RECURRENCE_FEW_VALUES (\d+)", text).group(1)) == g.RECURRENCE_FEW_VALUES
     assert "fp32 [(n + %d) / %d, f]" % (b.STATE_ROWS - 1, b.STATE_ROWS) in text
