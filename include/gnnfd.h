@@ -507,7 +507,8 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * [graphs, f], may be NULL) receives the last state of each graph; it may be d_initial itself where graphs = n and d_graph_ptr is NULL, and does not overlap it otherwise.  d_states
  * (may be NULL): fp32 [(n + 7) / 8, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
  * d_scratch: gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, d_graph_ptr == NULL, 0) bytes, 256-byte aligned (0
- * and NULL for up to GNNFD_RECURRENCE_FEW_ROWS rows, in the gradient of up to GNNFD_RECURRENCE_FEW_VALUES values).
+ * and NULL for up to GNNFD_RECURRENCE_FEW_ROWS rows, in the gradient half as many and of up to
+ * GNNFD_RECURRENCE_FEW_VALUES values).
  *
  * gnnfd_linear_recurrence_backward: for d_dout [n, ldd] of type dt and d_dfinal (fp32 [graphs, f]; NULL: 0), the gradients of out and the last states, d_dx and
  * d_dgate [n, ld*] of type gdt and d_dinitial (fp32 [graphs, f]; NULL: not wanted).  d_states as written by the forward call with the same arguments.  Rows
@@ -515,7 +516,7 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * GNNFD_TOO_LARGE: more than 2^31 - 65536 rows or 2^20 columns.  The calls only enqueue work. */
 typedef enum { GNNFD_GATE_FACTOR = 0, GNNFD_GATE_SIGMOID = 1 } gnnfd_gate_t;
 
-#define GNNFD_RECURRENCE_FEW_ROWS 2048
+#define GNNFD_RECURRENCE_FEW_ROWS 4096
 #define GNNFD_RECURRENCE_FEW_VALUES 524288
 int gnnfd_linear_recurrence_workspace_bytes(int64_t n, int32_t f, int64_t graphs, int equal_lengths, int backward, size_t* scratch_bytes);
 

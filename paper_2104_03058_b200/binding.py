@@ -7,6 +7,7 @@ the entry points raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -22,7 +23,7 @@ COMBINE_TF32, COMBINE_FP32 = 0, 1
 ACTIVATIONS = {"none": 0, "relu": 1, "elu": 2, "silu": 3, "gelu": 4}
 ROTARY_SCALINGS = {"none": 0, "position": 1, "base": 2, "ramp": 3}
 GATES = {"factor": 0, "sigmoid": 1}
-STATE_ROWS, RECURRENCE_FEW_ROWS, RECURRENCE_FEW_VALUES = 8, 2048, 524288
+STATE_ROWS, RECURRENCE_FEW_ROWS, RECURRENCE_FEW_VALUES = 8, 4096, 524288
 STATIC_SCRATCH_BYTES = 32 << 20
 HUB_DEGREE, HUB_SEGMENT, HUB_RANGE_ROWS = 2048, 1024, 524288
 EMBEDDING_FEW_IDS, EMBEDDING_FEW_ROWS = 16384, 3629056
@@ -740,6 +741,8 @@ def _stream_handle(index: int, stream) -> int:
 def _new(like: torch.Tensor, shape, dtype, stream):
     """Memory that a call allocates beside a tensor: taken under the stream the work runs on (see _alloc_bytes)."""
     if stream is None:
+        if like.shape == shape:                    # (the quicker of the two)
+            return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
         return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
@@ -1048,6 +1051,7 @@ def _column_values(x, f: int, name: str, t):
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=256)
 def layer_norm_backward_workspace_bytes(n: int, f: int) -> int:
     s = ctypes.c_size_t()
     _check(lib().gnnfd_layer_norm_backward_workspace_bytes(n, f, ctypes.byref(s)), "gnnfd_layer_norm_backward_workspace_bytes")
@@ -1138,6 +1142,7 @@ def rotary(x: torch.Tensor, freq: torch.Tensor, heads: int, dim: int, positions:
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def linear_recurrence_workspace_bytes(n: int, f: int, graphs: int = 1, equal_lengths: bool = False, backward: bool = False) -> int:
     s = ctypes.c_size_t()
     _check(lib().gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, int(equal_lengths), int(backward), ctypes.byref(s)),
@@ -1145,8 +1150,8 @@ def linear_recurrence_workspace_bytes(n: int, f: int, graphs: int = 1, equal_len
     return s.value
 
 
-def _recurrence_operands(x, gate, form: str, graph_ptr, graphs: int, f: int, **states):
-    """(pointer of x, pitch, pointer of the gates, pitch, form, graphs, offsets pointer, offsets type, pointers of the [graphs, f] states)"""
+def _recurrence_operands(x, gate, form: str, graph_ptr, graphs, f: int):
+    """(pointer of x, pitch, pointer of the gates, pitch, form, graphs, offsets pointer, offsets type)"""
     xp, ldx = _matrix(x, f, "x")
     gp, ldg = _matrix(gate, f, "gate")
     if gate.dtype != x.dtype:
@@ -1154,30 +1159,30 @@ def _recurrence_operands(x, gate, form: str, graph_ptr, graphs: int, f: int, **s
     if gate.device != x.device:
         _same_device(x.device, gate=gate)
     n = x.shape[0]
-    _need_rows_of(gate, n, "gate")
+    if gate.shape[0] < n:
+        _need_rows_of(gate, n, "gate")
     if form not in GATES:
         raise ValueError("form must be one of %s" % ", ".join(GATES))
-    pp, itype = None, I32
-    if graph_ptr is not None:
-        pp, count, itype = _index_list(graph_ptr, "graph_ptr")
-        if count < 2 or graph_ptr.device != x.device:
-            raise ValueError("graph_ptr must hold graphs + 1 >= 2 offsets on %s" % x.device)
-        if graphs is not None and graphs != count - 1:
-            raise ValueError("graph_ptr holds the offsets of %d graphs, not of %d" % (count - 1, graphs))
-        graphs = count - 1
-    else:
+    if graph_ptr is None:
         graphs = 1 if graphs is None else graphs
         if graphs < 1 or n % graphs:
             raise ValueError("%d rows do not make %d graphs of one length" % (n, graphs))
-    pointers = []
-    for name, t in states.items():
-        if t is None:
-            pointers.append(None)
-            continue
-        if t.dtype != torch.float32 or t.shape != (graphs, f) or not t.is_contiguous() or t.device != x.device:
-            raise ValueError("%s must be a contiguous float32 [graphs = %d, %d] tensor on %s" % (name, graphs, f, x.device))
-        pointers.append(t.data_ptr())
-    return xp, ldx, gp, ldg, GATES[form], graphs, pp, itype, pointers
+        return xp, ldx, gp, ldg, GATES[form], graphs, None, I32
+    pp, count, itype = _index_list(graph_ptr, "graph_ptr")
+    if count < 2 or graph_ptr.device != x.device:
+        raise ValueError("graph_ptr must hold graphs + 1 >= 2 offsets on %s" % x.device)
+    if graphs is not None and graphs != count - 1:
+        raise ValueError("graph_ptr holds the offsets of %d graphs, not of %d" % (count - 1, graphs))
+    return xp, ldx, gp, ldg, GATES[form], count - 1, pp, itype
+
+
+def _graph_states(t, x, graphs: int, f: int, name: str):
+    """Pointer of fp32 states [graphs, f] beside x, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (graphs, f) or not t.is_contiguous() or t.device != x.device:
+        raise ValueError("%s must be a contiguous float32 [graphs = %d, %d] tensor on %s" % (name, graphs, f, x.device))
+    return t.data_ptr()
 
 
 def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid", graph_ptr: torch.Tensor | None = None, graphs: int | None = None,
@@ -1194,7 +1199,8 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
                           with_states, scratch)
     n, width = x.shape
     f = width if f is None else f
-    xp, ldx, gp, ldg, code, graphs, pp, itype, (ip, fp) = _recurrence_operands(x, gate, form, graph_ptr, graphs, f, initial=initial, final=final)
+    xp, ldx, gp, ldg, code, graphs, pp, itype = _recurrence_operands(x, gate, form, graph_ptr, graphs, f)
+    ip, fp = _graph_states(initial, x, graphs, f, "initial"), _graph_states(final, x, graphs, f, "final")
     fresh = out is None
     if fresh:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
@@ -1239,17 +1245,20 @@ def linear_recurrence_backward(dout: torch.Tensor, x: torch.Tensor, gate: torch.
                           out_dtype, scratch)
     n, width = x.shape
     f = width if f is None else f
-    xp, ldx, gp, ldg, code, graphs, pp, itype, (ip, dfp) = _recurrence_operands(x, gate, form, graph_ptr, graphs, f, initial=initial, dfinal=dfinal)
+    xp, ldx, gp, ldg, code, graphs, pp, itype = _recurrence_operands(x, gate, form, graph_ptr, graphs, f)
+    ip, dfp = _graph_states(initial, x, graphs, f, "initial"), _graph_states(dfinal, x, graphs, f, "dfinal")
     dp, ldd = _matrix(dout, f, "dout")
     if dout.dtype != x.dtype:
         raise TypeError("dout must have the dtype of x")
-    _same_device(x.device, dout=dout)
+    if dout.device != x.device:
+        _same_device(x.device, dout=dout)
     _need_rows_of(dout, n, "dout")
-    if states.dtype != torch.float32 or tuple(states.shape) != (-(-n // STATE_ROWS), f) or not states.is_contiguous() or states.device != x.device:
+    if states.dtype != torch.float32 or states.shape != (-(-n // STATE_ROWS), f) or not states.is_contiguous() or states.device != x.device:
         raise ValueError("states must be the contiguous float32 [%d, %d] tensor of the forward call, on %s" % (-(-n // STATE_ROWS), f, x.device))
-    dx, dgate = (_new(x, (n, f), out_dtype or torch.float32, stream) for _ in range(2))
+    odt = out_dtype or torch.float32
+    dx, dgate = _new(x, (n, f), odt, stream), _new(x, (n, f), odt, stream)
     dinitial = _new(x, (graphs, f), torch.float32, stream) if initial is not None else None
-    if scratch is None and (n > RECURRENCE_FEW_ROWS or n * f > RECURRENCE_FEW_VALUES):
+    if scratch is None and (n > RECURRENCE_FEW_ROWS // 2 or n * f > RECURRENCE_FEW_VALUES):
         need = linear_recurrence_workspace_bytes(n, f, graphs, graph_ptr is None, True)
         scratch = _new(x, need, torch.uint8, stream) if need else None
     scr, scr_n = _scratch_args(scratch, x.device)

@@ -24,7 +24,7 @@ namespace gnnfd {
 constexpr int kLayerBlock = 256;
 constexpr int kLayerColumns = 8192;              // 512 lanes of 16 elements
 constexpr int kLayerSms = 148;
-constexpr int64_t kGradBlocks = 3 * kLayerSms;   // at most
+constexpr int64_t kGradBlocks = 3 * kLayerSms;   // of the gradient at most: the workspace has a row of sums for each
 
 struct LayerArgs {
     const void *x, *dout;
@@ -360,7 +360,8 @@ static void launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
     constexpr int kThreads = TEAM < kLayerBlock ? kLayerBlock : TEAM;
     if (a.dout) {
         static const int held = blocks_per_sm(layer_norm_grad<TI, V, N, TEAM>, kThreads, 0);
-        *blocks = (int32_t)(need < kLayerSms * held ? need : kLayerSms * held);
+        const int64_t most = kLayerSms * held < kGradBlocks ? kLayerSms * held : kGradBlocks;
+        *blocks = (int32_t)(need < most ? need : most);
         GNNFD_LAUNCH("layer_norm_grad", s, (layer_norm_grad<TI, V, N, TEAM>), (unsigned)*blocks, a.groups * a.lanes, 0, a);
     } else {
         static const int held = blocks_per_sm(layer_norm_rows<TI, V, N, kRows, TEAM>, kThreads, 0);

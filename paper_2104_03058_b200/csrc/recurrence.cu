@@ -1197,14 +1197,14 @@ static ScanPlan plan_scan(int64_t n, int32_t f, int64_t graphs, bool equal, bool
     const int64_t length = n / graphs, vectors = (f + 3) / 4;
     // Graphs of one length that are a thread's whole work, single tokens above all: x and gates are read once.  Up to 128 rows where there are enough threads (64 k rows of
     // 256 bf16 columns in graphs of 64: 39 us with the three launches, 20 so), of few rows only the shortest.  (The gradient wants graphs that start where states are kept.)
-    const int64_t longest = n <= kFewRows ? 4 : graphs * vectors >= kScanSms * 256 ? 128 : 64;
+    const int64_t longest = n <= 512 ? 4 : graphs * vectors >= kScanSms * 256 ? 128 : 64;
     if (equal && n > 0 && length <= longest && (!back || length % kStateRows == 0)) {
         p.direct = true;
         p.chunk_rows = (int32_t)length;
         p.chunks = graphs;
         return p;
     }
-    if (n <= kFewRows && (!back || n * f <= kFewValues)) {
+    if (n <= (back ? kFewRows / 2 : kFewRows) && (!back || n * f <= kFewValues)) {
         // as many blocks as leave a thread no more than eight rows, up to the eight of a cluster
         const int64_t ways = back ? Few<true>::kWays : Few<false>::kWays, unit = back ? kStateRows : 2;
         p.few = 1;
