@@ -186,19 +186,24 @@ __global__ void __launch_bounds__(kRotaryBlock, INTERLEAVED ? 4 : 3) rotary_rows
             unit[k].load(x + (row0 + row[k]) * a.ldx + column[k], a.half);
         }
         if (base == threadIdx.x) {                       // (uniform: the first turn of every thread)
-            for (int r = threadIdx.x; r < rows; r += kRotaryBlock) position[r] = position_of(a, row0 + r);
-            __syncthreads();
             // threads have a pair each and go from row to row with it; where there are more pairs than threads, from pair to pair
             const int across = min(a.half, kRotaryBlock), down = kRotaryBlock / across;
             const int mine = a.half > kRotaryBlock ? 0 : over(threadIdx.x, a.by_half);
+            int i = threadIdx.x - mine * across;
+            double freq = a.freq[min(i, a.half - 1)];
+            for (int r = threadIdx.x; r < rows; r += kRotaryBlock) position[r] = position_of(a, row0 + r);
+            __syncthreads();
             if (mine < down)
-                for (int i = threadIdx.x - mine * across; i < a.half; i += across) {
-                    const double quarters = a.freq[i] * 0.63661977236758138;      // 2 / pi
+                for (;;) {
+                    const double quarters = freq * 0.63661977236758138;           // 2 / pi
                     for (int r = mine; r < rows; r += down) {
                         const float2 t = turn_of(a, position[r], quarters);
                         cosine[r * a.half + i] = t.x;
                         sine[r * a.half + i] = t.y;
                     }
+                    i += across;
+                    if (i >= a.half) break;
+                    freq = a.freq[i];
                 }
             __syncthreads();
         }
