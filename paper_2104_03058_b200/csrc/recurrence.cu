@@ -1109,7 +1109,7 @@ __device__ __forceinline__ uint32_t cluster_size()
 }
 __device__ __forceinline__ void cluster_meets()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 // a map in the shared memory of another block of the cluster, at the same place as `here`
 __device__ __forceinline__ float2 map_of_block(const float2* here, uint32_t rank)
@@ -1240,26 +1240,51 @@ static int check_scan(int64_t n, int32_t f, int form, int64_t graphs, const void
     return GNNFD_OK;
 }
 
+// Blocks of `recurrence_rows` for chunks of some rows, and how many the chip holds.
+struct RowsShape {
+    uint32_t places, block, held;
+};
 template <typename TI, int W, int P, bool SIGMOID, bool BACK>
-static void launch_sums(ScanArgs& a, cudaStream_t s)
+static RowsShape rows_shape(const ScanArgs& a)
 {
+    constexpr int kBlock = BACK ? kGradBlock : kRowsBlock;
+    static const int held = blocks_per_sm(recurrence_rows<TI, W, P, SIGMOID, BACK>, kBlock, 0);
+    return RowsShape{(uint32_t)((a.f / W + P - 1) / P), kBlock, (uint32_t)(held * kScanSms)};
+}
+
+// Chunks as long as make few blocks fill the chip evenly: the time of a launch goes by the rounds of blocks that it takes and by a chunk's rows, beside which the start and
+// end of a block weigh like six.  133 k x 256 bf16, 518 blocks of 32 rows for 592 places 37 us, 592 of 28 34; gradient of 50 k x 128 bf16, chunks of 16 (1563 blocks for
+// 1480 places, two rounds) 29 us, of 24 27.
+template <bool BACK>
+static int32_t balanced(const ScanArgs& a, uint32_t held_sums, const RowsShape& r)
+{
+    constexpr uint32_t kUnit = BACK ? kStateRows : 4, kEnds = 6, kWeight = BACK ? 2 : 1;
+    const uint32_t n = (uint32_t)a.n, longest = (uint32_t)a.chunk_rows;
+    auto over = [](uint32_t x, uint32_t y) { return (x + y - 1) / y; };
+    auto rounds_of_sums = [&](uint32_t rows) { return over(over(n, rows * a.ways) * a.column_tiles, held_sums); };
+    if (rounds_of_sums(longest) > 4) return a.chunk_rows;
+    uint32_t best = longest, least = ~0u;
+    for (uint32_t rows = longest / 2; rows <= (longest == 16 ? 32u : longest); rows += kUnit) {
+        const uint32_t chunks = over(n, rows), rounds = rounds_of_sums(rows) + kWeight * over((uint32_t)(((uint64_t)chunks * r.places + r.block - 1) / r.block), r.held);
+        if ((rows + kEnds) * rounds <= least) {
+            least = (rows + kEnds) * rounds;
+            best = rows;
+        }
+    }
+    return (int32_t)best;
+}
+
+template <typename TI, int W, int P, bool SIGMOID, bool BACK>
+static void launch_sums(ScanArgs& a, const RowsShape& r, cudaStream_t s)
+{
+    static const int held = blocks_per_sm(recurrence_sums<TI, W, P, SIGMOID, BACK>, kRowsBlock, 0);
     a.places = (a.f / W + P - 1) / P;
     // 32 lanes of a row, or as many as waste no more than an eighth of them, down to 8
     a.lanes = 32;
     while (a.lanes > 8 && (a.places + a.lanes - 1) / a.lanes * a.lanes * 7 > a.places * 8) a.lanes /= 2;
     a.ways = a.tile_chunks = kRowsBlock / a.lanes;
     a.column_tiles = (a.places + a.lanes - 1) / a.lanes;
-    // Where there are few blocks, chunks as long as make them fill the chip's places evenly: 133 k x 256 bf16, 518 blocks of 32 rows a chunk for 592 places
-    // 37 us, 592 of 28 34; 1 M x 128 fp32 163 and 153.
-    constexpr int kUnit = BACK ? kStateRows : 4, kPlaces = 4 * kScanSms;
-    const int64_t longest = a.chunk_rows, blocks = (a.n + longest * a.ways - 1) / (longest * a.ways) * a.column_tiles, waves = (blocks + kPlaces - 1) / kPlaces;
-    if (waves <= 4) {
-        int64_t tiles = kPlaces * waves / a.column_tiles, rows;
-        tiles = tiles < 1 ? 1 : tiles;
-        rows = (a.n + tiles * a.ways - 1) / (tiles * a.ways);
-        rows = (rows + kUnit - 1) / kUnit * kUnit;
-        a.chunk_rows = (int32_t)(rows < longest / 2 ? longest / 2 : rows > longest ? longest : rows);
-    }
+    a.chunk_rows = balanced<BACK>(a, (uint32_t)(held * kScanSms), r);
     a.chunks = (int32_t)(((int64_t)a.n + a.chunk_rows - 1) / a.chunk_rows);
     a.tiles = (a.chunks + a.ways - 1) / a.ways;
     GNNFD_LAUNCH("recurrence_sums", s, (recurrence_sums<TI, W, P, SIGMOID, BACK>), (unsigned)(a.tiles * a.column_tiles), kRowsBlock, 0, a);
@@ -1296,19 +1321,25 @@ static int run_scan(ScanArgs& a, const ScanPlan& p, cudaStream_t s)
     a.chunks = (int32_t)p.chunks;
     // (8 bf16 elements a thread where there are enough threads all the same)
     const int most = xs == 2 && (int64_t)a.n * a.f >= (int64_t)kScanSms * 512 * 8 * p.chunk_rows ? 8 : 4;
+    // (the gradient's walk has no wider threads than of 4 elements: its shared memory)
+    const int rows = widest(BACK ? 4 : most, true);
+    auto with_rows = [&](auto f) {
+        with_vector<TI>(rows, [&](auto w) {
+            constexpr int W = decltype(w)::value < 4 || !BACK ? decltype(w)::value : 4;
+            f(std::integral_constant<int, W>(), std::integral_constant<int, W < 4 ? 4 / W : 1>());
+            return 0;
+        });
+    };
     if (!p.few && !p.direct) {
+        RowsShape shape{};
+        with_rows([&](auto w, auto q) { shape = rows_shape<TI, decltype(w)::value, decltype(q)::value, SIGMOID, BACK>(a); });
         with_vector<TI>(widest(most, false), [&](auto w) {
             constexpr int W = decltype(w)::value;
-            launch_sums<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, s);
+            launch_sums<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, shape, s);
             return 0;
         });
     }
-    // (the gradient's walk has no wider threads than of 4 elements: its shared memory)
-    with_vector<TI>(widest(BACK ? 4 : most, true), [&](auto w) {
-        constexpr int W = decltype(w)::value < 4 || !BACK ? decltype(w)::value : 4;
-        launch_rows<TI, W, W < 4 ? 4 / W : 1, SIGMOID, BACK>(a, (unsigned)p.few, s);
-        return 0;
-    });
+    with_rows([&](auto w, auto q) { launch_rows<TI, decltype(w)::value, decltype(q)::value, SIGMOID, BACK>(a, (unsigned)p.few, s); });
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
 }
