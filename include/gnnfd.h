@@ -578,7 +578,7 @@ int gnnfd_kernel_timing_enable(int on);
 int gnnfd_kernel_timing_read(const char** names, double* ms, int64_t* launches, int capacity);
 
 /* Drill of gnnfd_combine's give-up path, for tests.  (The paper has no counterpart.)  It arms the NEXT
- * gnnfd_combine / gnnfd_combine_ex / gnnfd_layer_* call made by this host thread, and only that one: every
+ * gnnfd_combine / gnnfd_combine_ex / gnnfd_layer_gcn / _sage / _gat call made by this host thread, and only that one: every
  * barrier wait of that launch is limited to wait_ns nanoseconds (0 keeps the usual second; at most 10^9) and the
  * loads of K block skip_k_block (32 fp32 or 64 bf16 columns of x per block; -1: none) are never issued.
  * Nothing is in flight for the block that was left out, so the waits of the other lanes run out, every thread

@@ -352,7 +352,7 @@ static int layer_vector(const LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt
 template <typename TI, int V, int N, int TEAM>
 static void launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
 {
-    constexpr int kRows = sizeof(TI) == 4 || N > 16 ? 1 : 2;
+    constexpr int kRows = sizeof(TI) == 4 ? (N == 4 ? 4 : 1) : N > 16 ? 1 : 2;      // rows of a lane, on their way and worked on
     const int lanes = (a.nvec + N / V - 1) / (N / V);
     a.lanes = TEAM >= 32 ? (lanes + 31) / 32 * 32 : 1 << ilog2(lanes);
     a.groups = a.lanes < kLayerBlock ? kLayerBlock / a.lanes : 1;

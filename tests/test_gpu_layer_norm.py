@@ -1,7 +1,7 @@
 """Layer norm and its gradients against an evaluation in 64 bits.
 
-Tolerances are first-order bounds, computed beside the reference (u = 2^-24 a rounding).  A sum over a row has a depth of 18 additions at most: 8 values of a lane,
-5 steps in a warp, 5 over warps.  The mean is then off by 20 u mean|x| (two more roundings for the division), the variance by 24 u of itself and what
+Tolerances are first-order bounds, computed beside the reference (u = 2^-24 a rounding).  A sum over a row has a depth of 18 additions at most: 8 in a lane (two
+sums of 8 values, then both; 12 where a row is a warp's and has 24 values a lane), 5 steps in a warp, 5 over warps.  The mean is then off by 20 u mean|x| (two more roundings for the division), the variance by 24 u of itself and what
 the mean's error makes of it, rstd by half of that, 1 u for adding eps and 4 u for the reciprocal root.  Columns of dw and db are summed
 over at most 300 roundings here: rows of a thread, groups of a block, then 64 bits.  Being bounds, they are wide for most values, so fp32
 results also have to be within 8 u in the root mean square: an output carries about six roundings of half a step.  (From 8 columns on.  Errors of xhat and dx grow with rstd and
