@@ -503,7 +503,8 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * Rows graph_ptr[b] .. graph_ptr[b + 1] - 1 are graph b, in order; its first row's h[t - 1] is d_initial[b] (fp32 [graphs, f]; NULL: 0).  d_graph_ptr [graphs + 1]
  * of type itype, ascending from 0; NULL: graphs of n / graphs rows each (n must be a multiple), so graphs = n is one token for each of n sequences.  Rows
  * behind the last offset are left as they are; graphs may be empty (their last state is the first one).  Offsets outside [0, n] or not ascending are cut to what is
- * inside: nothing outside of the arrays is touched.  d_x, d_gate [n, ld] of type dt, d_out [n, ldo] of type odt, not overlapping them.  d_final (fp32
+ * inside: nothing outside of the arrays is touched.  d_x, d_gate [n, ld] of type dt, d_out [n, ldo] of type odt, not overlapping them nor d_initial (a
+ * copy of the last row of a stretch that goes on in the same buffer will do; for single tokens, graphs = n without d_graph_ptr, d_initial may be d_out itself, fp32 with ldo = f).  d_final (fp32
  * [graphs, f], may be NULL) receives the last state of each graph; it may be d_initial itself where graphs = n and d_graph_ptr is NULL, and does not overlap it otherwise.  d_states
  * (may be NULL): fp32 [(n + 7) / 8, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
  * d_scratch: gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, d_graph_ptr == NULL, 0) bytes, 256-byte aligned (0

@@ -205,6 +205,13 @@ def _extent(t):
     return (begin, begin + (last + 1) * t.element_size())
 
 
+def _pitch_and_width(t):
+    """Bytes from row to row (0: a single stretch) and of a row."""
+    if t.is_contiguous() or t.shape[0] == 1:
+        return 0, t.numel() * t.element_size()
+    return t.stride(0) * t.element_size(), (t.shape[1] if t.dim() == 2 else 1) * t.element_size()
+
+
 def _no_overlap(a, b, name_a: str, name_b: str):
     """The kernels read features through the read-only data path, so an output that overlaps an input
     is undefined behaviour the header forbids: refuse it here."""
@@ -213,15 +220,14 @@ def _no_overlap(a, b, name_a: str, name_b: str):
     if not (a0 < b1 and b0 < a1):
         return
     # Two column ranges of one row-major buffer interleave row by row without sharing an element: same row
-    # pitch, and the column intervals (taken modulo the pitch) apart.
-    if a.dim() == 2 and b.dim() == 2 and a.shape[0] > 1 and b.shape[0] > 1:
-        pitch_a, pitch_b = a.stride(0) * a.element_size(), b.stride(0) * b.element_size()
-        if pitch_a == pitch_b and pitch_a > 0:
-            first, second = (a, b) if a0 <= b0 else (b, a)
-            off = (max(a0, b0) - min(a0, b0)) % pitch_a
-            w_first = first.shape[1] * first.element_size()
-            w_second = second.shape[1] * second.element_size()
-            if w_first <= off and off + w_second <= pitch_a:
+    # pitch (a contiguous tensor is one row, which goes with any), and the column intervals (taken modulo the pitch) apart.
+    if a.dim() <= 2 and b.dim() <= 2:
+        (pitch_a, width_a), (pitch_b, width_b) = _pitch_and_width(a), _pitch_and_width(b)
+        pitch = max(pitch_a, pitch_b)
+        if pitch > 0 and min(pitch_a, pitch_b) in (0, pitch):
+            w_first, w_second = (width_a, width_b) if a0 <= b0 else (width_b, width_a)
+            off = (max(a0, b0) - min(a0, b0)) % pitch
+            if w_first <= off and off + w_second <= pitch:
                 return
     raise ValueError("%s and %s overlap in memory" % (name_a, name_b))
 
@@ -1191,7 +1197,7 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
     """gnnfd_linear_recurrence: h[t] = a[t] h[t - 1] + b[t] down the rows of each graph of a batch, per column; ``form`` "factor": a = gate,
     b = x, "sigmoid": a = 1 / (1 + exp(-gate)), b = (1 - a) x.  ``graph_ptr`` [graphs + 1] holds the graphs' row offsets; without it the rows are
     ``graphs`` (1) graphs of one length, so graphs = n is a single token for each of n sequences.  ``initial`` [graphs, f]: states ahead of the
-    first rows.  Rows behind the last offset keep what ``out`` holds (undefined where the call allocates it).  Returns out, with ``with_final`` or
+    first rows; it does not lie in ``out`` (for single tokens it may be ``out``).  Rows behind the last offset keep what ``out`` holds (undefined where the call allocates it).  Returns out, with ``with_final`` or
     ``final`` (filled; for single tokens it may be ``initial``) also the last states, with ``with_states`` also what linear_recurrence_backward takes."""
     index = x.get_device()
     if index >= 0 and index != _current_device():
@@ -1210,6 +1216,9 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
         _need_rows_of(out, n, "out")
         _no_overlap(x, out, "x", "out")
         _no_overlap(gate, out, "gate", "out")
+        # (a single token's state is read by the thread that then writes its result to the same place)
+        if initial is not None and not (graph_ptr is None and graphs == n and ip == op and out.dtype == initial.dtype and (n == 1 or ldo == f)):
+            _no_overlap(initial, out, "initial", "out")
     if final is not None:
         if initial is not None and not (ip == fp and graph_ptr is None and graphs == n):
             _no_overlap(initial, final, "initial", "final")
@@ -1217,8 +1226,6 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
         _no_overlap(gate, final, "gate", "final")
         if not fresh:
             _no_overlap(final, out, "final", "out")
-            if initial is not None and ip != fp:
-                _no_overlap(initial, out, "initial", "out")
     elif with_final:
         final = _new(x, (graphs, f), torch.float32, stream)
         fp = final.data_ptr()

@@ -1240,6 +1240,16 @@ static int check_scan(int64_t n, int32_t f, int form, int64_t graphs, const void
     return GNNFD_OK;
 }
 
+// Whether `bytes` bytes from p on share any with n rows of `width` bytes, `pitch` apart.
+static bool shares_rows(const void* p, int64_t bytes, const void* rows, int64_t n, int64_t pitch, int64_t width)
+{
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)rows;
+    if (!p || n == 0 || a + bytes <= b || b + (n - 1) * pitch + width <= a) return false;
+    if (a < b) return true;
+    const int64_t off = (int64_t)((a - b) % (uintptr_t)pitch);
+    return off < width || off + bytes > pitch;
+}
+
 // Blocks of `recurrence_rows` for chunks of some rows, and how many the chip holds.
 struct RowsShape {
     uint32_t places, block, held;
@@ -1386,6 +1396,11 @@ int gnnfd_linear_recurrence(int64_t n, const void* d_x, int64_t ldx, const void*
     if (rc) return rc;
     if (ldx < f || ldg < f || ldo < f || (n > 0 && (!d_x || !d_gate || !d_out))) return GNNFD_INVALID_ARG;
     if (d_final && d_final == d_initial && (d_graph_ptr || graphs != n)) return GNNFD_INVALID_ARG;
+    // (a state that lies in the results would be written before some threads read it, but for those of single tokens)
+    const int os = odt == GNNFD_F32 ? 4 : 2;
+    if (!(!d_graph_ptr && graphs == n && d_initial == d_out && odt == GNNFD_F32 && (ldo == f || n == 1)) &&
+        shares_rows(d_initial, graphs * f * 4, d_out, n, ldo * os, (int64_t)f * os))
+        return GNNFD_INVALID_ARG;
     ScanArgs a{};
     a.x = d_x; a.gate = d_gate; a.out = d_out; a.ptr = d_graph_ptr; a.first = d_initial; a.last = d_final; a.states = d_states;
     a.ldx = ldx; a.ldg = ldg; a.ldo = ldo; a.n = (int32_t)n; a.graphs = (int32_t)graphs; a.length = (int32_t)(n / graphs); a.f = f;

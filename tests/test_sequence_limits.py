@@ -1,0 +1,69 @@
+"""What the layer norm, rotary and recurrence calls refuse or accept at their limits: host logic, before any launch."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2104_03058_b200 as g  # noqa: E402
+from paper_2104_03058_b200 import binding as b  # noqa: E402
+
+P = 1 << 20                                          # an aligned address that nothing reads
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The binding's checks on CPU tensors: a library that records its calls, operands taken without the test for their device."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: made.append((name, args)) or g.OK
+
+    def matrix(t, cols, name):
+        assert t.dim() == 2 and t.shape[1] >= cols
+        return t.data_ptr(), t.stride(0)
+
+    monkeypatch.setattr(b, "lib", Library)
+    monkeypatch.setattr(b, "_matrix", matrix)
+    monkeypatch.setattr(b, "_index_list", lambda t, name: (t.data_ptr(), t.numel(), b.I64))
+    monkeypatch.setattr(b, "_stream_handle", lambda index, stream: 0)
+    return made
+
+
+def test_states_do_not_lie_in_the_results(calls):
+    """A sequence in stretches that share one buffer: the row that the next stretch starts from is written before other threads read it."""
+    n, f = 64, 8
+    x, buf, wide = torch.zeros(n, f), torch.zeros(n, f), torch.zeros(n, 2 * f)
+    ptr, final = torch.tensor([0, 10, n]), torch.zeros(1, f)
+    for more in (dict(), dict(with_final=True), dict(final=final), dict(with_states=True)):
+        for initial, out in ((buf[-1:], buf), (buf[:1], buf), (wide[5:6, :f], wide[:, :f]), (wide.view(-1)[12:12 + f][None], wide[:, :f]), (buf[3:4], buf)):
+            with pytest.raises(ValueError, match="initial and out overlap"):
+                b.linear_recurrence(x, x, initial=initial, out=out, **more)
+    with pytest.raises(ValueError, match="initial and out overlap"):
+        b.linear_recurrence(x, x, graph_ptr=ptr, initial=buf[:2], out=buf)
+    with pytest.raises(ValueError, match="initial and out overlap"):
+        b.linear_recurrence(x, x, graphs=n // 4, initial=buf[:n // 4], out=buf)
+    assert not calls
+
+
+def test_states_beside_the_results_and_single_tokens_in_place(calls):
+    n, f = 64, 8
+    x, buf, wide = torch.zeros(n, f), torch.zeros(n, f), torch.zeros(n, 2 * f)
+    b.linear_recurrence(x, x, initial=torch.zeros(1, f), out=buf)
+    b.linear_recurrence(x, x, initial=wide[7:8, f:], out=wide[:, :f])             # between two rows of the results
+    b.linear_recurrence(x, x, graphs=n, initial=buf, out=buf)
+    b.linear_recurrence(x[:1], x[:1], initial=wide[7:8, :f], out=wide[7:8, :f])
+    assert len(calls) == 4
+    for initial, out in ((buf, wide[:, :f]), (wide.view(-1)[:n * f].view(n, f), wide[:, :f]), (buf.view(-1)[:n * f].view(n, f), buf.view(torch.bfloat16)[:, :f])):
+        if initial.data_ptr() == out.data_ptr():
+            with pytest.raises(ValueError, match="initial and out overlap"):       # another pitch or type than its own
+                b.linear_recurrence(x, x, graphs=n, initial=initial, out=out)
+
+
+def test_the_c_call_refuses_states_in_the_results():
+    L = g.lib()
+    scan = lambda first, out=P, ldo=8, odt=0, n=9000, graphs=1, ptr=None: (      # noqa: E731
+        L.gnnfd_linear_recurrence(n, 2 * P, 8, 3 * P, 8, 0, 8, 1, graphs, ptr, 0, first, out, ldo, odt, None, None, 4 * P, 1 << 40, None))
+    for first in (P, P + 4, P + 8999 * 32, P + 8999 * 32 + 28, P - 28):
+        assert scan(first) == g.INVALID_ARG
+    assert scan(P + 64 * 77, ldo=16) == scan(P + 64 * 77 + 60, ldo=16) == scan(P + 16 * 33, odt=1) == scan(P, n=9, graphs=3) == g.INVALID_ARG
+    assert scan(P, n=9, graphs=9, odt=1) == scan(P, n=9, graphs=9, ldo=9) == scan(P + 32, n=9, graphs=9) == scan(P, n=9, graphs=9, ptr=5 * P) == g.INVALID_ARG
