@@ -4,7 +4,9 @@
 //   g = dout * w,   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)),   dw = sum over the rows of dout * xhat,   db = sum over the rows of dout
 //
 // Bound by HBM: x is read once and stays in registers, so the variance is a sum of squares of distances from the mean that has been found
-// already.  A lane holds N = 16 elements of a row in vectors of 16 bytes (fewer where rows do not allow them), so a row has f / 16 lanes: part of a warp, a
+// already.  That mean is a rounded sum, off by up to 20 roundings of the values' size: the distances' own mean, which is what it is off by, is found beside their
+// squares and taken off mean, variance and distances (as sums leave them, rows of 12345.678 in 96 columns gave 0.3 in place of 0).  This costs odd widths and bf16 rows of
+// 4100 columns, which instructions bound, 6 to 11 %, others 2 % at most; as a branch for the rows that need it, it cost no less.  A lane holds N = 16 elements of a row in vectors of 16 bytes (fewer where rows do not allow them), so a row has f / 16 lanes: part of a warp, a
 // warp, or (WIDE) several warps that meet in shared memory.  Rows of 513 to 768 columns have 24 elements a lane, so that they need no meeting.  Blocks stay, as many as
 // the chip holds, and take rows in turn; the next row's loads are issued before this one is worked on.  In the gradient the sums of dw and db over the rows that
 // a lane has seen stay in registers as well; a second launch adds the blocks' sums up in 64 bits in ascending order.
@@ -14,6 +16,8 @@
 // 17 and 287 us without; the weights in shared memory instead of registers leave room for twice the warps, 64 to 512 columns 255 -> 200 us for 400 MB a tensor.)
 // Measured, 400 MB a tensor, fp32 / bf16: forward 0.87 - 0.97 of the copy peak, gradient 0.90 - 0.99 / 0.81 - 0.92 from 64 columns on; bf16 rows of 600 columns
 // 0.75 and 0.68 (a quarter of the lanes' places are empty), odd numbers of bf16 columns 0.3 to 0.6 (elements of 2 bytes one by one).
+#include <math.h>
+
 #include <type_traits>
 
 #include "schedule.cuh"
@@ -37,27 +41,49 @@ struct LayerArgs {
     int32_t f, nvec, lanes, groups, out_bf16;    // vectors and lanes of a row, rows side by side in a block
 };
 
-// The sums of N values over the lanes of a row, in all of them.  WIDE: lanes are whole warps; `red` has room for two calls in turn.
-template <int N, bool WIDE>
-__device__ __forceinline__ void row_sums(float (&s)[N], int lanes, float (*red)[32])
+// The sums of N values over the lanes of a row, in all of them.  TEAM > 32: lanes are whole warps of a block of up to TEAM threads; `red` has room for two calls in
+// turn.  Shuffles take as long as four other instructions there: of two values each half of a warp adds up one (the same additions in the same order), and the
+// warps' sums are added up by as many lanes as there are warps, several values side by side.  (With a shuffle for every step and value, rows of 1024 to 8192 bf16
+// columns 8 to 11 % slower.)
+constexpr int kRed = 40;                          // (rows of eight sums that are read side by side lie in different banks)
+template <int N, int TEAM>
+__device__ __forceinline__ void row_sums(float (&s)[N], int lanes, float (*red)[kRed])
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (WIDE || o < lanes)
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
-    if constexpr (WIDE) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5, first = threadIdx.x / lanes * warps;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) red[i][warp] = s[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = lane < warps ? red[i][first + lane] : 0.f;
+    if constexpr (TEAM <= 32) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
+            if (o < lanes)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+                for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+    } else {
+        constexpr int M = N % 2 == 0 ? N / 2 : N;             // values that a lane adds up
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5, first = threadIdx.x / lanes * warps;
+        const bool upper = M < N && lane >= 16;
+        float sum[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            sum[i] = upper ? s[i + N - M] : s[i];
+            sum[i] += __shfl_xor_sync(0xffffffffu, upper ? s[i] : s[i + N - M], 16);
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < M; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        if ((lane & (M < N ? 15 : 31)) == 0)
+#pragma unroll
+            for (int i = 0; i < M; ++i) red[i + (upper ? M : 0)][warp] = sum[i];
+        __syncthreads();
+        constexpr int P = TEAM / 32, G = 32 / P, R = N > G ? N / G : 1;      // lanes for a value, values side by side, one after the other
+        const int way = lane % P, group = lane / P;
+        float t[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) t[r] = way < warps ? red[N > G ? group * R + r : group % N][first + way] : 0.f;
+#pragma unroll
+        for (int o = P / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int r = 0; r < R; ++r) t[r] += __shfl_xor_sync(0xffffffffu, t[r], o);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = N == 1 ? t[0] : __shfl_sync(0xffffffffu, t[i % R], i / R * P);
     }
 }
 
@@ -153,7 +179,7 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM) layer
 {
     grid_dependency<true>();
     constexpr bool WIDE = TEAM > 32;
-    __shared__ float red[2][ROWS][32];
+    __shared__ float red[2][2 * ROWS][kRed];
     const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
     float w[N], b[N];
     load_columns<V>(a.weight, a, lanes, lane, 1.f, w);
@@ -174,32 +200,35 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM) layer
     int64_t base = (int64_t)blockIdx.x * per_block;
     fetch(base);
     for (; base < a.n; base += step) {
-        float x[ROWS][N], mean[ROWS], var[ROWS];
+        float x[ROWS][N], mean[ROWS], sums[2 * ROWS];
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) next[u].get(x[u]);
         fetch(base + step);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) mean[u] = total(x[u]);
-        row_sums<ROWS, WIDE>(mean, lanes, red[0]);
+        row_sums<ROWS, TEAM>(mean, lanes, red[0]);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
             mean[u] *= a.inv_f;
             const float shift[1] = {mean[u]};
             add_minus(x[u], shift);
             clear_outside<V>(lanes, left, x[u]);
-            var[u] = dot(x[u], x[u]);
+            sums[2 * u] = total(x[u]);
+            sums[2 * u + 1] = dot(x[u], x[u]);
         }
-        row_sums<ROWS, WIDE>(var, lanes, red[1]);
+        row_sums<2 * ROWS, TEAM>(sums, lanes, red[1]);
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
             const int64_t row = base + group + u * a.groups;
-            const float rstd = rsqrtf(fmaf(var[u], a.inv_f, a.eps));
+            // (squares beyond the type's range stay infinite, NaN stays NaN)
+            const float off = sums[2 * u] * a.inv_f, squares = sums[2 * u + 1] * a.inv_f;
+            const float rstd = rsqrtf((squares < INFINITY ? fmaxf(fmaf(-off, off, squares), 0.f) : squares) + a.eps);
             if (row >= a.n) continue;
-            scale(x[u], rstd);
+            scale_shift(x[u], rstd, -off * rstd);
             scale_shift(x[u], w, b);
             store_lane<V>(a, row * a.ldo + lane * V, lanes, left, x[u]);
             if (a.mean && lane == 0) {
-                a.mean[row] = mean[u];
+                a.mean[row] = mean[u] + off;
                 a.rstd[row] = rstd;
             }
         }
@@ -236,7 +265,7 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
 {
     grid_dependency<true>();
     constexpr bool WIDE = TEAM > 32;
-    __shared__ float red[2][2][32];
+    __shared__ float red[2][2][kRed];
     __shared__ __align__(16) float columns[(TEAM < kLayerBlock ? kLayerBlock : TEAM) * N];      // the weights, at the end the sums of columns
     const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
     const int left = a.nvec - lane;
@@ -278,7 +307,7 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
         if (a.weight) multiply_lane<V>(d, columns + lane * V, lanes);
         sums[0] = total(d);
         sums[1] = dot(d, x);
-        row_sums<2, WIDE>(sums, lanes, red[turn]);
+        row_sums<2, TEAM>(sums, lanes, red[turn]);
         if (row >= a.n) continue;
         // rstd (d - m1 - x m2)
         scale(x, -sums[1] * a.inv_f);

@@ -36,3 +36,44 @@ def test_single_tokens_in_place_of_their_states():
         x, gate, state = scan.rand(n, f, seed=1).contiguous(), scan.gates("sigmoid", n, f, seed=2), scan.rand(n, f, seed=3).contiguous()
         want = g.linear_recurrence(x, gate, graphs=n, initial=state)
         assert g.linear_recurrence(x, gate, graphs=n, initial=state, out=state) is state and torch.equal(state, want)
+
+
+# ---------------------------------------------------------------- layer norm
+
+@pytest.mark.parametrize("xdt", [F32, BF16])
+@pytest.mark.parametrize("f", [1, 3, 41, 96, 100, 600, 602, 1000, 4100, 8191])
+def test_rows_of_equal_values(f, xdt):
+    """A row's mean is a sum of f values (off by 20 u of itself as in the norm's own tests); the distances from it are exact, and their mean, another such sum, is taken off:
+    440 u^2 |value| are left (the product with rstd adds one rounding of 20 u), times rstd = eps^-1/2 = 317.  The mean is then the value itself, so that the gradient's
+    xhat, dw and the part of dx with xhat are exactly zero: dx = rstd (dout - mean(dout)), rstd within 8 u: (20 u)^2 of the value in
+    the variance, less than u of eps for values below 1e4 and 10 u for 12345.678 (half of that in rstd), and 4 u for adding and the root."""
+    eps, n = 1e-5, 70
+    bias = torch.linspace(-1.0, 1.0, f, device="cuda")
+    dout = torch.randn((n, f), generator=torch.Generator(device="cuda").manual_seed(f), device="cuda").to(xdt)
+    for value in (0.1, -10.1, 1000.1, 12345.678):
+        x = torch.full((n, f), value, device="cuda", dtype=xdt)
+        value = abs(float(x[0, 0]))
+        out, mean, rstd = g.layer_norm(x, None, bias, eps, with_stats=True)
+        assert ((out - bias).abs() <= 317 * 440 * U * U * value + 2 * U * bias.abs()).all(), (value, float((out - bias).abs().max()))
+        assert (mean == x[:, 0].float()).all()
+        assert ((rstd.double() * eps ** 0.5 - 1).abs() <= 10 * U).all()
+        dx, dw, db = g.layer_norm_backward(dout, x, mean, rstd)
+        do = dout.double()
+        assert (dw == 0).all()
+        size = do.abs() + do.abs().mean(1, keepdim=True)
+        assert ((dx.double() - eps ** -0.5 * (do - do.mean(1, keepdim=True))).abs() <= 317 * (10 + 24) * U * size).all()
+    # squares of the rounded distances beyond the type's range
+    assert torch.equal(g.layer_norm(torch.full((n, f), 3e30, device="cuda", dtype=xdt), None, bias), bias.expand(n, f))
+
+
+@pytest.mark.parametrize("f", [96, 602, 4100])
+def test_rows_whose_spread_is_below_the_means_roundings(f):
+    """Values 4096 + k 2^-11, k of -8 to 8, all exact in fp32: the mean as a sum is off by more than the spread.  Distances from it are exact or off by a rounding
+    of themselves, sums of them and of their squares by 20 and 24 roundings of a distance's size, which is up to 20 u 4096 = 2^-7.7 beside a spread of 2^-8.6: three roundings in place
+    of one, (60 + 40) u of xhat's size and as much for the part of rstd."""
+    k = torch.randint(-8, 9, (300, f), generator=torch.Generator(device="cuda").manual_seed(f), device="cuda")
+    x = 4096 + k.double() * 2.0 ** -11
+    out = g.layer_norm(x.float(), eps=1e-9).double()
+    off = x - x.mean(1, keepdim=True)
+    want = off / ((off ** 2).mean(1, keepdim=True) + 1e-9).sqrt()
+    assert float((out - want).abs().max()) <= 200 * U * float(want.abs().max())
