@@ -5,11 +5,14 @@
 //
 // Bound by HBM: x is read once and stays in registers, so the variance is a sum of squares of distances from the mean that has been found
 // already.  That mean is a rounded sum, off by up to 20 roundings of the values' size: the distances' own mean, which is what it is off by, is found beside their
-// squares and taken off mean, variance and distances (as sums leave them, rows of 12345.678 in 96 columns gave 0.3 in place of 0).  This costs odd widths and bf16 rows of
-// 4100 columns, which instructions bound, 6 to 11 %, others 2 % at most; as a branch for the rows that need it, it cost no less.  A lane holds N = 16 elements of a row in vectors of 16 bytes (fewer where rows do not allow them), so a row has f / 16 lanes: part of a warp, a
+// squares and taken off mean, variance and distances (as sums leave them, rows of 12345.678 in 96 columns gave 0.3 in place of 0).  This costs odd widths and bf16
+// rows of 4100 columns, which instructions bound, 6 to 11 %, others 2 % at most; as a branch for the rows that need it, it cost no less.
+// A lane holds N = 16 elements of a row in vectors of 16 bytes (fewer where rows do not allow them), so a row has f / 16 lanes: part of a warp, a
 // warp, or (WIDE) several warps that meet in shared memory.  Rows of 513 to 768 columns have 24 elements a lane, so that they need no meeting.  Blocks stay, as many as
-// the chip holds, and take rows in turn; the next row's loads are issued before this one is worked on.  In the gradient the sums of dw and db over the rows that
-// a lane has seen stay in registers as well; a second launch adds the blocks' sums up in 64 bits in ascending order.
+// the chip holds, and take rows in turn; the next row's loads are issued before this one is worked on.
+// In the gradient the sums of dw and db over kSumRows rows of a lane stay in registers as well and are then added in 64 bits to what the lane has in shared
+// memory (rows and groups all in fp32: db of 233 k x 602 off by 4.4 * 2^-24 in the root mean square, growing with the root of the rows; now 1.4; that cost even
+// widths 0 to 3 %).  A block's sums are rounded once more, and a second launch adds them up in 64 bits, all in a fixed order.
 //
 // What counts beside the bytes is instructions: arithmetic is done on two elements at a time, addresses are a lane's base and constants, and columns that a lane
 // does not have are registers set to 0 once.  (The gradient of 233 k x 602 fp32, in vectors of two: 58 instructions an element and 452 us with the checks inside,
@@ -28,6 +31,7 @@ namespace gnnfd {
 constexpr int kLayerBlock = 256;
 constexpr int kLayerColumns = 8192;              // 512 lanes of 16 elements
 constexpr int kLayerSms = 148;
+constexpr int kSumRows = 16;                     // rows whose sums are fp32 (of 8: 1.1 in place of 1.4 * 2^-24, 0.3 to 2 % slower)
 constexpr int64_t kGradBlocks = 3 * kLayerSms;   // of the gradient at most: the workspace has a row of sums for each
 
 struct LayerArgs {
@@ -266,12 +270,34 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
     grid_dependency<true>();
     constexpr bool WIDE = TEAM > 32;
     __shared__ float red[2][2][kRed];
-    __shared__ __align__(16) float columns[(TEAM < kLayerBlock ? kLayerBlock : TEAM) * N];      // the weights, at the end the sums of columns
+    constexpr int kThreads = TEAM < kLayerBlock ? kLayerBlock : TEAM;
+    extern __shared__ __align__(16) float columns[];            // the weights
+    double2* const kept = reinterpret_cast<double2*>(columns + kThreads * N);       // kThreads apart, each lane's sums of dout * xhat and dout
+    const uint32_t own = (uint32_t)__cvta_generic_to_shared(kept + threadIdx.x);
     const int lanes = TEAM == 32 ? 32 : a.lanes, lane = WIDE ? threadIdx.x % lanes : threadIdx.x & (lanes - 1), group = threadIdx.x / lanes;
     const int left = a.nvec - lane;
     float dw[N], db[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+    if (a.part)
+#pragma unroll
+        for (int i = 0; i < N; ++i) kept[i * kThreads + threadIdx.x] = make_double2(0.0, 0.0);
+    auto put_away = [&] {
+        constexpr int U = 4;                                     // at a time (all together would take all the registers there are)
+#pragma unroll
+        for (int i = 0; i < N; i += U) {
+            double s[U], t[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                asm volatile("ld.volatile.shared.v2.f64 {%0, %1}, [%2];" : "=d"(s[u]), "=d"(t[u]) : "r"(own + (i + u) * kThreads * (int)sizeof(double2)));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                asm volatile("st.volatile.shared.v2.f64 [%0], {%1, %2};" ::"r"(own + (i + u) * kThreads * (int)sizeof(double2)), "d"(s[u] + dw[i + u]),
+                             "d"(t[u] + db[i + u]) : "memory");
+                dw[i + u] = db[i + u] = 0.f;
+            }
+        }
+    };
     const int64_t step = (int64_t)gridDim.x * a.groups;
     Share<TI, V, N> next_x, next_d;
     next_x.clear();
@@ -291,7 +317,8 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
     if (a.weight)
         for (int c = threadIdx.x; c < lanes * N; c += blockDim.x) columns[c] = c < a.f ? load4(a.weight + c) : 0.f;
     __syncthreads();
-    for (int turn = 0; base < a.n; base += step, turn ^= 1) {
+    for (int turn = 0; base < a.n; base += step, ++turn) {
+        if (a.part && turn % kSumRows == kSumRows - 1) put_away();       // (kSumRows - 1 the first time; here the fewest registers are in use)
         const int64_t row = base + group;
         float x[N], d[N], sums[2];
         next_x.get(x);
@@ -307,7 +334,7 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
         if (a.weight) multiply_lane<V>(d, columns + lane * V, lanes);
         sums[0] = total(d);
         sums[1] = dot(d, x);
-        row_sums<2, TEAM>(sums, lanes, red[turn]);
+        row_sums<2, TEAM>(sums, lanes, red[turn & 1]);
         if (row >= a.n) continue;
         // rstd (d - m1 - x m2)
         scale(x, -sums[1] * a.inv_f);
@@ -318,19 +345,33 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
         store_lane<V>(a, row * a.ldo + lane * V, lanes, left, x);
     }
     if (!a.part) return;
-    // the block's sums of each column, over its groups in ascending order
-    for (int k = 0; k < 2; ++k) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < N / V; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) columns[((group * (N / V) + j) * lanes + lane) * V + i] = k == 0 ? dw[j * V + i] : db[j * V + i];
-        __syncthreads();
-        for (int c = threadIdx.x; c < a.f; c += blockDim.x) {
-            float sum = 0.f;
-            for (int q = 0; q < a.groups; ++q) sum += columns[q * N * lanes + c];
-            a.part[((int64_t)blockIdx.x * 2 + k) * a.f + c] = sum;
+    // The block's sums of each column, over its groups in ascending order; where a row has fewer columns than the block threads, first every ways-th of them.
+    put_away();
+    __syncthreads();
+    const int cells = N * lanes, threads = a.groups * lanes, ways = TEAM < 32 && cells < threads ? threads / cells : 1;
+    auto sum_of = [&](const double2* of, int q, int end, int by) {
+        double2 sum = make_double2(0.0, 0.0);
+#pragma unroll 4
+        for (; q < end; q += by) {
+            const double2 s = of[q * lanes];
+            sum.x += s.x;
+            sum.y += s.y;
         }
+        return sum;
+    };
+    if (ways > 1) {
+        const int way = threadIdx.x / cells, cell = threadIdx.x - way * cells;
+        double2* const of = kept + cell / lanes * kThreads + cell % lanes;
+        if (way < ways) of[way * lanes] = sum_of(of, way, a.groups, ways);       // (nobody else reads what this way does)
+        __syncthreads();
+    }
+    for (int cell = threadIdx.x; cell < cells; cell += threads) {
+        const int i = cell / lanes, l = cell - i * lanes, c = (i / V * lanes + l) * V + i % V;
+        if (c >= a.f) continue;
+        const double2 sum = sum_of(kept + i * kThreads + l, 0, ways > 1 ? ways : a.groups, 1);
+        float* const part = a.part + (int64_t)blockIdx.x * 2 * a.f + c;
+        part[0] = (float)sum.x;
+        part[a.f] = (float)sum.y;
     }
 }
 
@@ -379,7 +420,7 @@ static int layer_vector(const LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt
 }
 
 template <typename TI, int V, int N, int TEAM>
-static void launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
+static int launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
 {
     constexpr int kRows = sizeof(TI) == 4 ? (N == 4 ? 4 : 1) : N > 16 ? 1 : 2;      // rows of a lane, on their way and worked on
     const int lanes = (a.nvec + N / V - 1) / (N / V);
@@ -388,15 +429,19 @@ static void launch_layer_norm(LayerArgs& a, int32_t* blocks, cudaStream_t s)
     const int64_t per_block = a.groups * (a.dout ? 1 : kRows), need = (a.n + per_block - 1) / per_block;
     constexpr int kThreads = TEAM < kLayerBlock ? kLayerBlock : TEAM;
     if (a.dout) {
-        static const int held = blocks_per_sm(layer_norm_grad<TI, V, N, TEAM>, kThreads, 0);
+        constexpr int kShared = kThreads * N * (int)(sizeof(float) + sizeof(double2));
+        const auto kernel = layer_norm_grad<TI, V, N, TEAM>;
+        if (kShared > 40 * 1024) GNNFD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared));
+        static const int held = blocks_per_sm(kernel, kThreads, kShared);
         const int64_t most = kLayerSms * held < kGradBlocks ? kLayerSms * held : kGradBlocks;
         *blocks = (int32_t)(need < most ? need : most);
-        GNNFD_LAUNCH("layer_norm_grad", s, (layer_norm_grad<TI, V, N, TEAM>), (unsigned)*blocks, a.groups * a.lanes, 0, a);
+        GNNFD_LAUNCH("layer_norm_grad", s, kernel, (unsigned)*blocks, a.groups * a.lanes, kShared, a);
     } else {
         static const int held = blocks_per_sm(layer_norm_rows<TI, V, N, kRows, TEAM>, kThreads, 0);
         *blocks = (int32_t)(need < kLayerSms * held ? need : kLayerSms * held);
         GNNFD_LAUNCH("layer_norm_rows", s, (layer_norm_rows<TI, V, N, kRows, TEAM>), (unsigned)*blocks, a.groups * a.lanes, 0, a);
     }
+    return GNNFD_OK;
 }
 
 static int run_layer_norm(LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt, int32_t* blocks, cudaStream_t s)
@@ -405,19 +450,18 @@ static int run_layer_norm(LayerArgs& a, gnnfd_dtype_t xdt, gnnfd_dtype_t odt, in
     a.nvec = a.f / v;
     auto run = [&](auto type) {
         using TI = decltype(type);
-        with_vector<TI>(v, [&](auto w) {
+        return with_vector<TI>(v, [&](auto w) {
             constexpr int V = decltype(w)::value;
-            if (V == 1 && a.f <= 4 * 32) launch_layer_norm<TI, V, V == 1 ? 4 : 16, 16>(a, blocks, s);
-            else if (a.f <= 16 * 16) launch_layer_norm<TI, V, 16, 16>(a, blocks, s);
-            else if (a.f <= 16 * 32) launch_layer_norm<TI, V, 16, 32>(a, blocks, s);
-            else if (a.f <= 24 * 32) launch_layer_norm<TI, V, 24, 32>(a, blocks, s);
-            else if (a.f <= 16 * kLayerBlock) launch_layer_norm<TI, V, 16, kLayerBlock>(a, blocks, s);
-            else launch_layer_norm<TI, V, 16, 512>(a, blocks, s);
-            return 0;
+            if (V == 1 && a.f <= 4 * 32) return launch_layer_norm<TI, V, V == 1 ? 4 : 16, 16>(a, blocks, s);
+            if (a.f <= 16 * 16) return launch_layer_norm<TI, V, 16, 16>(a, blocks, s);
+            if (a.f <= 16 * 32) return launch_layer_norm<TI, V, 16, 32>(a, blocks, s);
+            if (a.f <= 24 * 32) return launch_layer_norm<TI, V, 24, 32>(a, blocks, s);
+            if (a.f <= 16 * kLayerBlock) return launch_layer_norm<TI, V, 16, kLayerBlock>(a, blocks, s);
+            return launch_layer_norm<TI, V, 16, 512>(a, blocks, s);
         });
     };
-    if (xdt == GNNFD_F32) run(float());
-    else run(__nv_bfloat16());
+    const int rc = xdt == GNNFD_F32 ? run(float()) : run(__nv_bfloat16());
+    if (rc) return rc;
     GNNFD_CUDA_CHECK(cudaGetLastError());
     return GNNFD_OK;
 }

@@ -77,3 +77,25 @@ def test_rows_whose_spread_is_below_the_means_roundings(f):
     off = x - x.mean(1, keepdim=True)
     want = off / ((off ** 2).mean(1, keepdim=True) + 1e-9).sqrt()
     assert float((out - want).abs().max()) <= 200 * U * float(want.abs().max())
+
+
+def test_sums_over_many_rows():
+    """dw and db over 240,000 rows of 1024 columns, 203 for each lane.  Sixteen rows are added up in fp32: a rounding of a sum of k terms of size s is at most evenly spread
+    over u sqrt(k) s, 0.58 of that in the root mean square, and those of 2 to 16 terms together 0.58 sqrt(135) u s = 1.7 u of the sixteen terms' own size, 4 s; terms of
+    either sign keep that proportion to the last sum.  A block's sum and the result are rounded once more (0.58 u each): 1.9 u in all for db.  The
+    terms of dw have errors of their own, 1.3 u: a rounding of the distance, of rstd, of xhat.  (All rows of a lane in fp32: 0.58 sqrt(203 / 2) = 5.8 u at
+    most and 4 u as roundings are usually spread.)"""
+    n, f = 240_000, 1024
+    x, dout = (torch.empty((n, f), device="cuda") for _ in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x.normal_(generator=gen), dout.normal_(generator=gen)
+    _, mean, rstd = g.layer_norm(x, out_dtype=BF16, with_stats=True)
+    _, dw, db = g.layer_norm_backward(dout, x, mean, rstd, out_dtype=BF16)
+    want = torch.zeros((2, f), dtype=torch.float64, device="cuda")
+    for k in range(0, n, 20_000):
+        xs, ds = x[k:k + 20_000].double(), dout[k:k + 20_000].double()
+        off = xs - xs.mean(1, keepdim=True)
+        want[0] += (ds * off / ((off ** 2).mean(1, keepdim=True) + 1e-5).sqrt()).sum(0)
+        want[1] += ds.sum(0)
+    for got, ref, most in ((dw, want[0], 2.5), (db, want[1], 2.0)):
+        assert float((got.double() - ref).pow(2).mean().sqrt()) <= most * U * float(ref.pow(2).mean().sqrt())
