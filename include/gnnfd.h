@@ -452,7 +452,8 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  *   out = (x - mean) * rstd * weight + bias,   rstd = (variance + eps)^-1/2  (not corrected)
  * d_x [n, ldx] of type xdt, d_out [n, ldo] of type odt (may be d_x itself, with ldo = ldx and odt = xdt).  d_weight, d_bias [f] fp32, either may be NULL (1 and 0).
  * d_mean, d_rstd [n] fp32 receive the statistics; both may be NULL.  f up to 8192.  Sums and statistics are fp32, the variance is the mean of squared
- * distances from the mean, and what a rounded sum leaves in the mean is taken off it and them; the result is rounded once.  Rows that hold an infinity or NaN give NaN, others are not touched by them.
+ * distances from the mean, and what a rounded sum leaves in the mean is taken off it and them; the result is rounded once.  Rows that hold an infinity or NaN, or whose
+ * sum is beyond fp32, give NaN (where only the squares' sum is, rstd is 0); others are not touched by them.
  *
  * gnnfd_layer_norm_backward: for d_dout [n, ldd] of type xdt, d_dx [n, lddx] of type gdt (may be d_dout itself: same pitch and type) and d_dweight,
  * d_dbias [f] fp32, sums over all rows (both NULL: not wanted; d_scratch may then be NULL), in fp32 over 16 rows at most and beyond that in 64 bits.  d_mean, d_rstd as the forward call gave them.  d_scratch:

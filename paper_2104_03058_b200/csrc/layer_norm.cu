@@ -327,7 +327,14 @@ __global__ void __launch_bounds__(TEAM < kLayerBlock ? kLayerBlock : TEAM, N > 1
         fetch(row + step);
         add_minus(x, shift);
         scale(x, rstd);
-        if (row < a.n) {                                         // (columns that a lane does not have: d is 0, x what it may)
+        // mean * rstd may be beyond the type's range where all values are the same: 0 times that is no 0
+        if constexpr (N == 4) {                                  // (the third and the fourth column, without a branch: 41 bf16 columns 1 against 6 %)
+            x[2] = 2 * lanes < left ? x[2] : 0.f;
+            x[3] = 3 * lanes < left ? x[3] : 0.f;
+        } else if (!(fabsf(shift[0] * rstd) < INFINITY)) {
+            clear_outside<V>(lanes, left, x);
+        }
+        if (row < a.n) {                                         // (columns that a lane does not have: d is 0, x finite)
             add_all(db, d);
             add_products(dw, d, x);
         }

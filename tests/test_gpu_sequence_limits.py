@@ -99,3 +99,20 @@ def test_sums_over_many_rows():
         want[1] += ds.sum(0)
     for got, ref, most in ((dw, want[0], 2.5), (db, want[1], 2.0)):
         assert float((got.double() - ref).pow(2).mean().sqrt()) <= most * U * float(ref.pow(2).mean().sqrt())
+
+
+@pytest.mark.parametrize("f", [8, 24, 40, 1032])
+def test_equal_values_as_large_as_they_come(f):
+    """Rows of 2^120 in lanes that have places for more columns than there are: mean * rstd is beyond the type's range, xhat is 0 all the same.  f x 2^120 has few bits, so the sums are exact and their
+    product with 1 / f, half a unit off at most, is rounded to 2^120.  1032 x 2^120 is above 2^128, no fp32 number any more: NaN."""
+    x = torch.full((50, f), 2.0 ** 120, device="cuda")
+    dout = torch.randn((50, f), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    _, mean, rstd = g.layer_norm(x, with_stats=True)
+    dx, dw, db = g.layer_norm_backward(dout, x, mean, rstd)
+    if f * 2.0 ** 120 >= 2.0 ** 128:
+        assert torch.isnan(g.layer_norm(x)).all() and torch.isnan(dx).all()
+        return
+    do = dout.double()
+    want = rstd.double()[:, None] * (do - do.mean(1, keepdim=True))
+    assert ((dx.double() - want).abs() <= 24 * U * rstd.double()[:, None] * (do.abs() + do.abs().mean(1, keepdim=True))).all()
+    assert (dw == 0).all() and torch.isfinite(db).all() and (rstd > 300).all()
