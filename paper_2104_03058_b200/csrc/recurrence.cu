@@ -1082,7 +1082,10 @@ __global__ void __launch_bounds__(BACK ? kGradBlock : kRowsBlock) recurrence_row
     Stream<TI, W, P, THREADS, false> stream;
     if constexpr (!BACK) stream.start(ring, a.gate, a.ldg, a.x, a.ldx, (int32_t)r0, most, c);
     const int32_t r1 = min(most, rows_used(a));
-    if (r0 >= r1) return;
+    if (r0 >= r1) {
+        if constexpr (!BACK && !kNarrow<TI, W>) all_but_last<0>();        // (a block does not end with rows on their way into its memory)
+        return;
+    }
     float s[V] = {};
     Graph g;
     if constexpr (BACK) {

@@ -38,6 +38,33 @@ def test_single_tokens_in_place_of_their_states():
         assert g.linear_recurrence(x, gate, graphs=n, initial=state, out=state) is state and torch.equal(state, want)
 
 
+@pytest.mark.parametrize("last", [0, 3, 100, 9_000])
+def test_many_rows_behind_the_last_offset(last):
+    """Most blocks have no rows, but have sent for some before they know: nothing of that shows in their rows, nor in what comes after on the stream."""
+    n, f = 20_000, 64
+    x, dout = scan.rand(n, f, seed=1).contiguous(), scan.rand(n, f, seed=2).contiguous()
+    want = g.layer_norm(x)
+    for form in ("factor", "sigmoid"):
+        gate = scan.gates(form, n, f, seed=3)
+        ptr = torch.tensor([0, last // 3, last], device="cuda")
+        ref = scan.reference(x, gate, form, scan.bounds_of(n, 2, ptr), None, dout)
+        for dtype in (F32, BF16):
+            ins = [t.to(dtype) for t in (x, gate, dout)]
+            if dtype == BF16:
+                ref = scan.reference(ins[0], ins[1], form, scan.bounds_of(n, 2, ptr), None, ins[2])
+            out = torch.full((n, f), 7.0, device="cuda")
+            results = []
+            for _ in range(3):
+                _, final, states = g.linear_recurrence(ins[0], ins[1], form, graph_ptr=ptr, out=out, with_final=True, with_states=True)
+                results.append(g.layer_norm(x))
+            dx, dgate, _ = g.linear_recurrence_backward(ins[2], ins[0], ins[1], states, form, graph_ptr=ptr)
+            assert all(torch.equal(r, want) for r in results) and (out[last:] == 7.0).all()
+            scan.check(out[:last], [t[:last] for t in ref["out"]], "out")
+            scan.check(final, ref["final"], "final")
+            scan.check(dx[:last], [t[:last] for t in ref["dx"]], "dx")
+            scan.check(dgate[:last], [t[:last] for t in ref["dgate"]], "dgate")
+
+
 # ---------------------------------------------------------------- layer norm
 
 @pytest.mark.parametrize("xdt", [F32, BF16])
