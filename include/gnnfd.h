@@ -455,7 +455,7 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * distances from the mean, and what a rounded sum leaves in the mean is taken off it and them; the result is rounded once.  Rows that hold an infinity or NaN, or whose
  * sum is beyond fp32, give NaN (where only the squares' sum is, rstd is 0); others are not touched by them.
  *
- * gnnfd_layer_norm_backward: for d_dout [n, ldd] of type xdt, d_dx [n, lddx] of type gdt (may be d_dout itself: same pitch and type) and d_dweight,
+ * gnnfd_layer_norm_backward: for d_dout [n, ldd] of type xdt, d_dx [n, lddx] of type gdt (may be d_dout itself: same pitch and type; not d_x) and d_dweight,
  * d_dbias [f] fp32, sums over all rows (both NULL: not wanted; d_scratch may then be NULL), in fp32 over 16 rows at most and beyond that in 64 bits.  d_mean, d_rstd as the forward call gave them.  d_scratch:
  * gnnfd_layer_norm_backward_workspace_bytes(n, f) bytes, 256-byte aligned.  The calls only enqueue work. */
 int gnnfd_layer_norm(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f, const float* d_weight, const float* d_bias,
@@ -513,7 +513,7 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * GNNFD_RECURRENCE_FEW_VALUES values).
  *
  * gnnfd_linear_recurrence_backward: for d_dout [n, ldd] of type dt and d_dfinal (fp32 [graphs, f]; NULL: 0), the gradients of out and the last states, d_dx and
- * d_dgate [n, ld*] of type gdt and d_dinitial (fp32 [graphs, f]; NULL: not wanted).  d_states as written by the forward call with the same arguments.  Rows
+ * d_dgate [n, ld*] of type gdt and d_dinitial (fp32 [graphs, f]; NULL: not wanted), none of which overlaps another or what is read.  d_states as written by the forward call with the same arguments.  Rows
  * behind the last offset are left as they are.  Scratch: the same query with backward = 1.
  * GNNFD_TOO_LARGE: more than 2^31 - 65536 rows or 2^20 columns.  The calls only enqueue work. */
 typedef enum { GNNFD_GATE_FACTOR = 0, GNNFD_GATE_SIGMOID = 1 } gnnfd_gate_t;

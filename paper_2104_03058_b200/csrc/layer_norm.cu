@@ -485,6 +485,7 @@ int gnnfd_layer_norm(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt,
     if (rc) return rc;
     if (ldx < f || ldo < f || !(eps >= 0.f) || (d_mean == nullptr) != (d_rstd == nullptr)) return GNNFD_INVALID_ARG;
     if (n > 0 && (!d_x || !d_out)) return GNNFD_INVALID_ARG;
+    if (n > 0 && d_x == d_out && (xdt != odt || (n > 1 && ldx != ldo))) return GNNFD_INVALID_ARG;      // (rows would be written that others still read)
     if (n == 0) return GNNFD_OK;
     LayerArgs a{};
     a.x = d_x; a.out = d_out; a.weight = d_weight; a.bias = d_bias; a.mean = d_mean; a.rstd = d_rstd;
@@ -529,6 +530,7 @@ int gnnfd_layer_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
         a.part = c.take<float>((size_t)(n < kGradBlocks ? n : kGradBlocks) * 2 * f);
         if (!c.ok) return GNNFD_WORKSPACE_TOO_SMALL;
     }
+    if (d_dx == d_x || (d_dx == d_dout && (xdt != gdt || (n > 1 && ldd != lddx)))) return GNNFD_INVALID_ARG;
     a.x = d_x; a.dout = d_dout; a.out = d_dx; a.weight = d_weight;
     a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
     a.n = n; a.ldx = ldx; a.ldd = ldd; a.ldo = lddx; a.f = f; a.inv_f = 1.f / (float)f; a.out_bf16 = gdt == GNNFD_BF16;

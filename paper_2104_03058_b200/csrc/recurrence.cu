@@ -1410,7 +1410,9 @@ int gnnfd_linear_recurrence(int64_t n, const void* d_x, int64_t ldx, const void*
     a.ptr64 = itype == GNNFD_I64; a.out_bf16 = odt == GNNFD_BF16;
     const ScanPlan p = plan_scan(n, f, graphs, !d_graph_ptr, false);
     const int room = scan_scratch(a, p, d_scratch, scratch_bytes);
-    return room ? room : run_scan<false>(a, p, dt, form, static_cast<cudaStream_t>(stream));
+    if (room) return room;
+    if (n > 0 && (d_out == d_x || d_out == d_gate)) return GNNFD_INVALID_ARG;
+    return run_scan<false>(a, p, dt, form, static_cast<cudaStream_t>(stream));
 }
 
 int gnnfd_linear_recurrence_backward(int64_t n, const void* d_dout, int64_t ldd, const void* d_x, int64_t ldx, const void* d_gate, int64_t ldg,
@@ -1431,7 +1433,11 @@ int gnnfd_linear_recurrence_backward(int64_t n, const void* d_dout, int64_t ldd,
     a.length = (int32_t)(n / graphs); a.f = f; a.ptr64 = itype == GNNFD_I64; a.out_bf16 = gdt == GNNFD_BF16;
     const ScanPlan p = plan_scan(n, f, graphs, !d_graph_ptr, true);
     const int room = scan_scratch(a, p, d_scratch, scratch_bytes);
-    return room ? room : run_scan<true>(a, p, dt, form, static_cast<cudaStream_t>(stream));
+    if (room) return room;
+    for (const void* written : {static_cast<const void*>(d_dx), static_cast<const void*>(d_dgate)})
+        if (n > 0 && (written == d_dout || written == d_x || written == d_gate)) return GNNFD_INVALID_ARG;
+    if ((n > 0 && d_dx == d_dgate) || (d_dinitial && d_dinitial == d_dfinal)) return GNNFD_INVALID_ARG;
+    return run_scan<true>(a, p, dt, form, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

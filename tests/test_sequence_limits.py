@@ -67,3 +67,19 @@ def test_the_c_call_refuses_states_in_the_results():
         assert scan(first) == g.INVALID_ARG
     assert scan(P + 64 * 77, ldo=16) == scan(P + 64 * 77 + 60, ldo=16) == scan(P + 16 * 33, odt=1) == scan(P, n=9, graphs=3) == g.INVALID_ARG
     assert scan(P, n=9, graphs=9, odt=1) == scan(P, n=9, graphs=9, ldo=9) == scan(P + 32, n=9, graphs=9) == scan(P, n=9, graphs=9, ptr=5 * P) == g.INVALID_ARG
+
+
+def test_the_c_calls_refuse_results_in_place_of_what_is_still_read():
+    L = g.lib()
+    norm = lambda n=9, ldx=8, xdt=0, out=P, ldo=8, odt=0: L.gnnfd_layer_norm(n, P, ldx, xdt, 8, None, None, 1e-5, out, ldo, odt, None, None, None)      # noqa: E731
+    assert norm(ldo=9) == norm(ldx=9) == norm(odt=1) == norm(xdt=1) == norm(n=1, odt=1) == g.INVALID_ARG
+    back = lambda dx, ldd=8, lddx=8, xdt=0, gdt=0, n=9: (      # noqa: E731
+        L.gnnfd_layer_norm_backward(n, P, ldd, 2 * P, 8, xdt, 8, None, 3 * P, 3 * P, dx, lddx, gdt, None, None, None, 0, None))
+    assert back(P, lddx=9) == back(P, ldd=9) == back(P, gdt=1) == back(P, xdt=1) == back(2 * P) == back(P, n=1, gdt=1) == g.INVALID_ARG
+    scan = lambda out: L.gnnfd_linear_recurrence(9000, P, 8, 2 * P, 8, 0, 8, 1, 1, None, 0, None, out, 8, 0, None, None, 5 * P, 1 << 40, None)      # noqa: E731
+    assert scan(P) == scan(2 * P) == g.INVALID_ARG
+    rev = lambda dx=6 * P, dgate=7 * P, dfinal=None, dinitial=None: (      # noqa: E731
+        L.gnnfd_linear_recurrence_backward(9000, P, 8, 2 * P, 8, 3 * P, 8, 0, 8, 0, 1, None, 0, None, 4 * P, dfinal, dx, 8, dgate, 8, 0, dinitial, 5 * P, 1 << 40, None))
+    for t in (P, 2 * P, 3 * P):
+        assert rev(dx=t) == rev(dgate=t) == g.INVALID_ARG
+    assert rev(dgate=6 * P) == rev(dfinal=8 * P, dinitial=8 * P) == g.INVALID_ARG
