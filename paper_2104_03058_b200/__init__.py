@@ -9,14 +9,16 @@ from . import build  # noqa: F401
 
 
 def __getattr__(name):
-    # the binding is imported on first use so that the package can be imported before the library is built
+    # The binding is imported on first use so that the package can be imported before the library is built; from then on its name is here.  (Names are not
+    # kept here, so that one replaced there is seen; asking import_module each time took 1 to 2 us of a call's 10.)
+    try:
+        return getattr(binding, name)
+    except (NameError, AttributeError):
+        pass
     if name.startswith("__") or name == "binding":
         raise AttributeError(name)
-    binding = importlib.import_module(__name__ + ".binding")
+    module = importlib.import_module(__name__ + ".binding")
     try:
-        value = getattr(binding, name)
+        return getattr(module, name)
     except AttributeError:
         raise AttributeError("module %r has no attribute %r" % (__name__, name)) from None
-    if callable(value):
-        globals()[name] = value         # found without this detour from the next call on (1 to 2 us of a call's 10)
-    return value

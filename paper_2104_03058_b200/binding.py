@@ -1033,12 +1033,13 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     wp, bp = _column_values(x, f, "weight", weight), _column_values(x, f, "bias", bias)
     if out is None:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
+        op, ldo = out.data_ptr(), f
     else:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
         if not _same_place(x, out):
             _no_overlap(x, out, "x", "out")
-    op, ldo = _matrix(out, f, "out")
+        op, ldo = _matrix(out, f, "out")
     mean = rstd = mp = rp = None
     if with_stats:
         mean, rstd = _new(x, (2, n), torch.float32, stream)
@@ -1083,13 +1084,14 @@ def layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, mean: torch.Tensor,
     mp, rp = _column_values(x, n, "mean", mean), _column_values(x, n, "rstd", rstd)
     if out is None:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
+        op, ldo = out.data_ptr(), f
     else:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
         _no_overlap(x, out, "x", "out")
         if not _same_place(dout, out):
             _no_overlap(dout, out, "dout", "out")
-    op, ldo = _matrix(out, f, "out")
+        op, ldo = _matrix(out, f, "out")
     dweight = dbias = dwp = dbp = None
     if with_params:
         dweight, dbias = _new(x, (2, f), torch.float32, stream)
@@ -1137,12 +1139,13 @@ def rotary(x: torch.Tensor, freq: torch.Tensor, heads: int, dim: int, positions:
             raise ValueError("positions must hold a position for each of the %d rows, on %s" % (n, x.device))
     if out is None:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
+        op, ldo = out.data_ptr(), f
     else:
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
         if not _same_place(x, out):
             _no_overlap(x, out, "x", "out")
-    op, ldo = _matrix(out, f, "out")
+        op, ldo = _matrix(out, f, "out")
     _check(lib().gnnfd_rotary(n, xp, ldx, _dtype_code(x), heads, dim, 2 * freq.shape[0], int(interleaved), pp, itype, freq.data_ptr(), scale,
                               int(inverse), op, ldo, _dtype_code(out), _stream_handle(index, stream)), "gnnfd_rotary")
     return out
@@ -1210,8 +1213,9 @@ def linear_recurrence(x: torch.Tensor, gate: torch.Tensor, form: str = "sigmoid"
     fresh = out is None
     if fresh:
         out = _new(x, (n, f), out_dtype or torch.float32, stream)
-    op, ldo = _matrix(out, f, "out")
-    if not fresh:
+        op, ldo = out.data_ptr(), f
+    else:
+        op, ldo = _matrix(out, f, "out")
         _same_device(x.device, out=out)
         _need_rows_of(out, n, "out")
         _no_overlap(x, out, "x", "out")

@@ -83,3 +83,15 @@ def test_the_c_calls_refuse_results_in_place_of_what_is_still_read():
     for t in (P, 2 * P, 3 * P):
         assert rev(dx=t) == rev(dgate=t) == g.INVALID_ARG
     assert rev(dgate=6 * P) == rev(dfinal=8 * P, dinitial=8 * P) == g.INVALID_ARG
+
+
+def test_the_package_has_what_its_binding_has_now(monkeypatch):
+    """A function that is replaced in the binding after its first use through the package (a tracer's wrapper) is what the package gives from then on."""
+    was = g.rotary_frequencies
+    assert was(8, device="cpu").shape == (4,) and was is b.rotary_frequencies
+    with monkeypatch.context() as m:
+        m.setattr(b, "rotary_frequencies", lambda *args, **kwargs: "wrapped")
+        assert g.rotary_frequencies(8, device="cpu") == "wrapped"
+    assert g.rotary_frequencies is was
+    with pytest.raises(AttributeError, match="no attribute 'rotary_frequency'"):
+        g.rotary_frequency
