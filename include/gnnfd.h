@@ -507,7 +507,8 @@ int gnnfd_rotary(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int
  * inside: nothing outside of the arrays is touched.  d_x, d_gate [n, ld] of type dt, d_out [n, ldo] of type odt, not overlapping them nor d_initial (a
  * copy of the last row of a stretch that goes on in the same buffer will do; for single tokens, graphs = n without d_graph_ptr, d_initial may be d_out itself, fp32 with ldo = f).  d_final (fp32
  * [graphs, f], may be NULL) receives the last state of each graph; it may be d_initial itself where graphs = n and d_graph_ptr is NULL, and does not overlap it otherwise.  d_states
- * (may be NULL): fp32 [(n + 7) / 8, f], states that the gradient starts from.  States and products of gates are fp32 or wider.
+ * (may be NULL): fp32 [(n + 7) / 8, f], states that the gradient starts from.  States and products of gates are fp32 or wider; of
+ * sigmoid gates a and 1 - a are within (10 + |gate| / 20) * 2^-24 of themselves (a above 2^-100).
  * d_scratch: gnnfd_linear_recurrence_workspace_bytes(n, f, graphs, d_graph_ptr == NULL, 0) bytes, 256-byte aligned (0
  * and NULL for up to GNNFD_RECURRENCE_FEW_ROWS rows, in the gradient half as many and of up to
  * GNNFD_RECURRENCE_FEW_VALUES values).

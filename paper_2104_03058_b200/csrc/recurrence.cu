@@ -68,16 +68,33 @@ __device__ __forceinline__ float smaller_or_nan(float x, float y)
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
     return z;
 }
+// e^g of t = g log2 e, for t up to 126: 2^t (1 + r) with r what the rounding of t leaves out, up to |g| 2^-24, found from the product back (log 2 in 32 bits is off
+// by 0.05 * 2^-24 for each unit of g).  t may have been cut at 126; where it is that large or infinite it is taken as it is.
+template <int V>
+__device__ __forceinline__ void exp_of(const float (&g)[V], float (&t)[V])
+{
+    float r[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = g[i];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) fma_pairs(r[i], r[i + 1], t[i], t[i + 1], -0.693147181f, -0.693147181f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float e = power_of_2(t[i]);
+        t[i] = fabsf(t[i]) < 125.9f ? fmaf(e, r[i], e) : e;
+    }
+}
 // a and 1 - a of a = 1 / (1 + e^-g), neither by subtraction, and `small`, the smaller one with g's sign, from which `sigmoid_parts` has both again
 template <int V>
 __device__ __forceinline__ void sigmoid_of(const float (&g)[V], float (&a)[V], float (&rest)[V], float (&small)[V])
 {
-    float t[V];
+    float size[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) t[i] = g[i];
-    scale(t, 1.4426950408889634f);
+    for (int i = 0; i < V; ++i) small[i] = size[i] = -fabsf(g[i]);
+    scale(small, 1.4426950408889634f);
+    exp_of(size, small);
 #pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = small[i] = power_of_2(-fabsf(t[i]));
+    for (int i = 0; i < V; ++i) a[i] = small[i];
     const float one[1] = {-1.f};
     add_minus(a, one);
 #pragma unroll
@@ -104,12 +121,15 @@ __device__ __forceinline__ void steps_of(const float (&g)[V], const float (&x)[V
     if constexpr (SIGMOID) {
         // e = e^-g up to 2^126, a = 1 / (1 + e), 1 - a = e a, without a choice by sign.  Gates below -87, where e is cut, have a = 2^-126: taken off, so that a gate
         // of -infinity keeps nothing (for others it is below a rounding down to 2^-102).
-        float e[V];
+        float e[V], minus[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = g[i];
-        scale(e, -1.4426950408889634f);
+        for (int i = 0; i < V; ++i) e[i] = minus[i] = -g[i];
+        scale(e, 1.4426950408889634f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = e[i] = power_of_2(smaller_or_nan(e[i], 126.f));
+        for (int i = 0; i < V; ++i) e[i] = smaller_or_nan(e[i], 126.f);
+        exp_of(minus, e);
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = e[i];
         const float one[1] = {-1.f}, least[1] = {1.17549435e-38f};
         add_minus(a, one);
 #pragma unroll

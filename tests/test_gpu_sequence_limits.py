@@ -65,6 +65,32 @@ def test_many_rows_behind_the_last_offset(last):
             scan.check(dgate[:last], [t[:last] for t in ref["dgate"]], "dgate")
 
 
+@pytest.mark.parametrize("how", ["length", "offsets"])
+@pytest.mark.parametrize("n,f", [(3, 5), (900, 64), (900, 33), (9_000, 64), (9_000, 31), (40_000, 512)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_sigmoid_gates_weights_at_any_size(dtype, n, f, how):
+    """Graphs of one row: a is what is left of a state of 1 where x is 0, 1 - a what comes of x = 1 where there is no state, a of a gradient of 1 behind the state, 1 - a
+    in front of x and a (1 - a) in front of the gate.  Relative to themselves: 4 u for the exponential, 1 u for the product that mends its argument, 0.05 u |gate| for log 2
+    in 32 bits, 1 u for adding 1, 3 u for the reciprocal, 1 u for a product; gates up to 69, so that a is above 2^-100.  dgate has two such weights and three products."""
+    gen = torch.Generator(device="cuda").manual_seed(n + f)
+    gate = ((torch.rand((n, f), generator=gen, device="cuda") - 0.5) * 138).to(dtype)
+    batch = dict(graphs=n) if how == "length" else dict(graph_ptr=torch.arange(n + 1, device="cuda"))
+    zero, one, state = torch.zeros_like(gate), torch.ones_like(gate), torch.ones((n, f), device="cuda")
+    a, rest = torch.sigmoid(gate.double()), torch.sigmoid(-gate.double())
+    bound = (0.05 * gate.double().abs() + 10) * U
+
+    def near(got, want, times=1.0, more=0.0):
+        assert (((got.double() / want) - 1).abs() <= times * bound + more * U).all(), float(((got.double() / want - 1).abs() / U).max())
+
+    out, _, states = g.linear_recurrence(zero, gate, initial=state, with_final=True, with_states=True, **batch)
+    near(out, a)
+    near(g.linear_recurrence(one, gate, **batch), rest)
+    dx, dgate, dinitial = g.linear_recurrence_backward(one, zero, gate, states, initial=state, **batch)
+    near(dx, rest)
+    near(dinitial, a)
+    near(dgate, a * rest, 2.0, 3.0)
+
+
 # ---------------------------------------------------------------- layer norm
 
 @pytest.mark.parametrize("xdt", [F32, BF16])
