@@ -485,7 +485,8 @@ int gnnfd_layer_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  *   GNNFD_ROTARY_POSITION  divided by factor (positions are squeezed),
  *   GNNFD_ROTARY_BASE      with base * factor^(rotary_dim / (rotary_dim - 2)): the last frequency is divided by factor, the first stays (rotary_dim > 2),
  *   GNNFD_ROTARY_RAMP      divided by factor where a frequency makes fewer than low_turns turns over `length` positions, kept where it makes more than
- *                          high_turns, in between kept * freq + (1 - kept) * freq / factor with kept = (turns - low_turns) / (high_turns - low_turns). */
+ *                          high_turns, in between kept * freq + (1 - kept) * freq / factor with kept = (turns - low_turns) / (high_turns - low_turns).
+ * GNNFD_INVALID_ARG where a frequency is beyond fp64. */
 typedef enum { GNNFD_ROTARY_NONE = 0, GNNFD_ROTARY_POSITION = 1, GNNFD_ROTARY_BASE = 2, GNNFD_ROTARY_RAMP = 3 } gnnfd_rotary_scaling_t;
 
 int gnnfd_rotary_frequencies(int32_t rotary_dim, double base, int scaling, double factor, int64_t length, double low_turns, double high_turns,

@@ -288,15 +288,16 @@ int gnnfd_rotary_frequencies(int32_t rotary_dim, double base, int scaling, doubl
     if (scaling < GNNFD_ROTARY_NONE || scaling > GNNFD_ROTARY_RAMP || rotary_dim > kRotaryPart) return GNNFD_UNSUPPORTED;
     if (scaling == GNNFD_ROTARY_BASE && rotary_dim < 4) return GNNFD_INVALID_ARG;
     if (scaling == GNNFD_ROTARY_RAMP && (length <= 0 || !(low_turns >= 0.0) || !(high_turns > low_turns) || isinf(high_turns))) return GNNFD_INVALID_ARG;
-    if (scaling == GNNFD_ROTARY_BASE) base *= pow(factor, (double)rotary_dim / (rotary_dim - 2));
     for (int i = 0; i < rotary_dim / 2; ++i) {
         double w = pow(base, -2.0 * i / rotary_dim);
+        if (scaling == GNNFD_ROTARY_BASE) w *= pow(factor, -2.0 * i / (rotary_dim - 2));        // (the base itself may have a power beyond the type)
         if (scaling == GNNFD_ROTARY_POSITION) w /= factor;
         if (scaling == GNNFD_ROTARY_RAMP) {
             double kept = (w * (double)length / 6.283185307179586 - low_turns) / (high_turns - low_turns);
             kept = kept < 0.0 ? 0.0 : kept > 1.0 ? 1.0 : kept;
             w *= kept + (1.0 - kept) / factor;
         }
+        if (!isfinite(w)) return GNNFD_INVALID_ARG;
         freq[i] = w;
     }
     return GNNFD_OK;

@@ -95,3 +95,18 @@ def test_the_package_has_what_its_binding_has_now(monkeypatch):
     assert g.rotary_frequencies is was
     with pytest.raises(AttributeError, match="no attribute 'rotary_frequency'"):
         g.rotary_frequency
+
+
+def test_frequencies_of_factors_of_any_size():
+    """The last frequency is divided by factor also where factor^(r / (r - 2)) has no number in 64 bits; frequencies that have none are refused."""
+    for r in (4, 8, 64):
+        plain = g.rotary_frequencies(r, 1e4, device="cpu")
+        for factor in (1e-200, 1e-150, 0.25, 8.0, 1e160, 1e200):
+            got = g.rotary_frequencies(r, 1e4, "base", factor, device="cpu")
+            assert got[0] == 1.0 and abs(float(got[-1]) / (float(plain[-1]) / factor) - 1) <= 2.0 ** -48
+            steps = got[1:] / got[:-1]
+            assert float((steps / steps[0] - 1).abs().max()) <= 2.0 ** -40          # a geometric series
+    for scaling in ("position", "base"):
+        with pytest.raises(g.GnnfdError) as err:
+            g.rotary_frequencies(8, 1e4, scaling, 1e-320, device="cpu")
+        assert err.value.status == g.INVALID_ARG
