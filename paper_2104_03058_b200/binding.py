@@ -150,6 +150,8 @@ def _matrix(t: torch.Tensor, cols: int, name: str):
     if t.is_cuda and t.dim() == 2:
         (rows, width), (pitch, step) = t.shape, t.stride()
         if width >= cols and (width <= 1 or step == 1):
+            if cols > 0x7fffffff:
+                raise ValueError("%s has more than 2^31 - 1 columns" % name)          # (the library's counters of columns are 32 bits)
             return t.data_ptr(), pitch if rows > 1 else max(pitch, width)
     raise ValueError("%s must be a 2-D CUDA tensor with unit column stride and >= %d columns" % (name, cols))
 

@@ -1,4 +1,6 @@
 """What the layer norm, rotary and recurrence calls refuse or accept at their limits: host logic, before any launch."""
+from types import SimpleNamespace
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -110,3 +112,15 @@ def test_frequencies_of_factors_of_any_size():
         with pytest.raises(g.GnnfdError) as err:
             g.rotary_frequencies(8, 1e4, scaling, 1e-320, device="cpu")
         assert err.value.status == g.INVALID_ARG
+
+
+def test_columns_beyond_32_bits_are_refused():
+    """A single row of 2^32 + 8 columns is no row of 8."""
+    def row(width):
+        return SimpleNamespace(is_cuda=True, dim=lambda: 2, shape=(1, width), stride=lambda: (width, 1), data_ptr=lambda: P)
+
+    for width in (1 << 31, (1 << 32) + 8):
+        with pytest.raises(ValueError, match="columns"):
+            b._matrix(row(width), width, "x")
+    assert b._matrix(row(1 << 32), 8, "x") == (P, 1 << 32)
+    assert b._matrix(row((1 << 31) - 1), (1 << 31) - 1, "x") == (P, (1 << 31) - 1)
