@@ -91,6 +91,50 @@ def test_a_sigmoid_gates_weights_at_any_size(dtype, n, f, how):
     near(dgate, a * rest, 2.0, 3.0)
 
 
+@pytest.mark.parametrize("n,f", [(2_000_003, 4), (1_500_000, 5), (1_000_001, 128)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_exact_sums_over_millions_of_rows(sign, n, f):
+    """Factors of 1 (or -1) add up (or alternate): of small whole numbers, one in ten not 0, every sum and every product of two is below 2^24 and thus exact, whatever
+    the joints, of which there are some thousand tiles of chunks."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    some = lambda: torch.randint(-10, 11, (n, f), generator=gen, device="cuda", dtype=torch.int8)      # noqa: E731
+    x, dout = ((t == 9).float() - (t == -9).float() for t in (some(), some()))
+    ptr = torch.tensor([0, n // 3, n // 3, n - 7, n], device="cuda")
+    initial, dfinal = torch.full((4, f), 5.0, device="cuda"), torch.full((4, f), -3.0, device="cuda")
+    turn = torch.where(torch.arange(n, device="cuda") % 2 == 0, 1, int(sign))[:, None].double()
+    h, before, total = (torch.empty((n, f), device="cuda") for _ in range(3))
+    final, dinitial = [], []
+    for b, (r0, r1) in enumerate(scan.bounds_of(n, 4, ptr)):
+        w, first = turn[r0:r1], initial[b].double()
+        if r0 == r1:
+            final.append(initial[b]), dinitial.append(dfinal[b])
+            continue
+        # h[t] w[t] = first w[r0] sign + the sum of x w so far; the gradients the same from the end
+        start = first * w[0] * sign
+        sums = start + (x[r0:r1].double() * w).cumsum(0)
+        h[r0:r1] = (sums * w).float()
+        before[r0], before[r0 + 1:r1] = initial[b], h[r0:r1 - 1]
+        back = dfinal[b].double() * w[-1] + (dout[r0:r1].double() * w).flip(0).cumsum(0).flip(0)
+        total[r0:r1] = (back * w).float()
+        final.append(h[r1 - 1]), dinitial.append(sign * total[r0])
+    out, last, states = g.linear_recurrence(x, torch.full_like(x, sign), "factor", graph_ptr=ptr, initial=initial, with_final=True, with_states=True)
+    assert torch.equal(out, h) and torch.equal(last, torch.stack(final))
+    dx, dgate, dfirst = g.linear_recurrence_backward(dout, x, torch.full_like(x, sign), states, "factor", graph_ptr=ptr, initial=initial, dfinal=dfinal)
+    assert torch.equal(dx, total) and torch.equal(dgate, total * before) and torch.equal(dfirst, torch.stack(dinitial))
+    assert float(total.abs().max()) * float(before.abs().max()) < 2.0 ** 24
+
+
+@pytest.mark.parametrize("form", ["factor", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,graphs,f", [(1_200_000, 1000, 16), (60_000, 60, 256), (150_000, 150, 41)])
+def test_longer_batches(n, graphs, f, dtype, form):
+    """Tiles by the thousand going back, and threads of eight bf16 columns."""
+    length = n // graphs
+    jitter = torch.randint(-length // 2, length // 2, (graphs - 1,), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    ptr = torch.cat([jitter.new_zeros(1), torch.arange(1, graphs, device="cuda") * length + jitter, jitter.new_full((1,), n)])
+    scan.both_ways(n, f, form, ptr=ptr, xdt=dtype, odt=dtype)
+
+
 # ---------------------------------------------------------------- layer norm
 
 @pytest.mark.parametrize("xdt", [F32, BF16])
