@@ -17,8 +17,9 @@
 // What counts beside the bytes is instructions: arithmetic is done on two elements at a time, addresses are a lane's base and constants, and columns that a lane
 // does not have are registers set to 0 once.  (The gradient of 233 k x 602 fp32, in vectors of two: 58 instructions an element and 452 us with the checks inside,
 // 17 and 287 us without; the weights in shared memory instead of registers leave room for twice the warps, 64 to 512 columns 255 -> 200 us for 400 MB a tensor.)
-// Measured, 400 MB a tensor, fp32 / bf16: forward 0.87 - 0.97 of the copy peak, gradient 0.90 - 0.99 / 0.81 - 0.92 from 64 columns on; bf16 rows of 600 columns
-// 0.75 and 0.68 (a quarter of the lanes' places are empty), odd numbers of bf16 columns 0.3 to 0.6 (elements of 2 bytes one by one).
+// Measured, 400 MB a tensor: 64 to 4096 fp32 columns in fours 0.84 - 0.97 of the copy peak forward, 0.89 - 0.99 in the gradient; 64 to 8192 bf16 columns in eights 0.84 - 0.94
+// and 0.75 - 0.91, but 600 columns 0.75 and 0.66 (a quarter of the lanes' places are empty).  41 fp32 columns 0.51 and 0.62, 41 and 301 bf16 columns 0.27 to 0.58
+// (elements of 2 bytes one by one), 4100 columns 0.48 to 0.74 (one block of nine warps an SM).
 #include <math.h>
 
 #include <type_traits>
