@@ -456,8 +456,8 @@ int gnnfd_group_norm_backward(int64_t n, const void* d_dout, int64_t ldd, const 
  * sum is beyond fp32, give NaN (where only the squares' sum is, rstd is 0); others are not touched by them.
  *
  * gnnfd_layer_norm_backward: for d_dout [n, ldd] of type xdt, d_dx [n, lddx] of type gdt (may be d_dout itself: same pitch and type; not d_x) and d_dweight,
- * d_dbias [f] fp32, sums over all rows (both NULL: not wanted; d_scratch may then be NULL), in fp32 over 16 rows at most and beyond that in 64 bits.  d_mean, d_rstd as the forward call gave them.  d_scratch:
- * gnnfd_layer_norm_backward_workspace_bytes(n, f) bytes, 256-byte aligned.  The calls only enqueue work. */
+ * d_dbias [f] fp32, sums over all rows (both NULL: not wanted; d_scratch may then be NULL), in fp32 over 16 rows at most and beyond that in 64 bits.  d_mean, d_rstd as the forward call gave
+ * them, so distances from the mean are those from its fp32 value.  d_scratch: gnnfd_layer_norm_backward_workspace_bytes(n, f) bytes, 256-byte aligned.  The calls only enqueue work. */
 int gnnfd_layer_norm(int64_t n, const void* d_x, int64_t ldx, gnnfd_dtype_t xdt, int32_t f, const float* d_weight, const float* d_bias,
                      float eps, void* d_out, int64_t ldo, gnnfd_dtype_t odt, float* d_mean, float* d_rstd, void* stream);
 
